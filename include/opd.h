@@ -40,7 +40,7 @@
 extern "C" {
 #endif
 
-#define OPD_VERSION 5
+#define OPD_VERSION 6
 /* Largest cached support size k, and largest sample count M. */
 #define OPD_K_MAX 256
 
@@ -49,13 +49,13 @@ typedef enum opd_status {
   OPD_ERR_NULL = -1,      /* a pointer the estimator needs is NULL */
   OPD_ERR_SHAPE = -2,     /* N < 0, V < 2, V >= 2^31, or ld < V */
   OPD_ERR_SUPPORT = -3,   /* k or M outside [1, min(V, OPD_K_MAX)], or RKL_MC1 with M != 1 */
-  OPD_ERR_DTYPE = -4,     /* unknown logits or dlogits dtype */
+  OPD_ERR_DTYPE = -4,     /* unknown logits or dlogits dtype, or scale type */
   OPD_ERR_ALIGN = -5,     /* a logit/gradient pointer or row stride is not 16-byte aligned */
   OPD_ERR_WORKSPACE = -6, /* split-vocabulary path forced with a missing or short workspace */
   OPD_ERR_ESTIMATOR = -7, /* unknown estimator */
   OPD_ERR_FLAGS = -8,     /* unknown or contradictory flag bits */
   OPD_ERR_HIP = -9,       /* a HIP runtime call or kernel launch failed */
-  OPD_ERR_PARAM = -10,    /* invalid scalar option (clip_eps of a clipped estimator), or
+  OPD_ERR_PARAM = -10,    /* invalid scalar option (clip_eps of a clipped estimator, block_rows), or
                              coverage_out for an estimator without a cached support */
   OPD_ERR_SCRATCH = -11   /* opd_loss_fwd_bwd_noalloc: the call needs more scratch than
                              OPD_NOALLOC_SCRATCH_BYTES */
@@ -344,6 +344,106 @@ int opd_topk_support(const void* logits, int32_t dtype, int64_t N, int64_t V, in
 int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t ld,
                       const int32_t* ids, int32_t K, const uint8_t* mask, float* logp,
                       float* lse_out, void* stream);
+
+/*
+ * The rows of logits (Sec. 4.1: Stage 1 draws from the rollout policy's rows,
+ * Stage 2 scores on the teacher's): the product of hidden states and an output
+ * head in 8-bit floating point, and the quantisation of both.  They serve
+ * Stages 1 and 2, which have no backward pass.
+ *
+ * 8-bit values are OCP e4m3 (no infinities, largest 448, NaN 0x7F / 0xFF).  A
+ * scale covers a block of 128 consecutive columns: [0, 128), [128, 256), ..; the
+ * last block of a row may be shorter.  nb = ceil(H / 128).  Scales are fp32
+ * (OPD_SCALE_F32) or powers of two held as OCP e8m0 (OPD_SCALE_E8M0: one byte,
+ * the exponent plus 127; 255 is NaN), which the matrix cores apply themselves.
+ *
+ * opd_quantize_blocks: blocks of block_rows (1 for hidden states, 128 for head
+ *   weights) rows by 128 columns, cut at the edges of x [N, H].  With a the
+ *   largest magnitude in the block, the scale s is max(a / 448, 2^-126) in fp32,
+ *   or the least power of two that is not below a / 448 (2^-127 at least), and
+ *   q = x / s, divided in fp32 and rounded to the nearest e4m3 value, ties to
+ *   even.  A block that holds a NaN or an infinity gets a NaN scale and values.
+ *     x [N, ldx] OPD_F32 or OPD_BF16; q [N, ldq] bytes, columns [H, ldq) are not
+ *     written; scales [ceil(N / block_rows), nb].
+ *   x and q are 16-byte aligned, ldx * element_size and ldq multiples of 16.
+ *
+ * opd_head_logits: logits[n, v] = sum_b sx[n, b] sw[v / 128, b] *
+ *   sum_{h in block b} x[n, h] w[v, h], in fp32 (products of 8-bit values are
+ *   exact), rounded once to logits_dtype (OPD_F32 or OPD_BF16).  A NaN in a
+ *   token's values or scales reaches its own row only, one in the weights its
+ *   own vocabulary entries (a scale: those of its block).
+ *     x [N, ldx], x_scales [N, nb]; w [V, ldw], w_scales [ceil(V / 128), nb];
+ *     logits [N, ld], as every call here reads them; columns [V, ld) are not
+ *     written.
+ *   x, w and logits are 16-byte aligned; ldx, ldw and ld * element_size are
+ *   multiples of 16.  Bytes [H, ldx) and [H, ldw) of the rows are not read.
+ *
+ * Errors: OPD_ERR_DTYPE (dtype or scale_type), OPD_ERR_SHAPE (N < 0, N or V >=
+ * 2^31, H outside [1, 2^24], V < 2, a row stride below its row's length),
+ * OPD_ERR_PARAM (block_rows not 1 or 128), OPD_ERR_ALIGN, OPD_ERR_NULL,
+ * OPD_ERR_HIP.  N == 0 is a no-op returning OPD_OK.
+ */
+typedef enum opd_scale { OPD_SCALE_F32 = 0, OPD_SCALE_E8M0 = 1 } opd_scale;
+
+int opd_quantize_blocks(const void* x, int32_t dtype, int64_t N, int64_t H, int64_t ldx,
+                        int32_t block_rows, int32_t scale_type, void* q, int64_t ldq,
+                        void* scales, void* stream);
+int opd_head_logits(const void* x, int64_t ldx, const void* x_scales, const void* w, int64_t ldw,
+                    const void* w_scales, int32_t scale_type, int64_t N, int64_t V, int64_t H,
+                    int32_t logits_dtype, void* logits, int64_t ld, void* stream);
+
+/*
+ * Verification of drafted tokens: Stage 1 with a drafter.  B sequences have up
+ * to D drafted tokens each; the rollout policy's rows of logits at all of them,
+ * and the one after, are at hand.  With p_i = softmax of target row i, q_i that of
+ * draft row i, x_i the drafted token and u the uniforms (supplied by the caller,
+ * as for opd_sample_actions), token i is kept while u[i] q_i(x_i) < p_i(x_i).  At
+ * the first that is not, one token is drawn from max(p_i - q_i, 0) divided by
+ * its sum; if all n are kept, from p_n.  If the drafts are draws from q, the
+ * tokens that come out are draws from p, whatever q is.
+ *
+ * The draw is by inversion in index order at u[D]: the first index at which the
+ * cumulative mass exceeds u[D] times the whole.  Tests and draw are evaluated in
+ * double precision, so they are those of exact arithmetic unless a uniform lies
+ * within about 1e-13 of a border.  Where a token is refused and rounding leaves
+ * no residual at all (p and q are equal to double precision but for it), the
+ * draw is from p.
+ *
+ *   target_logits  [B * (D + 1), ld], sequence b's rows b (D + 1) .. b (D + 1) + D
+ *   draft_logits   [B * D, draft_ld], nullable, of the same dtype: NULL means
+ *                  that the drafter is certain of its tokens (q_i is 1 at x_i,
+ *                  as for drafts copied from the prompt)
+ *   draft_ids      [B, D] int32
+ *   draft_lens     [B] int32, nullable (NULL: all D): sequence b has drafts
+ *                  [0, draft_lens[b]) and target rows [0, draft_lens[b]]; the
+ *                  others are not read.  0 is a plain draw.
+ *   uniforms       [B, D + 1] fp32 in [0, 1)
+ *   mask           [B] uint8, nullable; a masked sequence (0) is not read
+ *   accepted       [B] int32 out: the drafted tokens that were kept
+ *   ids            [B, D + 1] int32 out: those, then the drawn token, then -1
+ *   logp           [B, D + 1] fp32 out, nullable: log p at these tokens (what
+ *                  the MC estimators read as behav_logp), 0 past them
+ *   workspace      16-byte aligned, opd_verify_workspace_bytes(...) bytes
+ * Rows behind the first refusal have no part in the results and may stay unread.
+ * Masked sequences get accepted 0, ids -1 and logp 0.  A sequence ends with id -1
+ * and logp NaN, in place of the drawn token, at the first position whose
+ * target row (or draft row, where its token is tested) has a NaN or +inf logit or
+ * no finite one, whose uniform is outside [0, 1) or whose drafted id is outside
+ * [0, V); and at position 0 if draft_lens[b] is outside [0, D].
+ *
+ * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (B < 0, B (D + 1) >= 2^31, V or a stride
+ * out of range), OPD_ERR_SUPPORT (D outside [1, OPD_K_MAX]), OPD_ERR_ALIGN,
+ * OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  B == 0 is a no-op returning
+ * OPD_OK.
+ */
+int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32_t dtype,
+                      int64_t B, int32_t D, int64_t V, int64_t ld, int64_t draft_ld,
+                      const int32_t* draft_ids, const int32_t* draft_lens, const float* uniforms,
+                      const uint8_t* mask, int32_t* accepted, int32_t* ids, float* logp,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of opd_verify_drafts (0 for invalid arguments). */
+size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype);
 
 /*
  * Diagnostics of the Monte-Carlo estimator: the importance-ratio tail that

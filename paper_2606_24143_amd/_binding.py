@@ -8,6 +8,7 @@ calls fail loudly.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -39,7 +40,8 @@ STATUS = {0: "OPD_OK", -1: "OPD_ERR_NULL", -2: "OPD_ERR_SHAPE", -3: "OPD_ERR_SUP
 EXPORTS = ("opd_loss_fwd_bwd", "opd_loss_fwd_bwd_noalloc", "opd_noalloc_scratch_bytes",
            "opd_workspace_bytes", "opd_validate_cache", "opd_sample_actions",
            "opd_topk_support", "opd_score_actions", "opd_mc_diag_workspace_bytes",
-           "opd_mc_diagnostics", "opd_status_string", "opd_version")
+           "opd_mc_diagnostics", "opd_quantize_blocks", "opd_head_logits", "opd_verify_drafts",
+           "opd_verify_workspace_bytes", "opd_status_string", "opd_version")
 
 
 class OpdError(RuntimeError):
@@ -104,6 +106,15 @@ def lib():
                                          P, i32, i64, ctypes.POINTER(OpdMcDiag), P,
                                          ctypes.c_size_t, P]
         L.opd_mc_diagnostics.restype = ctypes.c_int
+        L.opd_quantize_blocks.argtypes = [P, i32, i64, i64, i64, i32, i32, P, i64, P, P]
+        L.opd_quantize_blocks.restype = ctypes.c_int
+        L.opd_head_logits.argtypes = [P, i64, P, P, i64, P, i32, i64, i64, i64, i32, P, i64, P]
+        L.opd_head_logits.restype = ctypes.c_int
+        L.opd_verify_workspace_bytes.argtypes = [i64, i32, i64, i32]
+        L.opd_verify_workspace_bytes.restype = ctypes.c_size_t
+        L.opd_verify_drafts.argtypes = [P, P, i32, i64, i32, i64, i64, i64, P, P, P, P, P, P, P, P,
+                                        ctypes.c_size_t, P]
+        L.opd_verify_drafts.restype = ctypes.c_int
         L.opd_status_string.argtypes = [ctypes.c_int]
         L.opd_status_string.restype = ctypes.c_char_p
         L.opd_version.restype = ctypes.c_int
@@ -430,6 +441,175 @@ def score_actions(logits: torch.Tensor, ids: torch.Tensor, *, mask=None, want_ls
     out = {"logp": logp}
     if lse is not None:
         out["lse"] = lse
+    return out
+
+
+# ---------------------------------------------------------------- rows of logits
+
+@contextlib.contextmanager
+def _on(dev: torch.device, stream):
+    """Launches and allocations on the tensors' device and the given stream (or
+    that device's current one): what is allocated inside belongs to that stream."""
+    if stream is not None and stream.device != dev:
+        raise ValueError("stream is on %s, the tensors on %s" % (stream.device, dev))
+    with torch.cuda.device(dev):
+        if stream is None:
+            yield ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        else:
+            with torch.cuda.stream(stream):
+                yield ctypes.c_void_p(stream.cuda_stream)
+
+
+BLOCK = 128  # columns of a block of 8-bit values (opd_quantize_blocks)
+_SCALES = {torch.float32: 0, torch.float8_e8m0fnu: 1}  # opd_scale
+
+
+def _blocks(n: int, size: int) -> int:
+    return (n + size - 1) // size
+
+
+def _need_stride(t: torch.Tensor, name: str) -> int:
+    """The row stride of a 2-D tensor of 8-bit values (or of hidden states), a
+    multiple of 16 bytes."""
+    ld = t.stride(0) if t.shape[0] > 1 else _blocks(t.shape[1] * t.element_size(), 16) * 16 // \
+        t.element_size()
+    if ld < t.shape[1] or ld * t.element_size() % 16 != 0 or t.data_ptr() % 16 != 0:
+        raise ValueError("%s must have 16-byte aligned rows" % name)
+    return ld
+
+
+def _need_scales(s, t: torch.Tensor, name: str, rows: int):
+    """Scales of t's blocks of `rows` rows."""
+    _need(s, name, tuple(_SCALES), (_blocks(t.shape[0], rows), _blocks(t.shape[1], BLOCK)),
+          t.device)
+
+
+def quantize_blocks(x: torch.Tensor, *, block_rows: int = 1, scale_dtype=torch.float32,
+                    stream=None) -> dict:
+    """x ([N, H] float32 or bfloat16, 16-byte aligned rows) as e4m3 values with
+    one scale for each block of block_rows (1, or 128 for head weights) rows by
+    128 columns; scale_dtype is torch.float32 or torch.float8_e8m0fnu (powers of
+    two).  Returns {"q" [N, H] float8_e4m3fn (a view of rows a multiple of 16
+    bytes apart), "scales" [ceil(N / block_rows), ceil(H / 128)]}."""
+    _rowmajor(x, "x")
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("x must be float32 or bfloat16, got %s" % x.dtype)
+    if scale_dtype not in _SCALES:
+        raise ValueError("scale_dtype must be torch.float32 or torch.float8_e8m0fnu")
+    if block_rows not in (1, BLOCK):
+        raise ValueError("block_rows must be 1 or %d" % BLOCK)
+    N, H = x.shape
+    ldx = _need_stride(x, "x")
+    _need_gpu(x, "x")
+    ldq = _blocks(H, 16) * 16
+    with _on(x.device, stream) as s:
+        q = torch.empty((N, ldq), dtype=torch.float8_e4m3fn, device=x.device)
+        scales = torch.empty((_blocks(N, block_rows), _blocks(H, BLOCK)), dtype=scale_dtype,
+                             device=x.device)
+        rc = lib().opd_quantize_blocks(_ptr(x), _dt(x), N, H, ldx, block_rows,
+                                       _SCALES[scale_dtype], _ptr(q), ldq, _ptr(scales), s)
+    if rc != 0:
+        raise OpdError(rc, "opd_quantize_blocks")
+    return {"q": q[:, :H], "scales": scales}
+
+
+def head_logits(hidden: torch.Tensor, hidden_scales: torch.Tensor, weight: torch.Tensor,
+                weight_scales: torch.Tensor, *, dtype=torch.bfloat16, out=None,
+                stream=None) -> dict:
+    """Logits of N tokens from their hidden states ([N, H] float8_e4m3fn, scales
+    [N, ceil(H / 128)]) and an output head ([V, H] float8_e4m3fn, scales
+    [ceil(V / 128), ceil(H / 128)]), both as quantize_blocks gives them.  Returns
+    {"logits" [N, V]}, a view of an [N, ld] buffer (`out`, if given) as the other
+    calls take it."""
+    e4m3 = (torch.float8_e4m3fn,)
+    for t, name in ((hidden, "hidden"), (weight, "weight")):
+        _rowmajor(t, name)
+        if t.dtype not in e4m3:
+            raise TypeError("%s must be float8_e4m3fn, got %s" % (name, t.dtype))
+    N, H = hidden.shape
+    V = weight.shape[0]
+    dev = hidden.device
+    if weight.shape[1] != H or weight.device != dev:
+        raise ValueError("weight must be [V, %d] on %s, got %s on %s" %
+                         (H, dev, tuple(weight.shape), weight.device))
+    _need_scales(hidden_scales, hidden, "hidden_scales", 1)
+    _need_scales(weight_scales, weight, "weight_scales", BLOCK)
+    if hidden_scales.dtype != weight_scales.dtype:
+        raise ValueError("hidden_scales and weight_scales must have one dtype")
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+    ldx, ldw = _need_stride(hidden, "hidden"), _need_stride(weight, "weight")
+    if out is not None:
+        ld = out.stride(0) if isinstance(out, torch.Tensor) and out.dim() == 2 and N > 1 else \
+            _blocks(V, 8) * 8
+        _need_rows(out, "out", dtype, N, V, ld, dev)
+    _need_gpu(hidden, "hidden")
+    with _on(dev, stream) as s:
+        if out is None:
+            ld = _blocks(V, 8) * 8
+            out = torch.empty((N, ld), dtype=dtype, device=dev)
+        rc = lib().opd_head_logits(_ptr(hidden), ldx, _ptr(hidden_scales), _ptr(weight), ldw,
+                                   _ptr(weight_scales), _SCALES[hidden_scales.dtype], N, V, H,
+                                   F32 if dtype == torch.float32 else BF16, _ptr(out), ld, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_head_logits")
+    return {"logits": out[:, :V]}
+
+
+# ---------------------------------------------------------------- drafted tokens
+
+def verify_drafts(target_logits: torch.Tensor, draft_ids: torch.Tensor, uniforms: torch.Tensor, *,
+                  draft_logits=None, draft_lens=None, mask=None, want_logp: bool = True,
+                  workspace=None, stream=None) -> dict:
+    """Which of B sequences' drafted tokens ([B, D] int32) the target keeps, and
+    the token drawn after them, at the given uniforms ([B, D + 1] float32 in
+    [0, 1)); see opd_verify_drafts.  target_logits: [B * (D + 1), V];
+    draft_logits: [B * D, V] of the same dtype, or None for drafts that are
+    certain; draft_lens: [B] int32 or None.  Returns {"accepted" [B] int32,
+    "ids" [B, D + 1] int32 (-1 past the drawn token), "logp" [B, D + 1]
+    (log-probs under the target, 0 past it)}."""
+    R, V, ld, dt = _row_call(target_logits)
+    if not isinstance(draft_ids, torch.Tensor) or draft_ids.dim() != 2:
+        raise ValueError("draft_ids must be a contiguous [B, D] int32 tensor")
+    B, D = draft_ids.shape
+    dev = target_logits.device
+    if D < 1 or R != B * (D + 1):
+        raise ValueError("target_logits must have B * (D + 1) rows, got %d for B = %d, D = %d" %
+                         (R, B, D))
+    _need(draft_ids, "draft_ids", (torch.int32,), (B, D), dev)
+    _need(uniforms, "uniforms", (torch.float32,), (B, D + 1), dev)
+    ldd = ld
+    if draft_logits is not None:
+        _rowmajor(draft_logits, "draft_logits")
+        if draft_logits.dtype != target_logits.dtype or draft_logits.device != dev or \
+                tuple(draft_logits.shape) != (B * D, V):
+            raise ValueError("draft_logits must be [%d, %d] %s on %s, got %s %s on %s" %
+                             (B * D, V, target_logits.dtype, dev, tuple(draft_logits.shape),
+                              draft_logits.dtype, draft_logits.device))
+        ldd = draft_logits.stride(0) if B * D > 1 else _blocks(V, 8) * 8
+    if draft_lens is not None:
+        _need(draft_lens, "draft_lens", (torch.int32,), (B,), dev)
+    if mask is not None:
+        _need(mask, "mask", _MASK_DTYPES, (B,), dev)
+    if workspace is not None:
+        _need(workspace, "workspace", (torch.uint8,), (workspace.numel(),), dev)
+    _need_gpu(target_logits, "target_logits")
+    with _on(dev, stream) as s:
+        if workspace is None:
+            nbytes = int(lib().opd_verify_workspace_bytes(B, D, V, dt))
+            workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
+        accepted = torch.empty(B, dtype=torch.int32, device=dev)
+        ids = torch.empty((B, D + 1), dtype=torch.int32, device=dev)
+        logp = torch.empty((B, D + 1), dtype=torch.float32, device=dev) if want_logp else None
+        rc = lib().opd_verify_drafts(_ptr(target_logits), _ptr(draft_logits), dt, B, D, V, ld,
+                                     ldd, _ptr(draft_ids), _ptr(draft_lens), _ptr(uniforms),
+                                     _ptr(mask), _ptr(accepted), _ptr(ids), _ptr(logp),
+                                     _ptr(workspace), workspace.numel(), s)
+    if rc != 0:
+        raise OpdError(rc, "opd_verify_drafts")
+    out = {"accepted": accepted, "ids": ids}
+    if logp is not None:
+        out["logp"] = logp
     return out
 
 

@@ -13,6 +13,7 @@ SOURCES = [os.path.join(CSRC, "opd_kernels.hip"), os.path.join(CSRC, "opd_cache_
            os.path.join(CSRC, "opd_diag_kernels.hip"), os.path.join(CSRC, "opd_noalloc.hip"),
            os.path.join(CSRC, "opd_api.cpp")]
 HEADERS = [os.path.join(CSRC, "opd_internal.h"), os.path.join(CSRC, "opd_device.h"),
+           os.path.join(CSRC, "opd_head.h"), os.path.join(CSRC, "opd_verify.h"),
            os.path.join(ROOT, "include", "opd.h")]
 
 # -packed-fp32-ops: no v_pk_* fp32 arithmetic in device code.

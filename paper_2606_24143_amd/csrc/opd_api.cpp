@@ -170,6 +170,7 @@ int64_t nvec_of(int64_t V, int32_t dt) {
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 // A HIP grid holds fewer than 2^32 work-items: calls with more rows than one
 // grid takes run as consecutive launches over row chunks.
@@ -252,6 +253,22 @@ opd::CacheArgs row_args(const void* logits, int32_t dtype, int64_t N, int64_t V,
 // A row that fits the registers of one workgroup is read once.
 bool row_fits(int64_t nvec, int32_t dtype) {
   return nvec <= (int64_t)opd::slots_large(dtype) * opd::kRowThreads;
+}
+
+// Arguments shared by the blockwise calls.
+constexpr int64_t kMaxHidden = (int64_t)1 << 24;
+int check_blocks(int64_t N, int64_t H, int32_t scale_type) {
+  if (scale_type != OPD_SCALE_F32 && scale_type != OPD_SCALE_E8M0) return OPD_ERR_DTYPE;
+  if (N < 0 || N > INT32_MAX || H < 1 || H > kMaxHidden) return OPD_ERR_SHAPE;
+  return OPD_OK;
+}
+
+int check_verify(int32_t dtype, int64_t B, int32_t D, int64_t V, int64_t ld, int64_t draft_ld) {
+  if (dtype != OPD_F32 && dtype != OPD_BF16) return OPD_ERR_DTYPE;
+  if (D < 1 || D > OPD_K_MAX) return OPD_ERR_SUPPORT;
+  if (int rc = check_shape(B, V, ld)) return rc;
+  if (B * (D + 1) > INT32_MAX || draft_ld < V) return OPD_ERR_SHAPE;
+  return OPD_OK;
 }
 
 // Workspace of opd_mc_diagnostics: regions in order, each 256-byte aligned.
@@ -523,6 +540,106 @@ int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, i
   a.ids = ids;
   const hipError_t err = launch_cache_chunks(a, opd::CacheOp::Score, dtype, row_fits(a.nvec, dtype),
                                            (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+int opd_quantize_blocks(const void* x, int32_t dtype, int64_t N, int64_t H, int64_t ldx,
+                        int32_t block_rows, int32_t scale_type, void* q, int64_t ldq,
+                        void* scales, void* stream) {
+  if (dtype != OPD_F32 && dtype != OPD_BF16) return OPD_ERR_DTYPE;
+  if (int rc = check_blocks(N, H, scale_type)) return rc;
+  if (ldx < H || ldq < H) return OPD_ERR_SHAPE;
+  if (block_rows != 1 && block_rows != 128) return OPD_ERR_PARAM;
+  if (N == 0) return OPD_OK;
+  if (!x || !q || !scales) return OPD_ERR_NULL;
+  if (!aligned16(x) || !aligned16(q)) return OPD_ERR_ALIGN;
+  if ((ldx * elt_bytes(dtype)) % 16 != 0 || ldq % 16 != 0) return OPD_ERR_ALIGN;
+  if (scale_type == OPD_SCALE_F32 && !aligned4(scales)) return OPD_ERR_ALIGN;
+  opd::QuantArgs a{};
+  a.x = x;
+  a.N = N;
+  a.H = H;
+  a.ldx = ldx;
+  a.nb = (H + 127) / 128;
+  a.block_rows = block_rows;
+  a.q = (uint8_t*)q;
+  a.ldq = ldq;
+  a.scales = scales;
+  const hipError_t err =
+      opd::launch_quantize(a, dtype, scale_type == OPD_SCALE_E8M0, (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+int opd_head_logits(const void* x, int64_t ldx, const void* x_scales, const void* w, int64_t ldw,
+                    const void* w_scales, int32_t scale_type, int64_t N, int64_t V, int64_t H,
+                    int32_t logits_dtype, void* logits, int64_t ld, void* stream) {
+  if (logits_dtype != OPD_F32 && logits_dtype != OPD_BF16) return OPD_ERR_DTYPE;
+  if (int rc = check_blocks(N, H, scale_type)) return rc;
+  if (int rc = check_shape(N, V, ld)) return rc;
+  if (ldx < H || ldw < H) return OPD_ERR_SHAPE;
+  if (N == 0) return OPD_OK;
+  if (!x || !x_scales || !w || !w_scales || !logits) return OPD_ERR_NULL;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(logits)) return OPD_ERR_ALIGN;
+  if (ldx % 16 != 0 || ldw % 16 != 0 || (ld * elt_bytes(logits_dtype)) % 16 != 0)
+    return OPD_ERR_ALIGN;
+  if (scale_type == OPD_SCALE_F32 && (!aligned4(x_scales) || !aligned4(w_scales)))
+    return OPD_ERR_ALIGN;
+  opd::HeadArgs a{};
+  a.x = (const uint8_t*)x;
+  a.sx = x_scales;
+  a.w = (const uint8_t*)w;
+  a.sw = w_scales;
+  a.ldx = ldx;
+  a.ldw = ldw;
+  a.N = N;
+  a.V = V;
+  a.H = H;
+  a.nb = (int)((H + 127) / 128);
+  a.out = logits;
+  a.ldo = ld;
+  const hipError_t err =
+      opd::launch_head(a, logits_dtype, scale_type == OPD_SCALE_E8M0, (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype) {
+  if (check_verify(dtype, B, D, V, V, V) != OPD_OK || B == 0) return 0;
+  return (size_t)B * (size_t)(2 * D + 1) * sizeof(double);
+}
+
+int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32_t dtype,
+                      int64_t B, int32_t D, int64_t V, int64_t ld, int64_t draft_ld,
+                      const int32_t* draft_ids, const int32_t* draft_lens, const float* uniforms,
+                      const uint8_t* mask, int32_t* accepted, int32_t* ids, float* logp,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_verify(dtype, B, D, V, ld, draft_logits ? draft_ld : V)) return rc;
+  if (B == 0) return OPD_OK;
+  if (!target_logits || !draft_ids || !uniforms || !accepted || !ids) return OPD_ERR_NULL;
+  if (!aligned16(target_logits) || (ld * elt_bytes(dtype)) % 16 != 0) return OPD_ERR_ALIGN;
+  if (draft_logits && (!aligned16(draft_logits) || (draft_ld * elt_bytes(dtype)) % 16 != 0))
+    return OPD_ERR_ALIGN;
+  if (!workspace || workspace_bytes < opd_verify_workspace_bytes(B, D, V, dtype) ||
+      !aligned16(workspace))
+    return OPD_ERR_WORKSPACE;
+  opd::VerifyArgs a{};
+  a.target = target_logits;
+  a.draft = draft_logits;
+  a.B = B;
+  a.V = V;
+  a.ld = ld;
+  a.ldd = draft_ld;
+  a.D = D;
+  a.nvec = nvec_of(V, dtype);
+  a.tail = (int)(V - (a.nvec - 1) * elems_per_vec(dtype));
+  a.ids = draft_ids;
+  a.lens = draft_lens;
+  a.u = uniforms;
+  a.mask = mask;
+  a.accepted = accepted;
+  a.ids_out = ids;
+  a.logp = logp;
+  a.ws = (double*)workspace;
+  const hipError_t err = opd::launch_verify(a, dtype, (hipStream_t)stream);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }
 

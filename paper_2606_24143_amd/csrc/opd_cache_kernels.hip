@@ -2128,3 +2128,6 @@ hipError_t launch_cache(const CacheArgs& a, CacheOp op, int in_dt, bool resident
 }
 
 }  // namespace opd
+
+#include "opd_head.h"
+#include "opd_verify.h"

@@ -1,0 +1,349 @@
+// The rows of logits themselves (Stages 1 and 2 read them; Sec. 4.1): hidden
+// states and an output head in 8-bit floating point (e4m3: 3 bits of mantissa,
+// values to 448) with a scale for each block of 128 columns, and their product.
+// Internal; included by opd_cache_kernels.hip only.
+//
+//   quantise  a block's scale is its largest magnitude over 448 (fp32, or the
+//             least power of two that is not below it), its values the nearest
+//             e4m3 values of x / s;
+//   product   z[n, v] = sum_b sx[n, b] sw[v / 128, b] sum_{h in b} x[n, h] w[v, h]
+//             on the matrix cores, accumulated in fp32.
+#pragma once
+
+#include "opd_device.h"
+
+namespace opd {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kBlk = 128;          // columns of a block
+constexpr float kTop = 448.0f;     // the largest e4m3 value
+constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
+
+// ---------------------------------------------------------------- quantisation
+
+// Eight consecutive elements of a row from column h on (columns past H read as 0).
+template <class TI>
+__device__ __forceinline__ void load8(const void* row, int64_t h, int64_t H, float (&f)[8]) {
+  if (h + 8 <= H) {
+    if constexpr (TI::BYTES == 2) {
+      const u32x4 x = *(const u32x4*)((const uint16_t*)row + h);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        f[2 * d] = __uint_as_float(x[d] << 16);
+        f[2 * d + 1] = __uint_as_float(x[d] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4 x0 = *(const f32x4*)((const float*)row + h);
+      const f32x4 x1 = *(const f32x4*)((const float*)row + h + 4);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        f[d] = x0[d];
+        f[4 + d] = x1[d];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = h + e < H ? load_elem<TI>(row, h + e) : 0.f;
+  }
+}
+
+// The largest magnitude as bits: an integer maximum, in which a NaN is above an
+// infinity and both above every number, so neither is lost.
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+struct Scale {
+  float s;         // what values are divided by (NaN: the block holds a NaN or an infinity)
+  float stored;    // fp32 scale, or its power of two
+  uint32_t e8m0;   // its biased exponent (255: NaN)
+};
+
+template <bool E8>
+__device__ __forceinline__ Scale block_scale(uint32_t top) {
+  Scale r;
+  const bool bad = top >= 0x7F800000u;
+  if constexpr (E8) {
+    // 448 = 1.75 * 2^8: a = m 2^e needs 2^(e - 8), or 2^(e - 7) for m > 1.75.
+    // (a below 2^-126 has e = -127 in its bits and gets the least power.)
+    int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    e = e < -127 ? -127 : e;
+    r.e8m0 = bad ? 255u : (uint32_t)(e + 127);
+    r.s = bad ? __builtin_nanf("") : ldexpf(1.0f, e);
+  } else {
+    r.s = bad ? __builtin_nanf("") : fmaxf(__uint_as_float(top) / kTop, kMinScale);
+    r.e8m0 = 0;
+  }
+  r.stored = r.s;
+  return r;
+}
+
+// The nearest e4m3 values of f / s, eight to a lane, packed; the quotient is the
+// correctly rounded fp32 one (its last bit decides the ties).
+template <bool E8>
+__device__ __forceinline__ u32x2 quant8(const float (&f)[8], const Scale& sc) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = f[e] / sc.s;
+  u32x2 r;
+#pragma unroll
+  for (int d = 0; d < 2; ++d) {
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * d], v[4 * d + 1], w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * d + 2], v[4 * d + 3], w, true);
+    r[d] = sc.s == sc.s ? (uint32_t)w : 0x7F7F7F7Fu;
+  }
+  return r;
+}
+
+__device__ __forceinline__ void store8(uint8_t* qrow, int64_t h, int64_t H, u32x2 q) {
+  if (h + 8 <= H) {
+    *(u32x2*)(qrow + h) = q;
+  } else {
+    for (int e = 0; h + e < H; ++e) qrow[h + e] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
+  }
+}
+
+template <bool E8>
+__device__ __forceinline__ void store_scale(void* scales, int64_t at, const Scale& s) {
+  if constexpr (E8)
+    ((uint8_t*)scales)[at] = (uint8_t)s.e8m0;
+  else
+    ((float*)scales)[at] = s.stored;
+}
+
+// A block of one row: 16 lanes, eight elements each.
+constexpr int kQuantThreads = 256;
+template <class TI, bool E8>
+__global__ void __launch_bounds__(kQuantThreads) k_quantize_rows(QuantArgs a) {
+  const int64_t g = (int64_t)blockIdx.x * (kQuantThreads / 16) + (threadIdx.x >> 4);
+  if (g >= a.N * a.nb) return;
+  const int64_t row = g / a.nb, b = g - row * a.nb;
+  const int64_t h = b * kBlk + 8 * (threadIdx.x & 15);
+  float f[8];
+  load8<TI>((const char*)a.x + row * a.ldx * TI::BYTES, h, a.H, f);
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  const Scale s = block_scale<E8>(top);
+  store8(a.q + row * a.ldq, h, a.H, quant8<E8>(f, s));
+  if ((threadIdx.x & 15) == 0) store_scale<E8>(a.scales, g, s);
+}
+
+// A block of 128 rows: a workgroup, eight passes of 16 rows held in registers.
+template <class TI, bool E8>
+__global__ void __launch_bounds__(kQuantThreads) k_quantize_tiles(QuantArgs a) {
+  __shared__ uint32_t red[kQuantThreads / 64];
+  const int64_t br = blockIdx.x / a.nb, b = blockIdx.x - br * a.nb;
+  const int64_t h = b * kBlk + 8 * (threadIdx.x & 15);
+  const int64_t r0 = br * kBlk + (threadIdx.x >> 4);
+  float f[8][8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const int64_t row = r0 + 16 * p;
+    if (row < a.N) {
+      load8<TI>((const char*)a.x + row * a.ldx * TI::BYTES, h, a.H, f[p]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[p][e]));
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kQuantThreads / 64; ++w) top = max(top, red[w]);
+  const Scale s = block_scale<E8>(top);
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const int64_t row = r0 + 16 * p;
+    if (row < a.N) store8(a.q + row * a.ldq, h, a.H, quant8<E8>(f[p], s));
+  }
+  if (threadIdx.x == 0) store_scale<E8>(a.scales, blockIdx.x, s);
+}
+
+template <class TI, bool E8>
+hipError_t launch_quantize_t(const QuantArgs& a, hipStream_t stream) {
+  if (a.block_rows == 1) {
+    const int64_t per = kQuantThreads / 16;
+    hipLaunchKernelGGL((k_quantize_rows<TI, E8>), dim3((unsigned)((a.N * a.nb + per - 1) / per)),
+                       dim3(kQuantThreads), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((k_quantize_tiles<TI, E8>),
+                       dim3((unsigned)((a.N + kBlk - 1) / kBlk * a.nb)), dim3(kQuantThreads), 0,
+                       stream, a);
+  }
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- product
+
+// 16 bytes of a row from byte h on; bytes at or past H read as 0.  (Only bytes
+// of [0, H) are touched.)
+__device__ __forceinline__ i32x4 load16(const uint8_t* row, int h, int H) {
+  if (h + 16 <= H) return *(const i32x4*)(row + h);
+  i32x4 r = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    if (h + e < H) r[e >> 2] |= (int)((uint32_t)row[h + e] << (8 * (e & 3)));
+  return r;
+}
+
+template <bool E8>
+__device__ __forceinline__ float load_scale(const void* s, int64_t at) {
+  if constexpr (E8) {
+    const uint32_t e = ((const uint8_t*)s)[at];
+    // 2^(e - 127); 2^-127 is not a normal number, 255 is NaN
+    return e == 255u ? __builtin_nanf("") : __uint_as_float(e ? e << 23 : 0x400000u);
+  } else {
+    return ((const float*)s)[at];
+  }
+}
+
+// Four logits of consecutive vocabulary entries v .. v + 3 of one token.
+template <class TO>
+__device__ __forceinline__ void store_logits(void* row, int64_t v, int64_t V, f32x4 z) {
+  if (v + 4 <= V) {
+    if constexpr (TO::BYTES == 4)
+      *(f32x4*)((float*)row + v) = z;
+    else
+      *(u32x2*)((uint16_t*)row + v) = u32x2{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+  } else {
+    for (int e = 0; v + e < V; ++e) {
+      if constexpr (TO::BYTES == 4)
+        ((float*)row)[v + e] = z[e];
+      else
+        ((uint16_t*)row)[v + e] = __builtin_bit_cast(uint16_t, (__bf16)z[e]);
+    }
+  }
+}
+
+// Eight e4m3 values as bf16, which holds them exactly.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// c += w x^T over 64 columns, of which a lane holds 32 of its row of each.
+// The 8-bit instruction cuts each product at 2^-13 of the largest of the 16 it
+// sums at once before they reach the fp32 accumulator (measured: 1.5e-5 of a
+// result of 64 normal products; the 16-bit instructions: 5e-9), far below
+// the rounding of bf16 logits (2^-8) but not that of fp32 ones, so these are
+// made by 16-bit instructions of exactly widened values, at half the rate.
+template <class TO>
+__device__ __forceinline__ f32x16 mma64(i32x8 w, i32x8 x, f32x16 c) {
+  if constexpr (TO::BYTES == 2) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[2 * k], w[2 * k + 1]),
+                                                  widen8(x[2 * k], x[2 * k + 1]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// A tile of 128 vocabulary entries by 128 tokens: four waves of 64 by 64.
+constexpr int kHeadThreads = 256;
+template <class TO, bool E8>
+__global__ void __launch_bounds__(kHeadThreads) k_head_tile(HeadArgs a) {
+  __shared__ __align__(16) uint8_t lds[2][128 * 128];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int64_t vt = blockIdx.x / a.ntiles, nt = blockIdx.x - vt * a.ntiles;
+  const int64_t v0 = vt * 128, n0 = nt * 128;
+  const int wv = (w & 1) * 64, wn = (w >> 1) * 64;
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  for (int b = 0; b < a.nb; ++b) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int r = p * 32 + (tid >> 3), c = tid & 7;
+      const int64_t rv = min(v0 + r, a.V - 1), rn = min(n0 + r, a.N - 1);
+      const int at = r * 128 + ((c ^ (r & 7)) << 4);
+      *(i32x4*)(lds[0] + at) = load16(a.w + rv * a.ldw, b * 128 + c * 16, (int)a.H);
+      *(i32x4*)(lds[1] + at) = load16(a.x + rn * a.ldx, b * 128 + c * 16, (int)a.H);
+    }
+    __syncthreads();
+    auto frag = [&](int m, int row, int t) {
+      const int c = 4 * t + 2 * (lane >> 5);
+      const uint8_t* p = lds[m] + row * 128;
+      const i32x4 lo = *(const i32x4*)(p + ((c ^ (row & 7)) << 4));
+      const i32x4 hi = *(const i32x4*)(p + (((c + 1) ^ (row & 7)) << 4));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const float sw = load_scale<E8>(a.sw, vt * a.nb + b);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int rn = wn + 32 * j + (lane & 31);
+      const float s = load_scale<E8>(a.sx, min(n0 + rn, a.N - 1) * a.nb + b) * sw;
+      const i32x8 x0 = frag(1, rn, 0), x1 = frag(1, rn, 1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int rv = wv + 32 * i + (lane & 31);
+        f32x16 p;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = 0.f;
+        p = mma64<TO>(frag(0, rv, 0), x0, p);
+        p = mma64<TO>(frag(0, rv, 1), x1, p);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = fmaf(p[e], s, acc[i][j][e]);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int64_t n = n0 + wn + 32 * j + (lane & 31);
+    if (n >= a.N) continue;
+    void* row = (char*)a.out + n * a.ldo * TO::BYTES;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        store_logits<TO>(row, v0 + wv + 32 * i + 8 * g + 4 * (lane >> 5), a.V,
+                         f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                               acc[i][j][4 * g + 3]});
+  }
+}
+
+template <class TO, bool E8>
+hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
+  a.ntiles = (a.N + 127) / 128;
+  const int64_t vtiles = (a.V + 127) / 128;
+  hipLaunchKernelGGL((k_head_tile<TO, E8>), dim3((unsigned)(vtiles * a.ntiles)),
+                     dim3(kHeadThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantArgs& a, int in_dt, bool e8m0, hipStream_t stream) {
+  if (in_dt == BF16)
+    return e8m0 ? launch_quantize_t<InBf16, true>(a, stream)
+                : launch_quantize_t<InBf16, false>(a, stream);
+  return e8m0 ? launch_quantize_t<InF32, true>(a, stream)
+              : launch_quantize_t<InF32, false>(a, stream);
+}
+
+hipError_t launch_head(const HeadArgs& a, int out_dt, bool e8m0, hipStream_t stream) {
+  if (out_dt == BF16)
+    return e8m0 ? launch_head_t<OutBf16, true>(a, stream) : launch_head_t<OutBf16, false>(a, stream);
+  return e8m0 ? launch_head_t<OutF32, true>(a, stream) : launch_head_t<OutF32, false>(a, stream);
+}
+
+}  // namespace opd

@@ -91,6 +91,52 @@ struct CacheArgs {
 hipError_t launch_cache(const CacheArgs& a, CacheOp op, int in_dt, bool resident,
                         hipStream_t stream);
 
+// Verification of drafted tokens (opd_verify_drafts).
+struct VerifyArgs {
+  const void* target;     // [B (D + 1), ld]
+  const void* draft;      // [B D, ldd]; NULL: drafts that are certain
+  int64_t B, V, ld, ldd;
+  int D;
+  int64_t nvec;           // 4-element vectors per row covering [0, V)
+  int tail;               // valid elements in the last vector
+  const int32_t* ids;     // [B, D]
+  const int32_t* lens;    // [B] nullable
+  const float* u;         // [B, D + 1]
+  const uint8_t* mask;    // [B] nullable
+  int32_t* accepted;      // [B]
+  int32_t* ids_out;       // [B, D + 1]
+  float* logp;            // [B, D + 1] nullable
+  double* ws;             // log-sum-exps: [B, D + 1] of the target, [B, D] of the drafts
+};
+hipError_t launch_verify(const VerifyArgs& a, int in_dt, hipStream_t stream);
+
+// Blockwise quantisation (opd_quantize_blocks) and the head's product
+// (opd_head_logits); blocks of kBlk columns.
+struct QuantArgs {
+  const void* x;          // [N, ldx]
+  int64_t N, H, ldx;
+  int64_t nb;             // blocks per row
+  int block_rows;         // 1 or 128
+  uint8_t* q;             // [N, ldq]
+  int64_t ldq;
+  void* scales;           // [ceil(N / block_rows), nb]
+};
+hipError_t launch_quantize(const QuantArgs& a, int in_dt, bool e8m0, hipStream_t stream);
+
+struct HeadArgs {
+  const uint8_t* x;       // [N, ldx] e4m3
+  const void* sx;         // [N, nb]
+  const uint8_t* w;       // [V, ldw] e4m3
+  const void* sw;         // [ceil(V / 128), nb]
+  int64_t ldx, ldw;
+  int64_t N, V, H;
+  int nb;                 // blocks per row
+  void* out;              // [N, ldo]
+  int64_t ldo;
+  int64_t ntiles;         // tiles of tokens (the launch sets it)
+};
+hipError_t launch_head(const HeadArgs& a, int out_dt, bool e8m0, hipStream_t stream);
+
 // Monte-Carlo diagnostics (opd_mc_diagnostics).
 constexpr int kDiagMaxGroups = 8;
 // workgroups of the rows launch (16 waves), each with its parts of the batch
