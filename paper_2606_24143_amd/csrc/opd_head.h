@@ -194,15 +194,16 @@ __device__ __forceinline__ i32x4 load16(const uint8_t* row, int h, int H) {
   return r;
 }
 
+// 2^(e - 127) (2^-127 is not a normal number; 255 is NaN)
+__device__ __forceinline__ float e8m0_value(uint32_t e) {
+  return e == 255u ? __builtin_nanf("") : __uint_as_float(e ? e << 23 : 0x400000u);
+}
 template <bool E8>
 __device__ __forceinline__ float load_scale(const void* s, int64_t at) {
-  if constexpr (E8) {
-    const uint32_t e = ((const uint8_t*)s)[at];
-    // 2^(e - 127); 2^-127 is not a normal number, 255 is NaN
-    return e == 255u ? __builtin_nanf("") : __uint_as_float(e ? e << 23 : 0x400000u);
-  } else {
+  if constexpr (E8)
+    return e8m0_value(((const uint8_t*)s)[at]);
+  else
     return ((const float*)s)[at];
-  }
 }
 
 // Four logits of consecutive vocabulary entries v .. v + 3 of one token.
@@ -253,10 +254,41 @@ __device__ __forceinline__ f32x16 mma64(i32x8 w, i32x8 x, f32x16 c) {
   }
 }
 
-// A tile of 128 vocabulary entries by 128 tokens: four waves of 64 by 64.
+// The product of 16 rows of each over 128 columns, of which a lane holds 32.
+template <class TO>
+__device__ __forceinline__ f32x4 mma128(i32x8 w, i32x8 x) {
+  f32x4 c = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (TO::BYTES == 2) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * k], w[2 * k + 1]),
+                                                  widen8(x[2 * k], x[2 * k + 1]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// Eight logits of consecutive entries from v on of one token.
+template <class TO>
+__device__ __forceinline__ void store8_logits(char* row, int64_t v, int64_t V, f32x4 a, f32x4 b) {
+  if constexpr (TO::BYTES == 2) {
+    if (v + 8 <= V) {
+      *(u32x4*)((uint16_t*)row + v) = u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
+                                            pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+      return;
+    }
+  }
+  store_logits<TO>(row, v, V, a);
+  store_logits<TO>(row, v + 4, V, b);
+}
+
+// Any width: a tile of 128 vocabulary entries by 128 tokens, four waves of 64 by
+// 64, blocks staged one at a time with their ends masked.  For widths the
+// kernels below do not take (no multiple of 16, or one block).
 constexpr int kHeadThreads = 256;
 template <class TO, bool E8>
-__global__ void __launch_bounds__(kHeadThreads) k_head_tile(HeadArgs a) {
+__global__ void __launch_bounds__(kHeadThreads) k_head_any(HeadArgs a) {
   __shared__ __align__(16) uint8_t lds[2][128 * 128];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int64_t vt = blockIdx.x / a.ntiles, nt = blockIdx.x - vt * a.ntiles;
@@ -321,12 +353,259 @@ __global__ void __launch_bounds__(kHeadThreads) k_head_tile(HeadArgs a) {
   }
 }
 
+// ---- many tokens
+// A tile of 256 vocabulary entries by 256 tokens, eight waves of 128 by 64, one
+// workgroup per CU that stays for all its tiles.  A block of 128 columns is a
+// stage: 64 KiB in LDS, twice.  While the waves multiply stage g, each thread moves
+// its eight pieces of stage g + 1 from registers to LDS and asks for those of stage
+// g + 2, a piece to a slice of the products (all at once they fill the queues
+// of the LDS and the address unit, and the matrix cores wait: 2.55 against 2.30
+// ms, e8m0, at 4,096 tokens, V = 151,936, H = 4,096).  The stages of the next tile
+// follow those of this one without a gap.
+//
+// The vocabulary is the matrix instructions' row index, so a lane's results are
+// consecutive entries of one token, and its scales one per 16 tokens; the head's
+// scale is the wave's.  e8m0 scales go to the instructions; fp32 ones multiply
+// each block's product as it is added to the sum, which costs the vector unit
+// half the matrix cores' time.
+//
+// LDS rows are 128 bytes, 16-byte pieces at piece ^ key(row): with the keys below
+// the 16 rows that a fragment read takes at once lie in different banks.  A fragment
+// is pieces k and k + 4 of a row (k: the lane's quarter of the wave): which columns a
+// lane holds does not matter as long as both operands agree.  Rows of the head are
+// read in an order that leaves a lane eight consecutive entries from two products.
+constexpr int kTileV = 256, kTileN = 256, kTileThreads = 512;
+constexpr uint32_t kHeadCus = 256;
+constexpr int kGroupV = 8;  // vocabulary tiles that take turns, so that rows of x stay in L2
+
+__device__ __forceinline__ uint32_t key_x(uint32_t row) { return (row >> 1) & 7u; }
+__device__ __forceinline__ uint32_t key_w(uint32_t row) {
+  return ((row >> 1) & 1u) | ((row >> 2) & 6u);
+}
+
+// bytes of rows from p on (none if bytes <= 0); reads past them give zeros
+__device__ __forceinline__ Rsrc rows_rsrc(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0,
+                                           (int)(uint32_t)(bytes > 0 ? bytes : 0), kRsrcWord3);
+}
+
+template <bool E8>
+struct HeadTile {  // where a tile's operands are (wave-uniform)
+  static constexpr int SB = E8 ? 1 : 4;
+  const uint8_t *w, *x, *s;
+  int64_t wbytes, xbytes;
+  int sbytes;
+  int64_t v0, n0;
+  // tile t of the launch; past its last one, a tile without rows
+  __device__ __forceinline__ HeadTile(const HeadArgs& a, uint32_t t, uint32_t tiles, bool scales_w) {
+    const uint32_t vtiles = (uint32_t)((a.V + kTileV - 1) / kTileV), nt = (uint32_t)a.ntiles;
+    const bool is = t < tiles;
+    t = is ? t : 0u;
+    const uint32_t per = kGroupV * nt, g = t / per, r = t - g * per;
+    const uint32_t gv = min((uint32_t)kGroupV, vtiles - g * kGroupV);
+    v0 = (int64_t)(g * kGroupV + r % gv) * kTileV;
+    n0 = (int64_t)(r / gv) * kTileN;
+    w = a.w + v0 * a.ldw;
+    x = a.x + n0 * a.ldx;
+    wbytes = is ? min((int64_t)kTileV, a.V - v0) * a.ldw : 0;
+    xbytes = is ? min((int64_t)kTileN, a.N - n0) * a.ldx : 0;
+    // scales: of the tokens, or of the tile's two blocks of the head
+    const int64_t s0 = scales_w ? v0 / kBlk : n0;
+    const int64_t srows = scales_w ? min((int64_t)2, (a.V + kBlk - 1) / kBlk - s0)
+                                   : min((int64_t)kTileN, a.N - n0);
+    s = (const uint8_t*)(scales_w ? a.sw : a.sx) + s0 * a.nb * SB;
+    sbytes = is ? (int)srows * a.nb * SB : 0;
+  }
+};
+
+template <class TO, bool E8>
+__global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
+  constexpr bool WIDE = TO::BYTES == 4;  // 16-bit instructions (mma128)
+  constexpr bool HW = E8 && !WIDE;       // the instructions apply the scales
+  constexpr int JH = HW ? 4 : 2;         // groups of 16 tokens at a time
+  constexpr int PF = HW ? 2 : 3;         // fragments of the head on the way
+  constexpr int SLICES = 32 / JH, FIRST = HW ? 0 : 1;
+  __shared__ __align__(16) uint8_t lds[2][2][256 * 128];  // [stage][head, tokens]
+  __shared__ uint32_t lsc[2][kTileN + 2];                 // tokens' scales, then the head's
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t tiles = (uint32_t)(((a.V + kTileV - 1) / kTileV) * a.ntiles);
+  // workgroups of XCD k (every eighth) share its contiguous part of the tiles
+  const uint32_t G = gridDim.x, xcds = min(G, (uint32_t)kXcds);
+  const uint32_t xcd = blockIdx.x % xcds, mine = blockIdx.x / xcds;
+  const uint32_t step = (G - xcd + xcds - 1) / xcds;
+  const uint32_t t1 = (uint32_t)((uint64_t)tiles * (xcd + 1) / xcds);
+  uint32_t t = (uint32_t)((uint64_t)tiles * xcd / xcds) + mine;
+  if (t >= t1) return;
+
+  const int wv = (w & 1) * 128, wn = (w >> 1) * 64;
+  const uint32_t ldw = (uint32_t)a.ldw, ldx = (uint32_t)a.ldx;
+  const uint32_t prow = (uint32_t)tid >> 3, piece = (uint32_t)tid & 7u;
+  const uint32_t ow = prow * ldw + piece * 16, ox = prow * ldx + piece * 16;
+  const uint32_t os = (uint32_t)(tid & 255) * a.nb * HeadTile<E8>::SB;
+  // (rows 64 apart have the same keys)
+  const uint32_t ww = prow * 128 + ((piece ^ key_w(prow)) << 4);
+  const uint32_t wx = prow * 128 + ((piece ^ key_x(prow)) << 4);
+  const uint32_t lr = (uint32_t)lane & 15u, lk = (uint32_t)lane >> 4;
+  const uint32_t rw = 8 * (lr >> 2) + (lr & 3);  // the head's row in a pair of products
+  const uint32_t fw0 = rw * 128 + ((lk ^ key_w(rw)) << 4);
+  const uint32_t fx0 = lr * 128 + ((lk ^ key_x(lr)) << 4);
+
+  u32x4 pw[4], px[4];  // the pieces on their way
+  uint32_t psc = 0;
+  auto ask = [&](const HeadTile<E8>& h, int b, int k) {
+    // (a piece past the row's end: past the buffer's, which gives zeros)
+    const bool in = b * kBlk + (int)piece * 16 < (int)a.H;
+    if (k < 4) {
+      const Rsrc r = rows_rsrc(h.w + b * kBlk, h.wbytes - b * kBlk);
+      pw[k] = __builtin_amdgcn_raw_buffer_load_b128(
+          r, in ? (int)(ow + (uint32_t)k * 64 * ldw) : INT32_MIN, 0, 0);
+    } else {
+      const Rsrc r = rows_rsrc(h.x + b * kBlk, h.xbytes - b * kBlk);
+      px[k - 4] = __builtin_amdgcn_raw_buffer_load_b128(
+          r, in ? (int)(ox + (uint32_t)(k - 4) * 64 * ldx) : INT32_MIN, 0, 0);
+    }
+    if (k == 0) {
+      const Rsrc r = rows_rsrc(h.s + b * HeadTile<E8>::SB, h.sbytes - b * HeadTile<E8>::SB);
+      if constexpr (E8)
+        psc = __builtin_amdgcn_raw_buffer_load_b8(r, (int)os, 0, 0);
+      else
+        psc = __builtin_amdgcn_raw_buffer_load_b32(r, (int)os, 0, 0);
+    }
+  };
+  auto put = [&](int buf, int k) {
+    if (k < 4)
+      *(u32x4*)(lds[buf][0] + ww + k * 8192) = pw[k];
+    else
+      *(u32x4*)(lds[buf][1] + wx + (k - 4) * 8192) = px[k - 4];
+    if (k == 0 && tid < kTileN + 2) lsc[buf][tid] = psc;
+  };
+  auto frag_w = [&](const uint8_t* base, int i) {
+    const uint8_t* p = base + (i >> 1) * 4096 + (i & 1) * 512;
+    const i32x4 lo = *(const i32x4*)(p + fw0), hi = *(const i32x4*)(p + (fw0 ^ 64u));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto frag_x = [&](const uint8_t* base, int j) {
+    const uint8_t* p = base + j * 2048;
+    const i32x4 lo = *(const i32x4*)(p + fx0), hi = *(const i32x4*)(p + (fx0 ^ 64u));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto scale_of = [&](uint32_t bits) {
+    return E8 ? e8m0_value(bits) : __uint_as_float(bits);
+  };
+
+  const bool scales_w = w >= 4;
+  HeadTile<E8> cur(a, t, tiles, scales_w);
+  HeadTile<E8> next(a, t + step < t1 ? t + step : tiles, tiles, scales_w);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) ask(cur, 0, k);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    put(0, k);
+    ask(cur, 1, k);
+  }
+  int buf = 0;
+  for (;;) {
+    f32x4 acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < a.nb; ++b, buf ^= 1) {
+      const uint8_t* fw = lds[buf][0] + wv * 128;
+      const uint8_t* fx = lds[buf][1] + wn * 128;
+      const bool over = b + 2 >= a.nb;  // stage g + 2 is the next tile's
+      HeadTile<E8> from = cur;
+      from.w = over ? next.w : cur.w;
+      from.x = over ? next.x : cur.x;
+      from.s = over ? next.s : cur.s;
+      from.wbytes = over ? next.wbytes : cur.wbytes;
+      from.xbytes = over ? next.xbytes : cur.xbytes;
+      from.sbytes = over ? next.sbytes : cur.sbytes;
+      const int fb = over ? b + 2 - a.nb : b + 2;
+      __syncthreads();  // stage g is in LDS; the other half is free
+      const uint32_t hs = lsc[buf][kTileN + (w & 1)];
+#pragma unroll
+      for (int h = 0; h < 4; h += JH) {
+        i32x8 bx[JH], aw[PF];
+        uint32_t ts[JH];
+        float s[JH];
+        f32x4 p[2][JH];
+#pragma unroll
+        for (int j = 0; j < JH; ++j) {
+          bx[j] = frag_x(fx, h + j);
+          ts[j] = lsc[buf][wn + 16 * (h + j) + lr];
+        }
+#pragma unroll
+        for (int i = 0; i < PF - 1; ++i) aw[i] = frag_w(fw, i);
+        if constexpr (!HW) {
+#pragma unroll
+          for (int j = 0; j < JH; ++j) s[j] = scale_of(ts[j]) * scale_of(hs);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < (HW ? 8 : 9); ++i) {
+          if (i < 9 - PF) aw[(i + PF - 1) % PF] = frag_w(fw, i + PF - 1);
+          const int k = h / JH * 8 + i - FIRST;
+          if (i < 8 && k >= 0 && k < 8) {
+            put(buf ^ 1, k);
+            ask(from, fb, k);
+          }
+          if constexpr (HW) {
+#pragma unroll
+            for (int j = 0; j < JH; ++j)
+              acc[i & 7][h + j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                  aw[i % PF], bx[j], acc[i & 7][h + j], 0, 0, 0, (int)hs, 0, (int)ts[j]);
+          } else {
+            if (i < 8) {
+#pragma unroll
+              for (int j = 0; j < JH; ++j) p[i & 1][j] = mma128<TO>(aw[i % PF], bx[j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (i > 0) {  // the products before are added meanwhile
+#pragma unroll
+              for (int j = 0; j < JH; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  acc[i - 1][h + j][e] = fmaf(p[(i - 1) & 1][j][e], s[j], acc[i - 1][h + j][e]);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t n = cur.n0 + wn + 16 * j + lr;
+      if (n < a.N) {
+        char* row = (char*)a.out + n * a.ldo * TO::BYTES;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2)
+          store8_logits<TO>(row, cur.v0 + wv + 16 * i + 8 * lk, a.V, acc[i][j], acc[i + 1][j]);
+      }
+    }
+    t += step;
+    if (t >= t1) break;
+    cur = next;
+    next = HeadTile<E8>(a, t + step < t1 ? t + step : tiles, tiles, scales_w);
+  }
+}
+
 template <class TO, bool E8>
 hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
-  a.ntiles = (a.N + 127) / 128;
-  const int64_t vtiles = (a.V + 127) / 128;
-  hipLaunchKernelGGL((k_head_tile<TO, E8>), dim3((unsigned)(vtiles * a.ntiles)),
-                     dim3(kHeadThreads), 0, stream, a);
+  // (a tile's rows have to lie within the 2 GiB that a buffer's offsets take here)
+  constexpr int64_t kMaxStride = (int64_t)1 << 22;
+  if (a.H % 16 != 0 || a.nb < 2 || a.ldw > kMaxStride || a.ldx > kMaxStride) {
+    a.ntiles = (a.N + 127) / 128;
+    const int64_t tiles = (a.V + 127) / 128 * a.ntiles;
+    hipLaunchKernelGGL((k_head_any<TO, E8>), dim3((unsigned)tiles), dim3(kHeadThreads), 0, stream,
+                       a);
+    return hipGetLastError();
+  }
+  a.ntiles = (a.N + kTileN - 1) / kTileN;
+  const int64_t tiles = (a.V + kTileV - 1) / kTileV * a.ntiles;
+  hipLaunchKernelGGL((k_head_tile<TO, E8>), dim3((unsigned)min(tiles, (int64_t)kHeadCus)),
+                     dim3(kTileThreads), 0, stream, a);
   return hipGetLastError();
 }
 

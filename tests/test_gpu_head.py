@@ -131,12 +131,13 @@ def test_head_logits(N, V, H, scale, out):
 
 @pytest.mark.parametrize("N", [1, 40, 300])
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
-def test_head_keeps_nan_to_its_rows(N, scale):
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_head_keeps_nan_to_its_rows(N, scale, out):
     V, H = 300, 400
     g = np.random.default_rng(5)
     x, sx, vx, vsx = quantized(g.normal(0, 1, (N, H)).astype(np.float32), 1, scale)
     w, sw, vw, vsw = quantized(g.normal(0, 1, (V, H)).astype(np.float32), 128, scale)
-    want = opd.head_logits(x, sx, w, sw, dtype=torch.float32)["logits"].clone()
+    want = opd.head_logits(x, sx, w, sw, dtype=DT[out])["logits"].clone()
     assert torch.isfinite(want).all()
     n, v, block = N // 2, 77, 2  # a value of one token, one of a head row, a scale of 128 rows
     x = x.clone()
@@ -150,7 +151,7 @@ def test_head_keeps_nan_to_its_rows(N, scale):
     else:
         sw2.view(torch.uint8)[block, 1] = 255
     got = opd.head_logits(xb.view(torch.float8_e4m3fn), sx, wb.view(torch.float8_e4m3fn), sw2,
-                          dtype=torch.float32)["logits"]
+                          dtype=DT[out])["logits"]
     torch.cuda.synchronize()
     bad = torch.zeros(N, V, dtype=torch.bool, device=DEV)
     bad[n] = True
