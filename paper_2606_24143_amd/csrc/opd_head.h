@@ -353,6 +353,189 @@ __global__ void __launch_bounds__(kHeadThreads) k_head_any(HeadArgs a) {
   }
 }
 
+__device__ __forceinline__ uint32_t key_x(uint32_t row) { return (row >> 1) & 7u; }
+__device__ __forceinline__ uint32_t key_w(uint32_t row) {
+  return ((row >> 1) & 1u) | ((row >> 2) & 6u);
+}
+
+// bytes of rows from p on (none if bytes <= 0); reads past them give zeros
+__device__ __forceinline__ Rsrc rows_rsrc(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0,
+                                           (int)(uint32_t)(bytes > 0 ? bytes : 0), kRsrcWord3);
+}
+
+// ---- few tokens
+// Up to 128 tokens the product is a read of the head.  W waves of 16 of its rows
+// each, all tokens (T groups of 16).  The head goes from memory to the matrix
+// instructions' registers, SB blocks ahead; the tokens through LDS, SB blocks a
+// stage, shared by the waves.  Workgroups start at different stages of the rows
+// (T > 1): rows are often a multiple of 4 KiB apart, and all reads at one place of
+// them wait for the same part of the memory (127 against 137 us at 32 tokens,
+// V = 151,936, H = 4,096).
+template <class TO, bool E8, int T, int SB, int W>
+__global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
+  constexpr bool HW = E8 && TO::BYTES == 2;
+  constexpr int SZ = E8 ? 1 : 4, THREADS = 64 * W;
+  constexpr int ROWS = 16 * T, PIECES = ROWS * SB * 8, PER = (PIECES + THREADS - 1) / THREADS;
+  static_assert(ROWS * SB <= THREADS * 2, "scales");
+  constexpr int SPER = (ROWS * SB + THREADS - 1) / THREADS;
+  __shared__ __align__(16) uint8_t lx[2][SB][ROWS * 128];
+  __shared__ uint32_t lsc[2][SB][ROWS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t lr = (uint32_t)lane & 15u, lk = (uint32_t)lane >> 4;
+  const int64_t v0 = ((int64_t)blockIdx.x * W + w) * 16;
+  const uint32_t ldw = (uint32_t)a.ldw, ldx = (uint32_t)a.ldx;
+  const int64_t vr = min(v0, a.V - 1);  // (a wave past the last row reads nothing)
+  const uint8_t* gw = a.w + vr * a.ldw;
+  const int64_t wbytes = v0 < a.V ? min((int64_t)16, a.V - v0) * a.ldw : 0;
+  const int64_t xbytes = a.N * a.ldx;
+  const int sbytes = (int)a.N * a.nb * SZ;
+  const uint8_t* gh = (const uint8_t*)a.sw + (vr / kBlk) * a.nb * SZ;  // (16 divides 128)
+  const uint32_t ow = lr * ldw + lk * 16;
+
+  u32x4 px[PER];
+  uint32_t ps[SPER], hs[SB];
+  i32x8 bw[SB];
+  auto ask_x = [&](int b0) {
+    const Rsrc q = rows_rsrc(a.x + (int64_t)b0 * kBlk, xbytes - (int64_t)b0 * kBlk);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const uint32_t i = (uint32_t)tid + k * THREADS, at = i & (SB * 8 - 1), row = i / (SB * 8);
+      const bool in = b0 * kBlk + (int)at * 16 < (int)a.H && (PIECES % THREADS == 0 || i < PIECES);
+      px[k] = __builtin_amdgcn_raw_buffer_load_b128(q, in ? (int)(row * ldx + at * 16) : INT32_MIN,
+                                                    0, 0);
+    }
+    const Rsrc qs = rows_rsrc((const uint8_t*)a.sx + b0 * SZ, sbytes - b0 * SZ);
+#pragma unroll
+    for (int k = 0; k < SPER; ++k) {
+      const uint32_t i = (uint32_t)tid + k * THREADS, row = i / SB, b = i & (SB - 1);
+      const int o = b0 + (int)b < a.nb && row < ROWS ? (int)((row * a.nb + b) * SZ) : INT32_MIN;
+      if constexpr (E8)
+        ps[k] = __builtin_amdgcn_raw_buffer_load_b8(qs, o, 0, 0);
+      else
+        ps[k] = __builtin_amdgcn_raw_buffer_load_b32(qs, o, 0, 0);
+    }
+  };
+  auto put_x = [&](int buf) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const uint32_t i = (uint32_t)tid + k * THREADS, at = i & (SB * 8 - 1), row = i / (SB * 8);
+      if (PIECES % THREADS == 0 || i < PIECES)
+        *(u32x4*)(lx[buf][at >> 3] + row * 128 + (((at & 7u) ^ key_x(row)) << 4)) = px[k];
+    }
+#pragma unroll
+    for (int k = 0; k < SPER; ++k) {
+      const uint32_t i = (uint32_t)tid + k * THREADS, row = i / SB;
+      if (row < ROWS) lsc[buf][i & (SB - 1)][row] = ps[k];
+    }
+  };
+  auto ask_w = [&](int d, int b) {
+    const int h = b * kBlk + (int)lk * 16;
+    const bool in0 = h < (int)a.H, in1 = h + 64 < (int)a.H;
+    const Rsrc q = rows_rsrc(gw + (int64_t)b * kBlk, wbytes - (int64_t)b * kBlk);
+    const u32x4 lo = __builtin_amdgcn_raw_buffer_load_b128(q, in0 ? (int)ow : INT32_MIN, 0, 0);
+    const u32x4 hi =
+        __builtin_amdgcn_raw_buffer_load_b128(q, in1 ? (int)(ow + 64) : INT32_MIN, 0, 0);
+    bw[d] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    const Rsrc qs = rows_rsrc(gh + b * SZ, b < a.nb ? SZ : 0);
+    if constexpr (E8)
+      hs[d] = __builtin_amdgcn_raw_buffer_load_b8(qs, 0, 0, 0);
+    else
+      hs[d] = __builtin_amdgcn_raw_buffer_load_b32(qs, 0, 0, 0);
+  };
+  f32x4 acc[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t fx0 = lr * 128 + ((lk ^ key_x(lr)) << 4);
+  auto multiply = [&](int d, int buf) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const uint8_t* p = lx[buf][d] + t * 2048;
+      const i32x4 lo = *(const i32x4*)(p + fx0), hi = *(const i32x4*)(p + (fx0 ^ 64u));
+      const i32x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      const uint32_t ts = lsc[buf][d][16 * t + lr];
+      if constexpr (HW) {
+        acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(bw[d], x, acc[t], 0, 0, 0,
+                                                                  (int)hs[d], 0, (int)ts);
+      } else {
+        const float s = E8 ? e8m0_value(ts) * e8m0_value(hs[d])
+                           : __uint_as_float(ts) * __uint_as_float(hs[d]);
+        const f32x4 q = mma128<TO>(bw[d], x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(q[e], s, acc[t][e]);
+        // (added here, not kept for later: the products would fill the registers)
+        if (T > 1) asm volatile("" : "+v"(acc[t]));
+      }
+      if (T > 2) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // stages in a cycle that starts elsewhere for each workgroup
+  const int stages = (a.nb + SB - 1) / SB;
+  int at_x = T > 1 ? (int)(blockIdx.x % (uint32_t)stages) : 0, at_w = at_x;
+  auto step = [&](int& at) { at = at + 1 == stages ? 0 : at + 1; };
+  ask_x(at_x * SB);
+  step(at_x);
+#pragma unroll
+  for (int d = 0; d < SB; ++d) ask_w(d, at_w * SB + d);
+  step(at_w);
+  put_x(0);
+  ask_x(at_x * SB);
+  step(at_x);
+  int buf = 0;
+  for (int i = 0; i < stages; ++i, buf ^= 1) {
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < SB; ++d) {
+      multiply(d, buf);
+      ask_w(d, at_w * SB + d);
+      __builtin_amdgcn_sched_barrier(0);
+      if (d == SB - 1) {
+        put_x(buf ^ 1);
+        ask_x(at_x * SB);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    step(at_x);
+    step(at_w);
+  }
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int64_t token = 16 * t + lr;
+    if (token < a.N)
+      store_logits<TO>((char*)a.out + token * a.ldo * TO::BYTES, v0 + 4 * lk, a.V, acc[t]);
+  }
+}
+
+template <class TO, bool E8, int T, int SB, int W>
+hipError_t launch_stream(const HeadArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((k_head_stream<TO, E8, T, SB, W>),
+                     dim3((unsigned)((a.V + 16 * W - 1) / (16 * W))), dim3(64 * W), 0,
+                     stream, a);
+  return hipGetLastError();
+}
+
+// Waves to a workgroup: many share their tokens, few spread a narrow head over the
+// CUs.  Measured, 2 / 4 / 8 waves, us: 1 token, V = 8,000, H = 4,096 10.8 / 13.8 / 21.1;
+// 32,000 x 2,048 - / 13.4 / 15.1; 32 tokens, 4,000 x 4,096 10.5 / 11.6 / 19.6;
+// 16,000 x 2,048 9.1 / 9.1 / 12.0; 32,000 x 4,096 34.2 / 30.5 / 28.4; 64 tokens, 4,000 18.8 /
+// 17.5 / 23.5; 16,000 x 2,048 14.3 / 11.5 / 14.4; 64,000 x 4,096 95.0 / 69.8 / 61.3.
+template <class TO, bool E8>
+hipError_t launch_few(const HeadArgs& a, hipStream_t stream) {
+  const bool narrow = a.V < 12288, wide = a.V >= 24576;
+  if (a.N <= 16)
+    return narrow ? launch_stream<TO, E8, 1, 4, 2>(a, stream)
+                  : launch_stream<TO, E8, 1, 4, 4>(a, stream);
+  if (a.N <= 32)
+    return narrow ? launch_stream<TO, E8, 2, 4, 2>(a, stream)
+           : wide ? launch_stream<TO, E8, 2, 4, 8>(a, stream)
+                  : launch_stream<TO, E8, 2, 4, 4>(a, stream);
+  if (a.N <= 64)
+    return wide ? launch_stream<TO, E8, 4, 4, 8>(a, stream)
+                : launch_stream<TO, E8, 4, 4, 4>(a, stream);
+  return launch_stream<TO, E8, 8, 2, 8>(a, stream);
+}
+
 // ---- many tokens
 // A tile of 256 vocabulary entries by 256 tokens, eight waves of 128 by 64, one
 // workgroup per CU that stays for all its tiles.  A block of 128 columns is a
@@ -377,17 +560,6 @@ __global__ void __launch_bounds__(kHeadThreads) k_head_any(HeadArgs a) {
 constexpr int kTileV = 256, kTileN = 256, kTileThreads = 512;
 constexpr uint32_t kHeadCus = 256;
 constexpr int kGroupV = 8;  // vocabulary tiles that take turns, so that rows of x stay in L2
-
-__device__ __forceinline__ uint32_t key_x(uint32_t row) { return (row >> 1) & 7u; }
-__device__ __forceinline__ uint32_t key_w(uint32_t row) {
-  return ((row >> 1) & 1u) | ((row >> 2) & 6u);
-}
-
-// bytes of rows from p on (none if bytes <= 0); reads past them give zeros
-__device__ __forceinline__ Rsrc rows_rsrc(const void* p, int64_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0,
-                                           (int)(uint32_t)(bytes > 0 ? bytes : 0), kRsrcWord3);
-}
 
 template <bool E8>
 struct HeadTile {  // where a tile's operands are (wave-uniform)
@@ -423,7 +595,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
   constexpr bool WIDE = TO::BYTES == 4;  // 16-bit instructions (mma128)
   constexpr bool HW = E8 && !WIDE;       // the instructions apply the scales
   constexpr int JH = HW ? 4 : 2;         // groups of 16 tokens at a time
-  constexpr int PF = HW ? 2 : 3;         // fragments of the head on the way
+  constexpr int PF = HW || WIDE ? 2 : 3;  // fragments of the head on the way
   constexpr int SLICES = 32 / JH, FIRST = HW ? 0 : 1;
   __shared__ __align__(16) uint8_t lds[2][2][256 * 128];  // [stage][head, tokens]
   __shared__ uint32_t lsc[2][kTileN + 2];                 // tokens' scales, then the head's
@@ -602,6 +774,7 @@ hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
                        a);
     return hipGetLastError();
   }
+  if (a.N <= 128) return launch_few<TO, E8>(a, stream);
   a.ntiles = (a.N + kTileN - 1) / kTileN;
   const int64_t tiles = (a.V + kTileV - 1) / kTileV * a.ntiles;
   hipLaunchKernelGGL((k_head_tile<TO, E8>), dim3((unsigned)min(tiles, (int64_t)kHeadCus)),
