@@ -271,6 +271,47 @@ int check_verify(int32_t dtype, int64_t B, int32_t D, int64_t V, int64_t ld, int
   return OPD_OK;
 }
 
+// How the rows of a verification are split.
+struct VerifyPlan {
+  int parts, draw_parts, nchunk, chunk_steps, round;
+  uint32_t part_groups;
+  bool table;
+  size_t ws_bytes;
+};
+VerifyPlan verify_plan(int64_t B, int32_t D, int64_t V, int32_t dtype, bool draft) {
+  VerifyPlan p{};
+  const int64_t groups = (V + 7) / 8;
+  const int64_t steps = (groups + 63) / 64;  // of 512 elements
+  // a row's parts, one to a wavefront, of whole tiles of 256 groups: at most (k_verify_rows
+  // takes as few as fill the GPU, or these where there are too many rows to count)
+  const int64_t tiles = (groups + 255) / 256;
+  int64_t parts = 16384 / B;
+  if (parts > tiles) parts = tiles;
+  if (parts > 64) parts = 64;
+  if (parts < 4) parts = tiles < 4 ? tiles : 4;
+  const int64_t per = (tiles + parts - 1) / parts;
+  p.parts = (int)((tiles + per - 1) / per);
+  p.part_groups = (uint32_t)(per * 256);
+  p.chunk_steps = (int)((steps + opd::kVerMaxChunks - 1) / opd::kVerMaxChunks);
+  p.nchunk = (int)((steps + p.chunk_steps - 1) / p.chunk_steps);
+  // the draw's parts, one to a workgroup: of 4,096 elements at least
+  int64_t k = (opd::kVerGroups + B - 1) / B;
+  if (k > groups / 512) k = groups / 512;
+  p.draw_parts = k < 1 ? 1 : (int)k;
+  p.table = B * V >= 4000000;
+  // The first round's positions: about 128 MB.  Every round costs some 15 us besides its
+  // reading (a launch, the table, the tests at its end), so small ones do not pay;
+  // later ones have twice the positions, as fewer sequences are left.
+  constexpr int64_t kRoundBytes = (int64_t)128 << 20;
+  const int64_t round = kRoundBytes / ((draft ? 2 : 1) * B * V * elt_bytes(dtype)) + 1;
+  p.round = (int)(round < D + 1 ? round : D + 1);
+  const size_t rows = (size_t)B * (size_t)(2 * D + 1);
+  p.ws_bytes = rows * 16 * (1 + (size_t)p.parts) +
+               (p.draw_parts > 1 ? (size_t)B * p.nchunk * 8 : 0) +
+               (size_t)B * (2 * (size_t)(D + 1) + 2) * 4;
+  return p;
+}
+
 // Workspace of opd_mc_diagnostics: regions in order, each 256-byte aligned.
 struct DiagLayout {
   size_t rho, x, psum, seq, parts, hist, total;
@@ -604,7 +645,7 @@ int opd_head_logits(const void* x, int64_t ldx, const void* x_scales, const void
 
 size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype) {
   if (check_verify(dtype, B, D, V, V, V) != OPD_OK || B == 0) return 0;
-  return (size_t)B * (size_t)(2 * D + 1) * sizeof(double);
+  return (verify_plan(B, D, V, dtype, true).ws_bytes + 255) & ~(size_t)255;
 }
 
 int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32_t dtype,
@@ -638,7 +679,15 @@ int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32
   a.accepted = accepted;
   a.ids_out = ids;
   a.logp = logp;
-  a.ws = (double*)workspace;
+  const VerifyPlan p = verify_plan(B, D, V, dtype, draft_logits != nullptr);
+  a.ws = workspace;
+  a.parts = p.parts;
+  a.part_groups = p.part_groups;
+  a.draw_parts = p.draw_parts;
+  a.nchunk = p.nchunk;
+  a.chunk_steps = p.chunk_steps;
+  a.table = p.table;
+  a.round = p.round;
   const hipError_t err = opd::launch_verify(a, dtype, (hipStream_t)stream);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }

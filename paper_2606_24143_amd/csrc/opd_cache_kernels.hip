@@ -838,9 +838,10 @@ struct TabLds {
 // Sets up the table with one exponential for every five entries: a magnitude is
 // (1 + h / 8 + l / 128) 2^x, so exp(z) is the entry at l = 0 times exp(+-l 2^(x
 // - 7)).  Ends with a barrier.
-__device__ __forceinline__ void tab_setup(TabLds& t) {
-  constexpr uint32_t T = kTabThreads, kHi = kTabSize / 16, kLo = kTabBinades * 32;
-  if (threadIdx.x < 2) t.e[kTabSize + threadIdx.x] = 0.0;
+template <uint32_t T>
+__device__ __forceinline__ void tab_setup(double* e, double* lo) {
+  constexpr uint32_t kHi = kTabSize / 16, kLo = kTabBinades * 32;
+  if (threadIdx.x < 2) e[kTabSize + threadIdx.x] = 0.0;
   for (uint32_t j = threadIdx.x; j < kHi + kLo; j += T) {
     const bool high = j < kHi;
     // the high entries by (binade, h, sign), the low factors by (binade, l, sign)
@@ -851,14 +852,14 @@ __device__ __forceinline__ void tab_setup(TabLds& t) {
     const double z = high ? (double)m : (double)m * ((double)((i >> 1) & 15u) / 128.0);
     const double v = exp(sign ? -z : z);
     if (high)
-      t.e[(x << 8) | (((i >> 1) & 7u) << 5) | sign] = v;
+      e[(x << 8) | (((i >> 1) & 7u) << 5) | sign] = v;
     else
-      t.lo[i] = v;
+      lo[i] = v;
   }
   __syncthreads();
   for (uint32_t j = threadIdx.x; j < kTabSize; j += T) {
     const uint32_t l = (j >> 1) & 15u;
-    if (l != 0u) t.e[j] = t.e[j & ~30u] * t.lo[((j >> 8) << 5) | (j & 31u)];
+    if (l != 0u) e[j] = e[j & ~30u] * lo[((j >> 8) << 5) | (j & 31u)];
   }
   __syncthreads();
 }
@@ -1029,7 +1030,7 @@ __global__ void __launch_bounds__(kTabThreads) k_sample_tab(CacheArgs a) {
   const uint32_t magic = 0xFFFFFFFFu / per + 1;  // i / per = mulhi(i, magic) for i per < 2^32
 
   for (int i = threadIdx.x; i < 1 + 4 * kTabMaxSlots; i += kTabThreads) (&sh.next)[i] = 0u;
-  tab_setup(sh);
+  tab_setup<kTabThreads>(sh.e, sh.lo);
 
   // (blocks of 64 rows to each XCD, as xcd_remap, with constant divisors)
   auto row_of = [&](uint32_t j) -> int64_t {

@@ -106,8 +106,17 @@ struct VerifyArgs {
   int32_t* accepted;      // [B]
   int32_t* ids_out;       // [B, D + 1]
   float* logp;            // [B, D + 1] nullable
-  double* ws;             // log-sum-exps: [B, D + 1] of the target, [B, D] of the drafts
+  void* ws;               // opd_verify_workspace_bytes (laid out by ver_ws)
+  int parts;              // of a row, each summed by one workgroup
+  uint32_t part_groups;   // groups of 8 elements in a part
+  int draw_parts;         // of the row that a sequence's last token is drawn from
+  int nchunk, chunk_steps;  // its chunks, of 512 chunk_steps elements
+  bool table;             // bf16 rows: exp(z) from a table
+  int round;              // positions of the first round of sums; each next one has twice
 };
+// two workgroups to a CU
+constexpr int kVerGroups = 512;
+constexpr int kVerMaxChunks = 2048;
 hipError_t launch_verify(const VerifyArgs& a, int in_dt, hipStream_t stream);
 
 // Blockwise quantisation (opd_quantize_blocks) and the head's product

@@ -1,5 +1,5 @@
 // Verification of drafted tokens (Stage 1 with a drafter; Sec. 4.1).  Included
-// by opd_cache_kernels.hip only, whose double-precision exponential, scans and
+// by opd_cache_kernels.hip only, whose double-precision exponentials, scans and
 // draw by inversion it uses.
 //
 // Sequence b has n drafted tokens x_0 .. x_{n-1}, target rows p_0 .. p_n and
@@ -10,128 +10,529 @@
 // under it are the cache's behav_logp.  All in double precision: the decisions
 // and the draw are those of exact arithmetic unless a uniform lies within about
 // 1e-13 of a border.
+//
+// k_verify_rows sums the rows, k_verify_draw draws.  Rows past a sequence's first
+// refusal have no part in the result, and they are an eighth to three quarters of
+// all rows.  So the positions are summed in rounds, a launch each (verify_round): a
+// round leaves out the sequences that the rounds before it ended.
 #pragma once
 
 namespace opd {
 namespace {
 
-constexpr int kVerThreads = 256;
+constexpr int kVerThreads = 512;
+constexpr int kVerWaves = kVerThreads / 64;
+// Sums of exp(z) itself, not of exp(z - max), need no maximum: a double holds them
+// for logits below 640.  A part of a row with others, or whose sum is so small that
+// its terms may have been cut off, is summed again relative to its maximum.
+constexpr float kVerTop = 640.f;
+constexpr double kVerMinSum = 8.75651076269652e-27;  // exp(-60)
 
-// A sequence's test of drafted token i.
-enum Test : int { kKept = 0, kRefused = 1, kBad = 2 };
+// A sequence's test of drafted token i (0: not made).
+enum Test : uint32_t { kUntested = 0, kKept = 1, kRefused = 2, kBad = 3 };
 
-// log-sum-exps of the target rows (VerifyArgs::ws), then of the draft rows; NaN
-// for a row without a distribution.
-__device__ __forceinline__ double* target_lse(const VerifyArgs& a, int64_t b) {
-  return a.ws + b * (a.D + 1);
+// What a part of a row sums to: s exp(m) (s NaN: no distribution), m 0 as a rule.
+struct VerRec {
+  double m, s;
+};
+// A row: its log-sum-exp (NaN: no distribution), and the largest m of its parts.
+struct VerRow {
+  double L, m;
+};
+
+// LDS of the terms: the 512 powers of the exponential, and exp(z) of each bf16 z.
+template <bool TABLE>
+struct VerTab {
+  double p[kExpTab];
+  double e[TABLE ? kTabSize + 2 : 1];
+};
+
+template <bool TABLE, int T>
+__device__ __forceinline__ void ver_setup(VerTab<TABLE>& t, double* scratch) {
+  for (int j = threadIdx.x; j < kExpTab; j += T) t.p[j] = exp2((double)j / kExpTab);
+  if constexpr (TABLE)
+    tab_setup<T>(t.e, scratch);
+  else
+    __syncthreads();
 }
-__device__ __forceinline__ double* draft_lse(const VerifyArgs& a, int64_t b) {
-  return a.ws + a.B * (a.D + 1) + b * a.D;
-}
 
-// The test of token i (any lane may make any test), from the rows' log-sum-exps.
+// Eight consecutive elements of a row.
 template <class TI>
-__device__ __forceinline__ int test_token(const VerifyArgs& a, int64_t b, int i) {
-  const int32_t x = a.ids[b * a.D + i];
-  const double L = target_lse(a, b)[i];
-  const float u = a.u[b * (a.D + 1) + i];
-  if ((uint32_t)x >= (uint64_t)a.V || !(L == L) || !(u >= 0.f && u < 1.f)) return kBad;
-  const double p =
-      exp((double)load_elem<TI>((const char*)a.target + (b * (a.D + 1) + i) * a.ld * TI::BYTES, x) - L);
-  double q = 1.0;
-  if (a.draft) {
-    const double Lq = draft_lse(a, b)[i];
-    if (!(Lq == Lq)) return kBad;
-    q = exp((double)load_elem<TI>((const char*)a.draft + (b * a.D + i) * a.ldd * TI::BYTES, x) - Lq);
+struct Group;
+template <>
+struct Group<InBf16> {
+  u32x4 x;
+};
+template <>
+struct Group<InF32> {
+  u32x4 x, y;
+};
+// (the whole group lies in the row)
+template <class TI>
+__device__ __forceinline__ Group<TI> group_load(const char* row, uint32_t g) {
+  Group<TI> r;
+  const u32x4* p = (const u32x4*)(row + (size_t)g * 8 * TI::BYTES);
+  r.x = __builtin_nontemporal_load(p);
+  if constexpr (TI::BYTES == 4) r.y = __builtin_nontemporal_load(p + 1);
+  return r;
+}
+// (elements at or past V, and groups at or past g1, read as -inf)
+template <class TI>
+__device__ __forceinline__ Group<TI> group_load_end(const char* row, uint32_t g, uint32_t g1,
+                                                    int64_t V) {
+  if (g < g1 && (int64_t)g * 8 + 8 <= V) return group_load<TI>(row, g);
+  Group<TI> r;
+  if constexpr (TI::BYTES == 2) {
+    r.x = u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};
+  } else {
+    r.x = u32x4{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u};
+    r.y = r.x;
   }
+  if (g < g1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if ((int64_t)g * 8 + e >= V) continue;
+      if constexpr (TI::BYTES == 2) {
+        const uint32_t b = ((const uint16_t*)row)[(size_t)g * 8 + e];
+        r.x[e / 2] = e & 1 ? (r.x[e / 2] & 0xFFFFu) | b << 16 : (r.x[e / 2] & 0xFFFF0000u) | b;
+      } else {
+        const uint32_t b = ((const uint32_t*)row)[(size_t)g * 8 + e];
+        if (e < 4)
+          r.x[e & 3] = b;
+        else
+          r.y[e & 3] = b;
+      }
+    }
+  }
+  return r;
+}
+template <class TI>
+__device__ __forceinline__ void group_values(const Group<TI>& g, float (&f)[8]) {
+  if constexpr (TI::BYTES == 2) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      f[2 * d] = __uint_as_float(g.x[d] << 16);
+      f[2 * d + 1] = __uint_as_float(g.x[d] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      f[d] = __uint_as_float(g.x[d]);
+      f[4 + d] = __uint_as_float(g.y[d]);
+    }
+  }
+}
+
+// exp(z) of a group's elements; rare is set where one is not below kVerTop.  By
+// the table, where a wavefront's values are all of magnitude [2^-17, 640), one LDS
+// read each.
+template <bool TABLE>
+__device__ __forceinline__ double table_term(uint32_t t, const VerTab<TABLE>& tab, double c2,
+                                             bool& rare) {
+  const float z = tab_logit(t);
+  const double d = (double)z;
+  // (tiny: the series' next term is below 7.5e-17; and at most -640, or rare)
+  const double tiny = fma(d, fma(d, 0.5, 1.0), 1.0), low = exp_reduced(d, tab.p, c2);
+  const bool is_tiny = t >= kTabTinyAt, in = t < kTabSize;
+  rare |= !in && !is_tiny && !(z < 0.f);
+  return in ? tab.e[min(t, kTabSize)] : is_tiny ? tiny : low;
+}
+template <class TI, bool TABLE>
+__device__ __forceinline__ void group_terms(const Group<TI>& g, const VerTab<TABLE>& tab,
+                                            double c2, bool& rare, double (&w)[8]) {
+  if constexpr (TABLE) {
+    u16x2 t[4], top = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      t[k] = tab_index(g.x[k]);
+      top = __builtin_elementwise_max(top, t[k]);
+    }
+    if (__ballot(top[0] >= kTabSize || top[1] >= kTabSize) == 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[2 * k] = tab.e[t[k][0]];
+        w[2 * k + 1] = tab.e[t[k][1]];
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[2 * k] = table_term(t[k][0], tab, c2, rare);
+        w[2 * k + 1] = table_term(t[k][1], tab, c2, rare);
+      }
+    }
+  } else {
+    float f[8];
+    group_values<TI>(g, f);
+    float top = f[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = max_nan(top, f[e]);
+    rare |= !(top < kVerTop);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = exp_reduced((double)f[e], tab.p, c2);
+  }
+}
+
+// ---------------------------------------------------------------- sums of the rows
+
+__device__ __forceinline__ double wave_sum_f64(double v) {  // the same in every lane
+  return from_lane(wave_incl_scan_f64(v), 63);
+}
+
+// The record of groups [g0, g1) of a row, by one wavefront, in tiles of K groups per
+// lane.
+template <class TI>
+constexpr int ver_k() { return TI::BYTES == 2 ? 4 : 2; }
+template <class TI, bool TABLE>
+__device__ __forceinline__ VerRec part_record(const char* row, uint32_t g0, uint32_t g1, int64_t V,
+                                              const VerTab<TABLE>& tab) {
+  constexpr int K = ver_k<TI>();
+  const uint32_t lane = threadIdx.x & 63;
+  const double c2 = c2_reg();
+  const uint32_t full = min(g1, (uint32_t)(V >> 3));  // groups that lie in the row
+  double acc[4] = {0.0, 0.0, 0.0, 0.0};
+  bool rare = false;
+  auto add = [&](const Group<TI>& g) {
+    if constexpr (TABLE) {
+      u16x2 t[4], top = {0, 0};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        t[k] = tab_index(g.x[k]);
+        top = __builtin_elementwise_max(top, t[k]);
+      }
+      if (__ballot(top[0] >= kTabSize || top[1] >= kTabSize) == 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          acc[k] += tab.e[t[k][0]];
+          acc[k] += tab.e[t[k][1]];
+        }
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) {
+          const u16x2 u = e < 4 ? (e < 2 ? t[0] : t[1]) : (e < 6 ? t[2] : t[3]);
+          acc[0] += table_term(e & 1 ? u[1] : u[0], tab, c2, rare);
+        }
+      }
+    } else {
+      double v[8];
+      group_terms<TI, TABLE>(g, tab, c2, rare, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e & 3] += v[e];
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (a group at a time: more do not fit the registers)
+  };
+  auto load = [&](Group<TI> (&x)[K], uint32_t at) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = group_load<TI>(row, at + 64 * k + lane);
+  };
+  uint32_t at = g0;
+  int tiles = full > g0 ? (int)((full - g0) / (64u * K)) : 0;
+  if (tiles > 0) {
+    Group<TI> x[K], y[K];
+    load(x, at);
+    // (two tiles a turn, the next one on its way meanwhile)
+    for (; tiles > 2; tiles -= 2, at += 128u * K) {
+      load(y, at + 64u * K);
+#pragma unroll
+      for (int k = 0; k < K; ++k) add(x[k]);
+      load(x, at + 128u * K);
+#pragma unroll
+      for (int k = 0; k < K; ++k) add(y[k]);
+    }
+    if (tiles == 2) load(y, at + 64u * K);
+#pragma unroll
+    for (int k = 0; k < K; ++k) add(x[k]);
+    if (tiles == 2) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) add(y[k]);
+    }
+    at += 64u * K * tiles;
+  }
+#pragma unroll 1
+  for (; at < g1; at += 64) add(group_load_end<TI>(row, at + lane, g1, V));
+  const double s = wave_sum_f64((acc[0] + acc[1]) + (acc[2] + acc[3]));
+  if (__ballot(rare) == 0 && s >= kVerMinSum) return VerRec{0.0, s};
+  float m = kNegInf;
+#pragma unroll 1
+  for (uint32_t g = g0 + lane; g < g1; g += 64) {
+    float f[8];
+    group_values<TI>(group_load_end<TI>(row, g, g1, V), f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max_nan(m, f[e]);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = max_nan(m, __shfl_xor(m, o, 64));
+  if (m == kNegInf) return VerRec{(double)kNegInf, 0.0};
+  if (!(m < __builtin_huge_valf())) return VerRec{0.0, __builtin_nan("")};
+  double t = 0.0;
+#pragma unroll 1
+  for (uint32_t g = g0 + lane; g < g1; g += 64) {
+    float f[8];
+    group_values<TI>(group_load_end<TI>(row, g, g1, V), f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t += term(f[e], (double)m, tab.p, c2);
+  }
+  return VerRec{(double)m, wave_sum_f64(t)};
+}
+
+// Words and doubles that workgroups pass each other within a launch: device-scope
+// stores go through to where every XCD's device-scope loads read.  shared_wait()
+// between such stores and the counter that announces them: they have arrived.  (A
+// release fence would write back the XCD's whole L2 as well, which cost 130 of
+// 160 us at 64 sequences.)
+__device__ __forceinline__ void shared_wait() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
+}
+template <class T>
+__device__ __forceinline__ T shared_load(const T* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class T>
+__device__ __forceinline__ void shared_store(T* p, T v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The workspace: rows (target, then draft), their parts, chunk masses, then the
+// words that start at 0.
+struct VerWs {
+  VerRow* row;
+  VerRec* rec;
+  double* mass;
+  uint32_t *test, *count, *stop, *done;
+};
+__device__ __forceinline__ VerWs ver_ws(const VerifyArgs& a) {
+  VerWs w;
+  const int64_t R = a.B * (2 * a.D + 1);
+  w.row = (VerRow*)a.ws;
+  w.rec = (VerRec*)(w.row + R);
+  w.mass = (double*)(w.rec + R * a.parts);
+  w.test = (uint32_t*)(w.mass + (a.draw_parts > 1 ? a.B * (int64_t)a.nchunk : 0));
+  w.count = w.test + a.B * (a.D + 1);
+  w.stop = w.count + a.B * (a.D + 1);
+  w.done = w.stop + a.B;
+  return w;
+}
+__device__ __forceinline__ int64_t target_row(const VerifyArgs& a, int64_t b, int i) {
+  return b * (a.D + 1) + i;
+}
+__device__ __forceinline__ int64_t draft_row(const VerifyArgs& a, int64_t b, int i) {
+  return b * a.D + i;
+}
+template <class TI>
+__device__ __forceinline__ const char* target_ptr(const VerifyArgs& a, int64_t b, int i) {
+  return (const char*)a.target + target_row(a, b, i) * a.ld * TI::BYTES;
+}
+template <class TI>
+__device__ __forceinline__ const char* draft_ptr(const VerifyArgs& a, int64_t b, int i) {
+  return (const char*)a.draft + draft_row(a, b, i) * a.ldd * TI::BYTES;
+}
+__device__ __forceinline__ int drafted(const VerifyArgs& a, int64_t b) {
+  if (a.mask && a.mask[b] == 0) return -1;
+  const int n = a.lens ? a.lens[b] : a.D;
+  return n > a.D ? -1 : n;
+}
+
+// A row from its parts (at most 64, one to a lane; the order of the sum is fixed).
+__device__ __forceinline__ VerRow row_of_parts(const VerRec* r, int parts, const double* tab) {
+  const int lane = threadIdx.x & 63;
+  VerRec x{(double)kNegInf, 0.0};
+  if (lane < parts) x = VerRec{shared_load(&r[lane].m), shared_load(&r[lane].s)};
+  double m = x.m;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o, 64));
+  if (m == (double)kNegInf) return VerRow{__builtin_nan(""), m};
+  const double s = wave_sum_f64(x.s * (x.m == m ? 1.0 : exp_neg(x.m - m, tab)));
+  return VerRow{m + log(s), m};
+}
+
+// The test of token i of sequence b, its rows summed (one lane).
+template <class TI>
+__device__ __forceinline__ uint32_t test_token(const VerifyArgs& a, int64_t b, int i, double L,
+                                               double Lq, const double* tab) {
+  const int32_t x = a.ids[b * a.D + i];
+  const float u = a.u[b * (a.D + 1) + i];
+  if ((uint64_t)(uint32_t)x >= (uint64_t)a.V || !(L == L) || !(Lq == Lq) || !(u >= 0.f && u < 1.f))
+    return kBad;
+  const double p = exp_neg((double)load_elem<TI>(target_ptr<TI>(a, b, i), x) - L, tab);
+  const double q =
+      a.draft ? exp_neg((double)load_elem<TI>(draft_ptr<TI>(a, b, i), x) - Lq, tab) : 1.0;
   return (double)u * q < p ? kKept : kRefused;
 }
 
-// How many of a sequence's first `upto` tokens are kept before the first that is
-// not (wave-uniform; every lane of the wave takes part).
-template <class TI>
-__device__ __forceinline__ int kept_tokens(const VerifyArgs& a, int64_t b, int upto, int& test) {
-  const int lane = threadIdx.x & 63;
-  test = kKept;
-  for (int i0 = 0; i0 < upto; i0 += 64) {
-    const int i = i0 + lane;
-    const int t = i < upto ? test_token<TI>(a, b, i) : kKept;
-    const int f = first_lane(__ballot(t != kKept));
-    if (f >= 0) {
-      test = __builtin_amdgcn_readlane(t, f);
-      return i0 + f;
+__global__ void __launch_bounds__(256) k_verify_clear(uint32_t* words, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    words[i] = 0u;
+}
+
+// The rows of positions [pos0, pos1) that the sequences still need: of sequence b,
+// `targets` and then `drafts` rows from pos0 on.
+struct RoundRows {
+  int targets, drafts;
+};
+__device__ __forceinline__ RoundRows round_rows(const VerifyArgs& a, const VerWs& ws, int64_t b,
+                                                int pos0, int pos1) {
+  const int n = drafted(a, b);
+  // (refused before this round; what this round refuses must not change its rows, which
+  // every workgroup counts for itself)
+  if (n < pos0 || pos0 + (int)ws.stop[b] > a.D + 1) return RoundRows{0, 0};
+  return RoundRows{min(pos1 - 1, n) - pos0 + 1, a.draft ? min(pos1, n) - pos0 : 0};
+}
+
+// A row's parts are a wavefront's items.  Up to kListed sequences, the workgroup
+// counts the round's rows in order, and cuts them so that the wavefronts share what
+// there is to do equally, however few sequences are left; of more, every row has its items, and
+// those of rows that are not needed are left out.  Who ends a position's last part
+// makes its test.
+constexpr int kListed = 2048;
+template <class TI, bool TABLE>
+__global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, int pos0, int pos1) {
+  __shared__ VerTab<TABLE> tab;
+  __shared__ union {
+    double factors[TABLE ? kTabBinades * 32 : 1];
+    uint32_t before[kListed];  // rows of the sequences before each
+  } c;
+  __shared__ uint32_t wsum[kVerWaves];
+  const int tid = threadIdx.x;
+  const uint32_t lane = tid & 63;
+  const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6);
+  const VerWs ws = ver_ws(a);
+  const uint32_t W = gridDim.x * kVerWaves;
+  uint32_t parts = (uint32_t)a.parts, part_groups = a.part_groups;
+  const uint32_t groups = (uint32_t)((a.V + 7) >> 3);
+  const bool listed = a.B <= kListed;
+  ver_setup<TABLE, kVerThreads>(tab, c.factors);
+  uint64_t items;
+  const uint32_t most = (uint32_t)(pos1 - pos0) * (a.draft ? 2u : 1u);  // rows of a sequence
+  if (listed) {
+    constexpr int PER = kListed / kVerThreads;
+    uint32_t mine[PER], sum = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int64_t b = (int64_t)tid * PER + k;
+      mine[k] = sum;
+      if (b < a.B) {
+        const RoundRows r = round_rows(a, ws, b, pos0, pos1);
+        sum += (uint32_t)(r.targets + r.drafts);
+      }
+    }
+    uint32_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t x = (uint32_t)__shfl_up((int)incl, o, 64);
+      if (lane >= (uint32_t)o) incl += x;
+    }
+    if (lane == 63) wsum[w] = incl;
+    __syncthreads();  // (the table's factors are no longer needed)
+    uint32_t at = incl - sum;
+    for (uint32_t k = 0; k < w; ++k) at += wsum[k];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) c.before[tid * PER + k] = at + mine[k];
+    uint32_t all = 0;
+#pragma unroll
+    for (int k = 0; k < kVerWaves; ++k) all += wsum[k];
+    __syncthreads();
+    // as many parts to a row as give the wavefronts the least to do: whole items, and
+    // for each kItemCost of a row besides (the first loads and the record)
+    constexpr float kItemCost = 0.03f;
+    const uint32_t tiles = (groups + 255) / 256;
+    float best = 1e30f;
+    for (uint32_t p = 1; p <= (uint32_t)a.parts; ++p) {
+      const float cost = (float)((all * p + W - 1) / W) * (1.f / (float)p + kItemCost);
+      if (cost < best) {
+        best = cost;
+        parts = p;
+      }
+    }
+    part_groups = (tiles + parts - 1) / parts * 256;
+    parts = (groups + part_groups - 1) / part_groups;
+    items = (uint64_t)all * parts;
+  } else {
+    items = (uint64_t)a.B * most * parts;
+  }
+  uint64_t k = (uint64_t)blockIdx.x * kVerWaves + w;
+  while (k < items) {
+    // up to 64 items, the j-th kept in mind by lane j; then they are announced together
+    int64_t my_tr = -1;
+    uint32_t my_b = 0;
+    int my_pos = 0, my_pair = 0;
+    uint32_t held = 0;
+    for (; k < items && held < 64; k += W) {
+      const uint64_t u = k / parts;
+      const uint32_t part = (uint32_t)(k - u * parts);
+      uint32_t r;
+      int64_t b;
+      if (listed) {
+        uint32_t lo = 0, hi = (uint32_t)a.B - 1;  // the last sequence with before <= u
+        while (lo < hi) {
+          const uint32_t mid = (lo + hi + 1) >> 1;
+          if (c.before[mid] <= (uint32_t)u) lo = mid;
+          else hi = mid - 1;
+        }
+        b = lo;
+        r = (uint32_t)u - c.before[lo];
+      } else {
+        b = (int64_t)(u / most);
+        r = (uint32_t)(u - (uint64_t)b * most);
+      }
+      b = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b);
+      r = (uint32_t)__builtin_amdgcn_readfirstlane((int)r);
+      const RoundRows rr = round_rows(a, ws, b, pos0, pos1);
+      if (r >= (uint32_t)(rr.targets + rr.drafts)) continue;  // (not listed)
+      const bool draft = r >= (uint32_t)rr.targets;
+      const int pos = pos0 + (int)(draft ? r - rr.targets : r);
+      if (pos + (int)ws.stop[b] > a.D + 1) continue;  // (refused by now)
+      const uint32_t g0 = part * part_groups, g1 = min(g0 + part_groups, groups);
+      const int64_t tr = target_row(a, b, pos), dr = a.B * (a.D + 1) + draft_row(a, b, pos);
+      const VerRec x = part_record<TI, TABLE>(
+          draft ? draft_ptr<TI>(a, b, pos) : target_ptr<TI>(a, b, pos), g0, g1, a.V, tab);
+      VerRec* rec = ws.rec + (draft ? dr : tr) * a.parts + part;
+      if (lane == 0) {
+        shared_store(&rec->m, x.m);
+        shared_store(&rec->s, x.s);
+      }
+      if (lane == held) {
+        my_tr = tr;
+        my_b = (uint32_t)b;
+        my_pos = pos;
+        my_pair = a.draft && pos < drafted(a, b);
+      }
+      ++held;
+    }
+    shared_wait();
+    uint32_t done = 0;
+    if (my_tr >= 0)
+      done = 1 + __hip_atomic_fetch_add(&ws.count[my_tr], 1u, __ATOMIC_RELAXED,
+                                        __HIP_MEMORY_SCOPE_AGENT);
+    // those that ended their position make its test
+    uint64_t ends = __ballot(my_tr >= 0 && done == parts * (my_pair ? 2u : 1u));
+    while (ends != 0) {
+      const int j = first_lane(ends);
+      ends &= ends - 1;
+      const int64_t b = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)my_b, j);
+      const int pos = __builtin_amdgcn_readlane(my_pos, j);
+      const bool pair = __builtin_amdgcn_readlane(my_pair, j) != 0;
+      const int64_t tr = target_row(a, b, pos), dr = a.B * (a.D + 1) + draft_row(a, b, pos);
+      const VerRow rt = row_of_parts(ws.rec + tr * a.parts, (int)parts, tab.p);
+      const VerRow rd =
+          pair ? row_of_parts(ws.rec + dr * a.parts, (int)parts, tab.p) : VerRow{0.0, 0.0};
+      if (lane == 0) {
+        ws.row[tr] = rt;
+        if (pair) ws.row[dr] = rd;
+        if (pos < drafted(a, b)) {
+          const uint32_t t = test_token<TI>(a, b, pos, rt.L, rd.L, tab.p);
+          ws.test[tr] = t;
+          // (D + 1 - the first refusal, or 0)
+          if (t != kKept)
+            __hip_atomic_fetch_max(&ws.stop[b], (uint32_t)(a.D + 1 - pos), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+        }
+      }
     }
   }
-  return upto;
 }
 
-__device__ __forceinline__ int drafted(const VerifyArgs& a, int64_t b) {
-  return a.lens ? a.lens[b] : a.D;
-}
-
-// The log-sum-exp of each target and draft row of positions [pos0, pos1) of the
-// sequences whose tokens before pos0 are all kept: a workgroup per row, target
-// rows first.
-// (WIDE: rows of 2 GiB and more, whose offsets pass a buffer's 32 bits.)
-template <class TI, bool WIDE>
-__global__ void __launch_bounds__(kVerThreads) k_verify_rows(VerifyArgs a, int pos0, int pos1) {
-  constexpr int W = kVerThreads / 64;
-  __shared__ double tab[kExpTab];
-  __shared__ float redm[W];
-  __shared__ double reds[W];
-  const int np = pos1 - pos0;
-  const int64_t per = a.B * np;
-  const bool is_draft = blockIdx.x >= per;
-  const int64_t k = blockIdx.x - (is_draft ? per : 0);
-  const int64_t b = k / np;
-  const int i = pos0 + (int)(k - b * np);
-  if (a.mask && a.mask[b] == 0) return;
-  const int n = drafted(a, b);
-  if (n < 0 || n > a.D || i > n || (is_draft && i >= n)) return;
-  int test;
-  if (pos0 > 0 && kept_tokens<TI>(a, b, pos0, test) < pos0) return;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int j = tid; j < kExpTab; j += kVerThreads) tab[j] = exp2((double)j / kExpTab);
-  __syncthreads();
-  const char* row = is_draft ? (const char*)a.draft + (b * a.D + i) * a.ldd * TI::BYTES
-                             : (const char*)a.target + (b * (a.D + 1) + i) * a.ld * TI::BYTES;
-  const uint32_t nvec = (uint32_t)a.nvec;
-  const uint32_t steps = (nvec + kSmpStepVecs - 1) / kSmpStepVecs;
-  // one DPP row per chunk of 128 vectors; a lane of it merges its chunks
-  float m = kNegInf;
-  double s = 0.0;
-  for (uint32_t q0 = 4u * w; q0 < steps; q0 += 4u * W) {
-    float mq;
-    double sq;
-    chunk_record<TI, WIDE>(row, q0 + ((uint32_t)lane >> 4), q0, kSmpStepVecs, nvec, a.tail, tab, mq,
-                           sq);
-    const float mn = max_nan(m, mq);
-    s = mn == kNegInf ? 0.0
-                      : (m == kNegInf ? 0.0 : s * exp_neg((double)m - (double)mn, tab)) +
-                            (mq == kNegInf ? 0.0 : sq * exp_neg((double)mq - (double)mn, tab));
-    m = mn;
-  }
-  // the four DPP rows of each wave, then the waves
-  float wm = m;
-  wm = max_nan(wm, __shfl_xor(wm, 16, 64));
-  wm = max_nan(wm, __shfl_xor(wm, 32, 64));
-  if (lane == 0) redm[w] = wm;
-  __syncthreads();
-  float M = redm[0];
-  for (int k2 = 1; k2 < W; ++k2) M = max_nan(M, redm[k2]);
-  double sw = m == kNegInf ? 0.0 : s * exp_neg((double)m - (double)M, tab);
-  sw += __shfl_xor(sw, 16, 64);
-  sw += __shfl_xor(sw, 32, 64);
-  if (lane == 0) reds[w] = sw;
-  __syncthreads();
-  if (tid == 0) {
-    double S = 0.0;
-    for (int k2 = 0; k2 < W; ++k2) S += reds[k2];
-    const bool defined = S > 0.0 && M < __builtin_huge_valf();
-    double* to = is_draft ? draft_lse(a, b) + i : target_lse(a, b) + i;
-    *to = defined ? (double)M + log(S) : __builtin_nan("");
-  }
-}
+// ---------------------------------------------------------------- the draw
 
 // The masses that the last token of a sequence is drawn from.
 enum Mass : int { kTarget, kResidual, kWithout };  // p; max(p - q, 0); p but for x
@@ -139,59 +540,90 @@ enum Mass : int { kTarget, kResidual, kWithout };  // p; max(p - q, 0); p but fo
 template <class TI>
 struct DrawRow {
   const char* z;
-  const char* y;  // kResidual
+  const char* y;     // kResidual
   double L, Lq;
-  int64_t x;      // kWithout: the refused token
+  double ps, qs;     // exp(-L), exp(-Lq)
+  int64_t x;         // kWithout: the refused token
   int mass;
-  const double* tab;
+  bool direct;       // from exp(z) (as the rows were summed), else from exp(z - L)
 };
 
-// This lane's eight masses of the 128-vector step at vector v0 (0 at or past c1).
-template <class TI>
-__device__ __forceinline__ void step_masses(const DrawRow<TI>& d, uint32_t v0, uint32_t c1,
-                                            uint32_t nvec, int tail, double c2, double (&w)[8]) {
-  typename TI::Vec xz[2], xy[2];
-  step_load<TI>(d.z, v0, c1, nvec, tail, xz);
-  if (d.mass == kResidual) step_load<TI>(d.y, v0, c1, nvec, tail, xy);
-  const uint32_t v = v0 + 2u * (uint32_t)(threadIdx.x & 63);
+// The masses of a lane's group, in index order.
+template <class TI, bool TABLE>
+__device__ __forceinline__ void group_masses(const DrawRow<TI>& d, const Group<TI>& z,
+                                             const Group<TI>& y, uint32_t g, const VerTab<TABLE>& tab,
+                                             double c2, double (&w)[8]) {
+  bool rare = false;
+  if (d.direct) {
+    group_terms<TI, TABLE>(z, tab, c2, rare, w);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float fz[4], fy[4];
-    unpack<TI>(xz[h], fz);
-    if (d.mass == kResidual) unpack<TI>(xy[h], fy);
+    for (int e = 0; e < 8; ++e) w[e] *= d.ps;
+    if (d.mass == kResidual) {
+      double v[8];
+      group_terms<TI, TABLE>(y, tab, c2, rare, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      double p = exp_reduced((double)fz[e] - d.L, d.tab, c2);
-      if (d.mass == kResidual) p = fmax(p - exp_reduced((double)fy[e] - d.Lq, d.tab, c2), 0.0);
-      if (d.mass == kWithout && (int64_t)(v + h) * 4 + e == d.x) p = 0.0;
-      w[4 * h + e] = v + h < c1 ? p : 0.0;
+      for (int e = 0; e < 8; ++e) w[e] = fmax(fma(-v[e], d.qs, w[e]), 0.0);
+    }
+  } else {
+    float f[8], h[8];
+    group_values<TI>(z, f);
+    group_values<TI>(y, h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      double v = exp_reduced((double)f[e] - d.L, tab.p, c2);
+      if (d.mass == kResidual) v = fmax(v - exp_reduced((double)h[e] - d.Lq, tab.p, c2), 0.0);
+      w[e] = v;
     }
   }
+  if (d.mass == kWithout && (d.x >> 3) == (int64_t)g) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if ((d.x & 7) == e) w[e] = 0.0;
+  }
+}
+// (of group g, read here; groups at or past g1 have none)
+template <class TI, bool TABLE>
+__device__ __forceinline__ void masses_at(const VerifyArgs& a, const DrawRow<TI>& d, uint32_t g,
+                                          uint32_t g1, const VerTab<TABLE>& tab, double c2,
+                                          double (&w)[8]) {
+  const Group<TI> z = group_load_end<TI>(d.z, g, g1, a.V);
+  const Group<TI> y = d.mass == kResidual ? group_load_end<TI>(d.y, g, g1, a.V) : z;
+  group_masses<TI, TABLE>(d, z, y, g, tab, c2, w);
 }
 
-// The index drawn from the masses of chunk q: the first at which they exceed r,
-// or (where rounding leaves none) the first or last of positive mass.
-template <class TI>
-__device__ __forceinline__ int64_t mass_element(const DrawRow<TI>& d, DrawAt at, uint32_t CV,
-                                                uint32_t nvec, int tail, double c2) {
+struct DrawLds {
+  double s[kSmpMaxChunks];  // chunk masses
+  double p[kVerThreads];    // inclusive prefix of the runs
+  double wt[kVerWaves];
+  uint32_t word;
+};
+
+// The index drawn from the masses of chunk at.q (chunks of CG groups): the first at
+// which they exceed at.r, or (where rounding leaves none) the first or last of
+// positive mass.  (One wavefront.)
+template <class TI, bool TABLE>
+__device__ __forceinline__ int64_t mass_element(const VerifyArgs& a, const DrawRow<TI>& d,
+                                                DrawAt at, uint32_t CG, uint32_t groups,
+                                                const VerTab<TABLE>& tab, double c2) {
   if (at.q < 0) return -1;
-  const uint32_t c0 = (uint32_t)at.q * CV, c1 = min(c0 + CV, nvec);
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t c0 = (uint32_t)at.q * CG, c1 = min(c0 + CG, groups);
   double w[8];
   if (at.pick == kCross) {
     double acc = 0.0;
-    for (uint32_t v0 = c0; v0 < c1; v0 += kSmpStepVecs) {
-      step_masses<TI>(d, v0, c1, nvec, tail, c2, w);
+    for (uint32_t g = c0; g < c1; g += 64) {
+      masses_at<TI, TABLE>(a, d, g + lane, c1, tab, c2, w);
       const int k = step_crossing(w, at.r, 1.0, acc);
-      if (k >= 0) return (int64_t)v0 * 4 + k;
+      if (k >= 0) return (int64_t)g * 8 + k;
       if (k == -2) break;
     }
     at.pick = kLast;
   }
   const bool last = at.pick == kLast;
-  const uint32_t nsteps = (c1 - c0 + kSmpStepVecs - 1) / kSmpStepVecs;
-  for (uint32_t k = 0; k < nsteps; ++k) {
-    const uint32_t v0 = c0 + (last ? nsteps - 1 - k : k) * kSmpStepVecs;
-    step_masses<TI>(d, v0, c1, nvec, tail, c2, w);
+  const uint32_t steps = (c1 - c0 + 63) / 64;
+  for (uint32_t k = 0; k < steps; ++k) {
+    const uint32_t g = c0 + (last ? steps - 1 - k : k) * 64;
+    masses_at<TI, TABLE>(a, d, g + lane, c1, tab, c2, w);
     int ef = -1, eb = -1;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -200,139 +632,221 @@ __device__ __forceinline__ int64_t mass_element(const DrawRow<TI>& d, DrawAt at,
         eb = e;
       }
     const int vl = last ? last_lane(__ballot(eb >= 0)) : first_lane(__ballot(ef >= 0));
-    if (vl >= 0) return ((int64_t)v0 + 2 * vl) * 4 + __builtin_amdgcn_readlane(last ? eb : ef, vl);
+    if (vl >= 0) return (int64_t)(g + vl) * 8 + __builtin_amdgcn_readlane(last ? eb : ef, vl);
   }
   return -1;
 }
 
-struct DrawLds {
-  double s[kSmpMaxChunks];  // chunk masses
-  double p[kVerThreads];    // inclusive prefix of the runs
-  double tab[kExpTab];
-  double wt[kVerThreads / 64];
-};
-
-// A sequence's tokens: the kept ones, then the draw.  A workgroup per sequence.
-template <class TI>
-__global__ void __launch_bounds__(kVerThreads) k_verify_draw(VerifyArgs a) {
-  constexpr int T = kVerThreads, W = T / 64;
-  __shared__ DrawLds c;
-  const int64_t b = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int32_t* ids = a.ids_out + b * (a.D + 1);
-  float* logp = a.logp ? a.logp + b * (a.D + 1) : nullptr;
-  const int n = drafted(a, b);
-  const bool masked = a.mask && a.mask[b] == 0;
-  int kept = 0, test = kKept;
-  if (!masked) {
-    test = kBad;
-    if (n >= 0 && n <= a.D) kept = kept_tokens<TI>(a, b, n, test);
-  }
-  for (int i = tid; i <= a.D; i += T) {
-    const bool mine = !masked && i < kept;
-    const int32_t x = mine ? a.ids[b * a.D + i] : -1;
-    ids[i] = x;
-    if (logp)
-      logp[i] = mine ? (float)((double)load_elem<TI>(
-                                   (const char*)a.target + (b * (a.D + 1) + i) * a.ld * TI::BYTES, x) -
-                               target_lse(a, b)[i])
-                     : 0.f;
-  }
-  if (tid == 0) a.accepted[b] = kept;
-  if (masked) return;
-  __syncthreads();  // (the slot of the draw is written again below)
-  const float u = a.u[b * (a.D + 1) + a.D];
-  DrawRow<TI> d;
-  d.z = (const char*)a.target + (b * (a.D + 1) + kept) * a.ld * TI::BYTES;
-  d.L = test == kBad ? __builtin_nan("") : target_lse(a, b)[kept];
-  d.y = nullptr;
-  d.Lq = 0.0;
-  d.x = -1;
-  d.mass = kTarget;
-  if (test == kRefused) {
-    d.mass = a.draft ? kResidual : kWithout;
-    d.x = a.ids[b * a.D + kept];
-    if (a.draft) {
-      d.y = (const char*)a.draft + (b * a.D + kept) * a.ldd * TI::BYTES;
-      d.Lq = draft_lse(a, b)[kept];
+// The masses of chunks [q0, q1), each by a wavefront; out[q] (shared: by other
+// workgroups, too).
+template <class TI, bool TABLE>
+__device__ __forceinline__ void chunk_masses(const VerifyArgs& a, const DrawRow<TI>& d, uint32_t q0,
+                                             uint32_t q1, uint32_t CG, uint32_t groups,
+                                             const VerTab<TABLE>& tab, double c2, double* out,
+                                             bool shared) {
+  constexpr int K = TI::BYTES == 2 ? 4 : 2;  // chunks of one step at a time
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t full = (uint32_t)(a.V >> 3);
+  auto put = [&](uint32_t q, double sum) {
+    const double all = wave_incl_scan_f64(sum);
+    if (lane == 63) {
+      if (shared)
+        shared_store(out + q, all);
+      else
+        out[q] = all;
     }
-  }
-  if (!(d.L == d.L) || !(u >= 0.f && u < 1.f)) {
-    if (tid == 0 && logp) logp[kept] = __builtin_nanf("");
-    return;
-  }
-  for (int j = tid; j < kExpTab; j += T) c.tab[j] = exp2((double)j / kExpTab);
-  __syncthreads();
-  d.tab = c.tab;
-  const double c2 = c2_reg();
-  const uint32_t nvec = (uint32_t)a.nvec;
-  const uint32_t steps = (nvec + kSmpStepVecs - 1) / kSmpStepVecs;
-  const uint32_t G = (steps + kSmpMaxChunks - 1) / kSmpMaxChunks;
-  const uint32_t CV = G * kSmpStepVecs, nchunk = (nvec + CV - 1) / CV;
-  double S = 0.0;
-  for (;;) {
-    for (uint32_t q = w; q < nchunk; q += W) {
-      const uint32_t c0 = q * CV, c1 = min(c0 + CV, nvec);
-      double sum = 0.0;
-      for (uint32_t v0 = c0; v0 < c1; v0 += kSmpStepVecs) {
-        double m[8];
-        step_masses<TI>(d, v0, c1, nvec, a.tail, c2, m);
+  };
+  uint32_t q = q0 + w * K;
+  if (CG == 64) {
+    for (; q + K <= q1 && (q + K) * 64 <= full; q += kVerWaves * K) {
+      Group<TI> z[K], y[K];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += m[e];
+      for (int k = 0; k < K; ++k) {
+        z[k] = group_load<TI>(d.z, (q + k) * 64 + lane);
+        y[k] = d.mass == kResidual ? group_load<TI>(d.y, (q + k) * 64 + lane) : z[k];
       }
-      const double all = wave_incl_scan_f64(sum);
-      if (lane == 63) c.s[q] = all;
-    }
-    __syncthreads();
-    const uint32_t C = (nchunk + T - 1) / T;
-    const uint32_t r0 = min((uint32_t)tid * C, nchunk), r1 = min(r0 + C, nchunk);
-    double run = 0.0;
-    for (uint32_t q = r0; q < r1; ++q) run += c.s[q];
-    const double incl = wave_incl_scan_f64(run);
-    if (lane == 63) c.wt[w] = incl;
-    __syncthreads();
-    double before = 0.0;
-    for (int k = 0; k < w; ++k) before += c.wt[k];
-    c.p[tid] = before + incl;
-    S = 0.0;
 #pragma unroll
-    for (int k = 0; k < W; ++k) S += c.wt[k];
-    __syncthreads();
-    // p(x) < q(x) leaves a residual; where rounding hides it the draw is from p
-    if (S > 0.0 || d.mass == kTarget) break;
-    d.mass = kTarget;
+      for (int k = 0; k < K; ++k) {
+        double v[8], sum = 0.0;
+        group_masses<TI, TABLE>(d, z[k], y[k], (q + k) * 64 + lane, tab, c2, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[e];
+        put(q + k, sum);
+      }
+    }
   }
-  if (w != 0) return;
-  const uint32_t C = (nchunk + T - 1) / T;
-  const DrawAt at = smp_locate<T>(c, nchunk, C, (double)u * S, S);
-  const int64_t id = mass_element<TI>(d, at, CV, nvec, a.tail, c2);
-  if (lane == 0) {
-    ids[kept] = (int32_t)id;
-    if (logp)
-      logp[kept] = id >= 0 ? (float)((double)load_elem<TI>(d.z, id) - d.L) : __builtin_nanf("");
+  for (; q < q1; q += kVerWaves * K) {
+#pragma unroll 1
+    for (uint32_t k = q; k < min(q + K, q1); ++k) {
+      double sum = 0.0;
+      const uint32_t c1 = min(k * CG + CG, groups);
+      for (uint32_t g = k * CG; g < c1; g += 64) {
+        double v[8];
+        masses_at<TI, TABLE>(a, d, g + lane, c1, tab, c2, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[e];
+      }
+      put(k, sum);
+    }
   }
 }
 
-template <class TI>
+// A sequence's tokens: the kept ones, then the draw.  Item k: part k % draw_parts of
+// the row that sequence k / draw_parts is drawn from; whoever ends a sequence's
+// last part draws.
+template <class TI, bool TABLE>
+__global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
+  __shared__ VerTab<TABLE> tab;
+  __shared__ DrawLds c;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const VerWs ws = ver_ws(a);
+  const uint32_t groups = (uint32_t)((a.V + 7) >> 3);
+  const uint32_t nchunk = (uint32_t)a.nchunk, CG = 64u * (uint32_t)a.chunk_steps;
+  const int parts = a.draw_parts;
+  const double c2 = c2_reg();
+  static_assert(kTabBinades * 32 <= kSmpMaxChunks, "the table's factors fit the masses");
+  ver_setup<TABLE, kVerThreads>(tab, c.s);
+  for (int64_t k = blockIdx.x; k < a.B * parts; k += gridDim.x) {
+    const int64_t b = k / parts;
+    const uint32_t part = (uint32_t)(k - b * parts);
+    int32_t* ids = a.ids_out + b * (a.D + 1);
+    float* logp = a.logp ? a.logp + b * (a.D + 1) : nullptr;
+    const bool masked = a.mask && a.mask[b] == 0;
+    const int n = drafted(a, b);
+    // the first token that is not kept
+    const uint32_t st = n < 0 ? 0 : ws.stop[b];
+    const int kept = n < 0 ? 0 : st ? a.D + 1 - (int)st : n;
+    const uint32_t test = n < 0 ? (uint32_t)kBad : st ? ws.test[b * (a.D + 1) + kept] : (uint32_t)kKept;
+    const float u = a.u[b * (a.D + 1) + a.D];
+    DrawRow<TI> d{};
+    VerRow rt{__builtin_nan(""), 0.0}, rd{0.0, 0.0};
+    if (!masked && test != kBad) {
+      rt = ws.row[target_row(a, b, kept)];
+      d.z = target_ptr<TI>(a, b, kept);
+      d.mass = kTarget;
+      if (test == kRefused) {
+        d.mass = a.draft ? kResidual : kWithout;
+        d.x = a.ids[b * a.D + kept];
+        if (a.draft) {
+          rd = ws.row[a.B * (a.D + 1) + draft_row(a, b, kept)];
+          d.y = draft_ptr<TI>(a, b, kept);
+        }
+      }
+      d.L = rt.L;
+      d.Lq = rd.L;
+      d.ps = exp(-rt.L);
+      d.qs = exp(-rd.L);
+      // (both rows summed as exp(z): no logit at or past kVerTop, and no tiny sum)
+      d.direct = rt.m == 0.0 && rd.m == 0.0;
+    }
+    const bool draws = rt.L == rt.L && u >= 0.f && u < 1.f;
+    if (parts > 1) {
+      if (draws) {
+        const uint32_t per = (nchunk + parts - 1) / parts;
+        const uint32_t q0 = min(part * per, nchunk), q1 = min(q0 + per, nchunk);
+        chunk_masses<TI, TABLE>(a, d, q0, q1, CG, groups, tab, c2,
+                                ws.mass + b * (int64_t)nchunk, true);
+        shared_wait();
+      }
+      __syncthreads();
+      if (tid == 0)
+        c.word = __hip_atomic_fetch_add(&ws.done[b], 1u, __ATOMIC_RELAXED,
+                                        __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)parts - 1;
+      __syncthreads();
+      const bool last = c.word != 0u;
+      __syncthreads();
+      if (!last) continue;
+    }
+    for (int i = tid; i <= a.D; i += kVerThreads) {
+      const bool mine = !masked && i < kept;
+      const int32_t x = mine ? a.ids[b * a.D + i] : -1;
+      if (i != kept || masked || !draws) ids[i] = x;
+      if (logp && (i != kept || masked || !draws))
+        logp[i] = mine ? (float)((double)load_elem<TI>(target_ptr<TI>(a, b, i), x) -
+                                 ws.row[target_row(a, b, i)].L)
+                       : (i == kept && !masked ? __builtin_nanf("") : 0.f);
+    }
+    if (tid == 0) a.accepted[b] = kept;
+    if (masked || !draws) continue;
+    double S = 0.0;
+    bool mine = parts == 1;  // this workgroup makes the masses
+    for (;;) {
+      if (mine)
+        chunk_masses<TI, TABLE>(a, d, 0, nchunk, CG, groups, tab, c2, c.s, false);
+      else
+        for (uint32_t q = tid; q < nchunk; q += kVerThreads)
+          c.s[q] = shared_load(ws.mass + b * (int64_t)nchunk + q);
+      __syncthreads();
+      const uint32_t C = (nchunk + kVerThreads - 1) / kVerThreads;
+      const uint32_t r0 = min((uint32_t)tid * C, nchunk), r1 = min(r0 + C, nchunk);
+      double run = 0.0;
+      for (uint32_t q = r0; q < r1; ++q) run += c.s[q];
+      const double incl = wave_incl_scan_f64(run);
+      if (lane == 63) c.wt[w] = incl;
+      __syncthreads();
+      double before = 0.0;
+      for (int i = 0; i < w; ++i) before += c.wt[i];
+      c.p[tid] = before + incl;
+      S = 0.0;
+#pragma unroll
+      for (int i = 0; i < kVerWaves; ++i) S += c.wt[i];
+      __syncthreads();
+      // p(x) < q(x) leaves a residual; where rounding hides it the draw is from p
+      if (S > 0.0 || d.mass == kTarget) break;
+      d.mass = kTarget;
+      d.direct = rt.m == 0.0;
+      mine = true;
+    }
+    if (w == 0) {
+      const uint32_t C = (nchunk + kVerThreads - 1) / kVerThreads;
+      const DrawAt at = smp_locate<kVerThreads>(c, nchunk, C, (double)u * S, S);
+      const int64_t id = mass_element<TI, TABLE>(a, d, at, CG, groups, tab, c2);
+      if (lane == 0) {
+        ids[kept] = (int32_t)id;
+        if (logp)
+          logp[kept] =
+              id >= 0 ? (float)((double)load_elem<TI>(d.z, id) - d.L) : __builtin_nanf("");
+      }
+    }
+    __syncthreads();  // (the masses are used until here)
+  }
+}
+
+template <class TI, bool TABLE>
 hipError_t launch_verify_t(const VerifyArgs& a, hipStream_t stream) {
-  const int64_t rows = a.B * (a.D + 1) + (a.draft ? a.B * (a.D + 1) : 0);
-  if (a.nvec * (int64_t)sizeof(typename TI::Vec) < (int64_t)1 << 31)
-    hipLaunchKernelGGL((k_verify_rows<TI, false>), dim3((unsigned)rows), dim3(kVerThreads), 0,
-                       stream, a, 0, a.D + 1);
-  else
-    hipLaunchKernelGGL((k_verify_rows<TI, true>), dim3((unsigned)rows), dim3(kVerThreads), 0,
-                       stream, a, 0, a.D + 1);
+  const int64_t words = a.B * (2 * (a.D + 1) + 2);
+  const int64_t R = a.B * (2 * a.D + 1);
+  uint32_t* first = (uint32_t*)((char*)a.ws + R * sizeof(VerRow) +
+                                R * a.parts * sizeof(VerRec) +
+                                (a.draw_parts > 1 ? a.B * (int64_t)a.nchunk * sizeof(double) : 0));
+  hipLaunchKernelGGL(k_verify_clear, dim3((unsigned)min((words + 255) / 256, (int64_t)64)), dim3(256),
+                     0, stream, first, words);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_verify_draw<TI>), dim3((unsigned)a.B), dim3(kVerThreads), 0, stream, a);
+  for (int pos = 0, many = a.round; pos <= a.D; pos += many, many *= 2) {
+    if (many > a.D + 1 - pos) many = a.D + 1 - pos;
+    const int64_t items = a.B * a.parts * many * (a.draft ? 2 : 1);  // at most
+    hipLaunchKernelGGL((k_verify_rows<TI, TABLE>),
+                       dim3((unsigned)min((items + kVerWaves - 1) / kVerWaves, (int64_t)kVerGroups)),
+                       dim3(kVerThreads), 0, stream, a, pos, pos + many);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_verify_draw<TI, TABLE>),
+                     dim3((unsigned)min(a.B * a.draw_parts, (int64_t)kVerGroups)),
+                     dim3(kVerThreads), 0, stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_verify(const VerifyArgs& a, int in_dt, hipStream_t stream) {
-  return in_dt == BF16 ? launch_verify_t<InBf16>(a, stream) : launch_verify_t<InF32>(a, stream);
+  if (in_dt == F32) return launch_verify_t<InF32, false>(a, stream);
+  // The table is set up by each workgroup (a few us); few rows are summed without it.
+  return a.table ? launch_verify_t<InBf16, true>(a, stream)
+                 : launch_verify_t<InBf16, false>(a, stream);
 }
 
 }  // namespace opd
