@@ -378,8 +378,8 @@ int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, i
  *   x, w and logits are 16-byte aligned; ldx, ldw and ld * element_size are
  *   multiples of 16.  Bytes [H, ldx) and [H, ldw) of the rows are not read.
  *
- * Errors: OPD_ERR_DTYPE (dtype or scale_type), OPD_ERR_SHAPE (N < 0, N or V >=
- * 2^31, H outside [1, 2^24], V < 2, a row stride below its row's length),
+ * Errors: OPD_ERR_DTYPE (dtype or scale_type), OPD_ERR_SHAPE (N < 0, N >=
+ * 2^31, V outside [2, 2^30], H outside [1, 2^24], a row stride below its row's length),
  * OPD_ERR_PARAM (block_rows not 1 or 128), OPD_ERR_ALIGN, OPD_ERR_NULL,
  * OPD_ERR_HIP.  N == 0 is a no-op returning OPD_OK.
  */

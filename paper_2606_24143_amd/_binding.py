@@ -8,7 +8,6 @@ calls fail loudly.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -446,18 +445,36 @@ def score_actions(logits: torch.Tensor, ids: torch.Tensor, *, mask=None, want_ls
 
 # ---------------------------------------------------------------- rows of logits
 
-@contextlib.contextmanager
-def _on(dev: torch.device, stream):
+class _On:
     """Launches and allocations on the tensors' device and the given stream (or
-    that device's current one): what is allocated inside belongs to that stream."""
-    if stream is not None and stream.device != dev:
-        raise ValueError("stream is on %s, the tensors on %s" % (stream.device, dev))
-    with torch.cuda.device(dev):
-        if stream is None:
-            yield ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-        else:
-            with torch.cuda.stream(stream):
-                yield ctypes.c_void_p(stream.cuda_stream)
+    that device's current one): what is allocated inside belongs to that stream.
+    Entering gives the stream's handle."""
+    __slots__ = ("_dev", "_stream", "_held")
+
+    def __init__(self, dev: torch.device, stream):
+        if stream is not None and stream.device != dev:
+            raise ValueError("stream is on %s, the tensors on %s" % (stream.device, dev))
+        self._dev, self._stream, self._held = dev, stream, None
+
+    def __enter__(self) -> int:
+        if self._stream is None:
+            index = self._dev.index
+            if index != torch.cuda.current_device():
+                self._held = torch.cuda.device(self._dev)
+                self._held.__enter__()
+            # (torch.cuda.current_stream() makes an object for the handle: 4 of a call's 14 us)
+            return torch._C._cuda_getCurrentRawStream(index)
+        self._held = torch.cuda.stream(self._stream)  # (and its device)
+        self._held.__enter__()
+        return self._stream.cuda_stream
+
+    def __exit__(self, *exc):
+        if self._held is not None:
+            self._held.__exit__(*exc)
+
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 BLOCK = 128  # columns of a block of 8-bit values (opd_quantize_blocks)
@@ -502,12 +519,12 @@ def quantize_blocks(x: torch.Tensor, *, block_rows: int = 1, scale_dtype=torch.f
     ldx = _need_stride(x, "x")
     _need_gpu(x, "x")
     ldq = _blocks(H, 16) * 16
-    with _on(x.device, stream) as s:
+    with _On(x.device, stream) as s:
         q = torch.empty((N, ldq), dtype=torch.float8_e4m3fn, device=x.device)
         scales = torch.empty((_blocks(N, block_rows), _blocks(H, BLOCK)), dtype=scale_dtype,
                              device=x.device)
-        rc = lib().opd_quantize_blocks(_ptr(x), _dt(x), N, H, ldx, block_rows,
-                                       _SCALES[scale_dtype], _ptr(q), ldq, _ptr(scales), s)
+        rc = lib().opd_quantize_blocks(_at(x), _dt(x), N, H, ldx, block_rows,
+                                       _SCALES[scale_dtype], _at(q), ldq, _at(scales), s)
     if rc != 0:
         raise OpdError(rc, "opd_quantize_blocks")
     return {"q": q[:, :H], "scales": scales}
@@ -544,13 +561,13 @@ def head_logits(hidden: torch.Tensor, hidden_scales: torch.Tensor, weight: torch
             _blocks(V, 8) * 8
         _need_rows(out, "out", dtype, N, V, ld, dev)
     _need_gpu(hidden, "hidden")
-    with _on(dev, stream) as s:
+    with _On(dev, stream) as s:
         if out is None:
             ld = _blocks(V, 8) * 8
             out = torch.empty((N, ld), dtype=dtype, device=dev)
-        rc = lib().opd_head_logits(_ptr(hidden), ldx, _ptr(hidden_scales), _ptr(weight), ldw,
-                                   _ptr(weight_scales), _SCALES[hidden_scales.dtype], N, V, H,
-                                   F32 if dtype == torch.float32 else BF16, _ptr(out), ld, s)
+        rc = lib().opd_head_logits(_at(hidden), ldx, _at(hidden_scales), _at(weight), ldw,
+                                   _at(weight_scales), _SCALES[hidden_scales.dtype], N, V, H,
+                                   F32 if dtype == torch.float32 else BF16, _at(out), ld, s)
     if rc != 0:
         raise OpdError(rc, "opd_head_logits")
     return {"logits": out[:, :V]}
@@ -594,17 +611,17 @@ def verify_drafts(target_logits: torch.Tensor, draft_ids: torch.Tensor, uniforms
     if workspace is not None:
         _need(workspace, "workspace", (torch.uint8,), (workspace.numel(),), dev)
     _need_gpu(target_logits, "target_logits")
-    with _on(dev, stream) as s:
+    with _On(dev, stream) as s:
         if workspace is None:
             nbytes = int(lib().opd_verify_workspace_bytes(B, D, V, dt))
             workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
         accepted = torch.empty(B, dtype=torch.int32, device=dev)
         ids = torch.empty((B, D + 1), dtype=torch.int32, device=dev)
         logp = torch.empty((B, D + 1), dtype=torch.float32, device=dev) if want_logp else None
-        rc = lib().opd_verify_drafts(_ptr(target_logits), _ptr(draft_logits), dt, B, D, V, ld,
-                                     ldd, _ptr(draft_ids), _ptr(draft_lens), _ptr(uniforms),
-                                     _ptr(mask), _ptr(accepted), _ptr(ids), _ptr(logp),
-                                     _ptr(workspace), workspace.numel(), s)
+        rc = lib().opd_verify_drafts(_at(target_logits), _at(draft_logits), dt, B, D, V, ld,
+                                     ldd, _at(draft_ids), _at(draft_lens), _at(uniforms),
+                                     _at(mask), _at(accepted), _at(ids), _at(logp),
+                                     _at(workspace), workspace.numel(), s)
     if rc != 0:
         raise OpdError(rc, "opd_verify_drafts")
     out = {"accepted": accepted, "ids": ids}

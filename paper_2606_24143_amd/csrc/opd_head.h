@@ -25,68 +25,103 @@ constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
 
 // ---------------------------------------------------------------- quantisation
 
-// Eight consecutive elements of a row from column h on (columns past H read as 0).
+// Eight consecutive elements of a row from column h on, as they are stored
+// (columns past H read as 0).
 template <class TI>
-__device__ __forceinline__ void load8(const void* row, int64_t h, int64_t H, float (&f)[8]) {
+struct Eight {
+  u32x4 v[TI::BYTES / 2];
+};
+template <class TI>
+__device__ __forceinline__ Eight<TI> load8(const char* row, int64_t h, int64_t H) {
+  Eight<TI> r;
+  const u32x4* p = (const u32x4*)(row + h * TI::BYTES);
   if (h + 8 <= H) {
-    if constexpr (TI::BYTES == 2) {
-      const u32x4 x = *(const u32x4*)((const uint16_t*)row + h);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        f[2 * d] = __uint_as_float(x[d] << 16);
-        f[2 * d + 1] = __uint_as_float(x[d] & 0xFFFF0000u);
-      }
-    } else {
-      const f32x4 x0 = *(const f32x4*)((const float*)row + h);
-      const f32x4 x1 = *(const f32x4*)((const float*)row + h + 4);
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        f[d] = x0[d];
-        f[4 + d] = x1[d];
-      }
-    }
+    for (int d = 0; d < TI::BYTES / 2; ++d) r.v[d] = __builtin_nontemporal_load(p + d);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = h + e < H ? load_elem<TI>(row, h + e) : 0.f;
+    for (int d = 0; d < TI::BYTES / 2; ++d) r.v[d] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (h + e >= H) continue;
+      if constexpr (TI::BYTES == 2)
+        r.v[0][e / 2] |= (uint32_t)((const uint16_t*)row)[h + e] << (16 * (e & 1));
+      else
+        r.v[e / 4][e & 3] = ((const uint32_t*)row)[h + e];
+    }
   }
+  return r;
 }
-
+template <class TI>
+__device__ __forceinline__ float elem8(const Eight<TI>& x, int e) {
+  if constexpr (TI::BYTES == 2)
+    return __uint_as_float(e & 1 ? x.v[0][e / 2] & 0xFFFF0000u : x.v[0][e / 2] << 16);
+  else
+    return __uint_as_float(x.v[e / 4][e & 3]);
+}
 // The largest magnitude as bits: an integer maximum, in which a NaN is above an
 // infinity and both above every number, so neither is lost.
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+template <class TI>
+__device__ __forceinline__ uint32_t top8(const Eight<TI>& x, uint32_t top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(elem8<TI>(x, e)) & 0x7FFFFFFFu);
+  return top;
+}
 
 struct Scale {
-  float s;         // what values are divided by (NaN: the block holds a NaN or an infinity)
-  float stored;    // fp32 scale, or its power of two
-  uint32_t e8m0;   // its biased exponent (255: NaN)
+  float s;        // what values are divided by (NaN: the block holds a NaN or an infinity)
+  float inv;      // 1 / s (e8m0: exact)
+  uint32_t e8m0;  // its biased exponent (255: NaN)
 };
 
 template <bool E8>
 __device__ __forceinline__ Scale block_scale(uint32_t top) {
   Scale r;
   const bool bad = top >= 0x7F800000u;
+  r.e8m0 = 255u;
   if constexpr (E8) {
     // 448 = 1.75 * 2^8: a = m 2^e needs 2^(e - 8), or 2^(e - 7) for m > 1.75.
     // (a below 2^-126 has e = -127 in its bits and gets the least power.)
     int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     e = e < -127 ? -127 : e;
-    r.e8m0 = bad ? 255u : (uint32_t)(e + 127);
+    if (!bad) r.e8m0 = (uint32_t)(e + 127);
     r.s = bad ? __builtin_nanf("") : ldexpf(1.0f, e);
+    r.inv = ldexpf(1.0f, -e);
   } else {
     r.s = bad ? __builtin_nanf("") : fmaxf(__uint_as_float(top) / kTop, kMinScale);
-    r.e8m0 = 0;
+    r.inv = 1.0f / r.s;
   }
-  r.stored = r.s;
   return r;
 }
 
-// The nearest e4m3 values of f / s, eight to a lane, packed; the quotient is the
-// correctly rounded fp32 one (its last bit decides the ties).
+// f / s, correctly rounded (its last bit decides the ties of the 8-bit rounding).
+// A power of two's inverse is exact.  Else two corrections of f times the rounded
+// inverse, by their exact remainders: the first leaves less than a step, from which
+// the second gives the rounded quotient (Markstein, IBM J. Res. Dev. 34(1), 1990).
+// Five instructions for a division's eleven; where the remainders of such values
+// could underflow (s below 2^-60) it divides.
+constexpr float kSmallScale = 8.6736174e-19f;  // 2^-60
 template <bool E8>
-__device__ __forceinline__ u32x2 quant8(const float (&f)[8], const Scale& sc) {
+__device__ __forceinline__ float quotient(float f, const Scale& sc, bool small) {
+  if constexpr (E8) return f * sc.inv;
+  if (small) return f / sc.s;
+  float q = f * sc.inv;
+  q = fmaf(fmaf(-q, sc.s, f), sc.inv, q);
+  return fmaf(fmaf(-q, sc.s, f), sc.inv, q);
+}
+
+// The nearest e4m3 values of f / s, eight to a lane, packed.
+template <class TI, bool E8>
+__device__ __forceinline__ u32x2 quant8(const Eight<TI>& x, const Scale& sc) {
+  const bool small = !E8 && __ballot(!(sc.s >= kSmallScale)) != 0;
   float v[8];
+  if (small) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = f[e] / sc.s;
+    for (int e = 0; e < 8; ++e) v[e] = quotient<E8>(elem8<TI>(x, e), sc, true);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = quotient<E8>(elem8<TI>(x, e), sc, false);
+  }
   u32x2 r;
 #pragma unroll
   for (int d = 0; d < 2; ++d) {
@@ -100,7 +135,7 @@ __device__ __forceinline__ u32x2 quant8(const float (&f)[8], const Scale& sc) {
 
 __device__ __forceinline__ void store8(uint8_t* qrow, int64_t h, int64_t H, u32x2 q) {
   if (h + 8 <= H) {
-    *(u32x2*)(qrow + h) = q;
+    __builtin_nontemporal_store(q, (u32x2*)(qrow + h));
   } else {
     for (int e = 0; h + e < H; ++e) qrow[h + e] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
   }
@@ -111,47 +146,60 @@ __device__ __forceinline__ void store_scale(void* scales, int64_t at, const Scal
   if constexpr (E8)
     ((uint8_t*)scales)[at] = (uint8_t)s.e8m0;
   else
-    ((float*)scales)[at] = s.stored;
+    ((float*)scales)[at] = s.s;
 }
 
-// A block of one row: 16 lanes, eight elements each.
+// Blocks of one row: 16 lanes, eight elements each, to a block; the 16 lanes take
+// QB consecutive blocks (of the rows one after the other).
 constexpr int kQuantThreads = 256;
-template <class TI, bool E8>
-__global__ void __launch_bounds__(kQuantThreads) k_quantize_rows(QuantArgs a) {
-  const int64_t g = (int64_t)blockIdx.x * (kQuantThreads / 16) + (threadIdx.x >> 4);
-  if (g >= a.N * a.nb) return;
-  const int64_t row = g / a.nb, b = g - row * a.nb;
-  const int64_t h = b * kBlk + 8 * (threadIdx.x & 15);
-  float f[8];
-  load8<TI>((const char*)a.x + row * a.ldx * TI::BYTES, h, a.H, f);
-  uint32_t top = 0;
+template <class TI, bool E8, int QB>
+__global__ void __launch_bounds__(kQuantThreads) k_quantize_rows(QuantArgs a, int64_t first) {
+  const int64_t blocks = a.N * a.nb;
+  const int64_t g0 = first + ((int64_t)blockIdx.x * (kQuantThreads / 16) + (threadIdx.x >> 4)) * QB;
+  if (g0 >= blocks) return;
+  int64_t row = g0 / a.nb, b = g0 - row * a.nb;
+  Eight<TI> x[QB];
+  int64_t rows[QB], h[QB];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+  for (int k = 0; k < QB; ++k) {
+    rows[k] = row;
+    h[k] = b * kBlk + 8 * (threadIdx.x & 15);
+    if (g0 + k < blocks)
+      x[k] = load8<TI>((const char*)a.x + row * a.ldx * TI::BYTES, h[k], a.H);
+    if (++b == a.nb) {
+      b = 0;
+      ++row;
+    }
+  }
 #pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  const Scale s = block_scale<E8>(top);
-  store8(a.q + row * a.ldq, h, a.H, quant8<E8>(f, s));
-  if ((threadIdx.x & 15) == 0) store_scale<E8>(a.scales, g, s);
+  for (int k = 0; k < QB; ++k) {
+    if (g0 + k >= blocks) break;
+    uint32_t top = top8<TI>(x[k], 0u);
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    const Scale s = block_scale<E8>(top);
+    store8(a.q + rows[k] * a.ldq, h[k], a.H, quant8<TI, E8>(x[k], s));
+    if ((threadIdx.x & 15) == 0) store_scale<E8>(a.scales, g0 + k, s);
+  }
 }
 
 // A block of 128 rows: a workgroup, eight passes of 16 rows held in registers.
 template <class TI, bool E8>
-__global__ void __launch_bounds__(kQuantThreads) k_quantize_tiles(QuantArgs a) {
+__global__ void __launch_bounds__(kQuantThreads) k_quantize_tiles(QuantArgs a, int64_t first) {
   __shared__ uint32_t red[kQuantThreads / 64];
-  const int64_t br = blockIdx.x / a.nb, b = blockIdx.x - br * a.nb;
+  const int64_t at = first + blockIdx.x;
+  const int64_t br = at / a.nb, b = at - br * a.nb;
   const int64_t h = b * kBlk + 8 * (threadIdx.x & 15);
   const int64_t r0 = br * kBlk + (threadIdx.x >> 4);
-  float f[8][8];
+  Eight<TI> x[8];
   uint32_t top = 0;
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
-    const int64_t row = r0 + 16 * p;
-    if (row < a.N) {
-      load8<TI>((const char*)a.x + row * a.ldx * TI::BYTES, h, a.H, f[p]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[p][e]));
-    }
+    const int64_t row = min(r0 + 16 * p, a.N - 1);  // (the last row again: the same maximum)
+    x[p] = load8<TI>((const char*)a.x + row * a.ldx * TI::BYTES, h, a.H);
   }
+#pragma unroll
+  for (int p = 0; p < 8; ++p) top = top8<TI>(x[p], top);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
@@ -162,23 +210,32 @@ __global__ void __launch_bounds__(kQuantThreads) k_quantize_tiles(QuantArgs a) {
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     const int64_t row = r0 + 16 * p;
-    if (row < a.N) store8(a.q + row * a.ldq, h, a.H, quant8<E8>(f[p], s));
+    if (row < a.N) store8(a.q + row * a.ldq, h, a.H, quant8<TI, E8>(x[p], s));
   }
-  if (threadIdx.x == 0) store_scale<E8>(a.scales, blockIdx.x, s);
+  if (threadIdx.x == 0) store_scale<E8>(a.scales, at, s);
 }
+
+// (a launch has fewer than 2^32 work-items: larger calls are several)
+constexpr int64_t kMaxGroups = 0xFFFFFFFFll / kQuantThreads;
 
 template <class TI, bool E8>
 hipError_t launch_quantize_t(const QuantArgs& a, hipStream_t stream) {
-  if (a.block_rows == 1) {
-    const int64_t per = kQuantThreads / 16;
-    hipLaunchKernelGGL((k_quantize_rows<TI, E8>), dim3((unsigned)((a.N * a.nb + per - 1) / per)),
-                       dim3(kQuantThreads), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL((k_quantize_tiles<TI, E8>),
-                       dim3((unsigned)((a.N + kBlk - 1) / kBlk * a.nb)), dim3(kQuantThreads), 0,
-                       stream, a);
+  constexpr int QB = 2;
+  const bool rows = a.block_rows == 1;
+  const int64_t blocks = (rows ? a.N : (a.N + kBlk - 1) / kBlk) * a.nb;
+  const int64_t per = rows ? kQuantThreads / 16 * QB : 1;  // blocks of a workgroup
+  for (int64_t first = 0; first < blocks; first += kMaxGroups * per) {
+    const int64_t groups = min((blocks - first + per - 1) / per, kMaxGroups);
+    if (rows)
+      hipLaunchKernelGGL((k_quantize_rows<TI, E8, QB>), dim3((unsigned)groups), dim3(kQuantThreads),
+                         0, stream, a, first);
+    else
+      hipLaunchKernelGGL((k_quantize_tiles<TI, E8>), dim3((unsigned)groups), dim3(kQuantThreads), 0,
+                         stream, a, first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 // ---------------------------------------------------------------- product
@@ -764,7 +821,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
 }
 
 template <class TO, bool E8>
-hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
+hipError_t launch_head_rows(HeadArgs a, hipStream_t stream) {
   // (a tile's rows have to lie within the 2 GiB that a buffer's offsets take here)
   constexpr int64_t kMaxStride = (int64_t)1 << 22;
   if (a.H % 16 != 0 || a.nb < 2 || a.ldw > kMaxStride || a.ldx > kMaxStride) {
@@ -780,6 +837,23 @@ hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
   hipLaunchKernelGGL((k_head_tile<TO, E8>), dim3((unsigned)min(tiles, (int64_t)kHeadCus)),
                      dim3(kTileThreads), 0, stream, a);
   return hipGetLastError();
+}
+
+// (so many tokens to a launch that its tiles can be counted: all but never less
+// than all)
+template <class TO, bool E8>
+hipError_t launch_head_t(const HeadArgs& a, hipStream_t stream) {
+  const int64_t most = max((int64_t)256, ((int64_t)1 << 38) / a.V / 256 * 256);
+  for (int64_t n = 0; n < a.N; n += most) {
+    HeadArgs b = a;
+    b.N = min(most, a.N - n);
+    b.x = a.x + n * a.ldx;
+    b.sx = (const char*)a.sx + n * a.nb * (E8 ? 1 : 4);
+    b.out = (char*)a.out + n * a.ldo * TO::BYTES;
+    const hipError_t e = launch_head_rows<TO, E8>(b, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
