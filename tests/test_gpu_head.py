@@ -100,7 +100,8 @@ def head_tolerance(mags, z, H, out, x, sx, w, sw):
     (1, 2, 1), (1, 130, 128), (2, 257, 129), (5, 1000, 640), (15, 333, 1000), (16, 2048, 256),
     (17, 129, 384), (33, 515, 2000), (63, 700, 384), (64, 1030, 512), (65, 256, 257),
     (100, 1537, 768), (128, 384, 128), (129, 260, 1024), (200, 3001, 896), (256, 512, 2048),
-    (257, 1025, 272), (300, 2050, 1152), (520, 777, 640)])
+    (257, 1025, 272), (300, 2050, 1152), (520, 777, 640),
+    (600, 30011, 272), (16, 13001, 384), (40, 25003, 256), (90, 30000, 640)])
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_head_logits(N, V, H, scale, out):
