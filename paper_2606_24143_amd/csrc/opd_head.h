@@ -311,17 +311,32 @@ __device__ __forceinline__ f32x16 mma64(i32x8 w, i32x8 x, f32x16 c) {
   }
 }
 
-// The product of 16 rows of each over 128 columns, of which a lane holds 32.
+// The product of 16 rows of each over 128 columns, of which a lane holds 32: as the
+// matrix instructions of TO take them.
 template <class TO>
-__device__ __forceinline__ f32x4 mma128(i32x8 w, i32x8 x) {
+struct Frag {
+  i32x8 v;
+  __device__ __forceinline__ explicit Frag(i32x8 x) : v(x) {}
+  Frag() = default;
+};
+template <>
+struct Frag<OutF32> {
+  bf16x8 v[4];
+  __device__ __forceinline__ explicit Frag(i32x8 x) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = widen8(x[2 * k], x[2 * k + 1]);
+  }
+  Frag() = default;
+};
+template <class TO>
+__device__ __forceinline__ f32x4 mma128(const Frag<TO>& w, const Frag<TO>& x) {
   f32x4 c = {0.f, 0.f, 0.f, 0.f};
   if constexpr (TO::BYTES == 2) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, c, 0, 0, 0, 0, 0, 0);
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * k], w[2 * k + 1]),
-                                                  widen8(x[2 * k], x[2 * k + 1]), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[k], x.v[k], c, 0, 0, 0);
     return c;
   }
 }
@@ -506,6 +521,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint32_t fx0 = lr * 128 + ((lk ^ key_x(lr)) << 4);
   auto multiply = [&](int d, int buf) {
+    const Frag<TO> head(bw[d]);
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const uint8_t* p = lx[buf][d] + t * 2048;
@@ -518,7 +534,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
       } else {
         const float s = E8 ? e8m0_value(ts) * e8m0_value(hs[d])
                            : __uint_as_float(ts) * __uint_as_float(hs[d]);
-        const f32x4 q = mma128<TO>(bw[d], x);
+        const f32x4 q = mma128<TO>(head, Frag<TO>(x));
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(q[e], s, acc[t][e]);
         // (added here, not kept for later: the products would fill the registers)
@@ -652,7 +668,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
   constexpr bool WIDE = TO::BYTES == 4;  // 16-bit instructions (mma128)
   constexpr bool HW = E8 && !WIDE;       // the instructions apply the scales
   constexpr int JH = HW ? 4 : 2;         // groups of 16 tokens at a time
-  constexpr int PF = HW || WIDE ? 2 : 3;  // fragments of the head on the way
+  constexpr int PF = 2;                  // fragments of the head on the way
   constexpr int SLICES = 32 / JH, FIRST = HW ? 0 : 1;
   __shared__ __align__(16) uint8_t lds[2][2][256 * 128];  // [stage][head, tokens]
   __shared__ uint32_t lsc[2][kTileN + 2];                 // tokens' scales, then the head's
@@ -756,13 +772,14 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
       const uint32_t hs = lsc[buf][kTileN + (w & 1)];
 #pragma unroll
       for (int h = 0; h < 4; h += JH) {
-        i32x8 bx[JH], aw[PF];
+        Frag<TO> bx[JH];
+        i32x8 aw[PF];
         uint32_t ts[JH];
         float s[JH];
         f32x4 p[2][JH];
 #pragma unroll
         for (int j = 0; j < JH; ++j) {
-          bx[j] = frag_x(fx, h + j);
+          bx[j] = Frag<TO>(frag_x(fx, h + j));
           ts[j] = lsc[buf][wn + 16 * (h + j) + lr];
         }
 #pragma unroll
@@ -784,11 +801,25 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
 #pragma unroll
             for (int j = 0; j < JH; ++j)
               acc[i & 7][h + j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                  aw[i % PF], bx[j], acc[i & 7][h + j], 0, 0, 0, (int)hs, 0, (int)ts[j]);
+                  aw[i % PF], bx[j].v, acc[i & 7][h + j], 0, 0, 0, (int)hs, 0, (int)ts[j]);
+          } else if constexpr (WIDE) {
+            // (the registers hold one set of products)
+            if (i < 8) {
+              const Frag<TO> head(aw[i % PF]);
+#pragma unroll
+              for (int j = 0; j < JH; ++j) p[0][j] = mma128<TO>(head, bx[j]);
+#pragma unroll
+              for (int j = 0; j < JH; ++j) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  acc[i & 7][h + j][e] = fmaf(p[0][j][e], s[j], acc[i & 7][h + j][e]);
+                asm volatile("" : "+v"(acc[i & 7][h + j]));
+              }
+            }
           } else {
             if (i < 8) {
 #pragma unroll
-              for (int j = 0; j < JH; ++j) p[i & 1][j] = mma128<TO>(aw[i % PF], bx[j]);
+              for (int j = 0; j < JH; ++j) p[i & 1][j] = mma128<TO>(Frag<TO>(aw[i % PF]), bx[j]);
             }
             __builtin_amdgcn_sched_barrier(0);
             if (i > 0) {  // the products before are added meanwhile
