@@ -256,7 +256,10 @@ bool row_fits(int64_t nvec, int32_t dtype) {
 }
 
 // Arguments shared by the blockwise calls.
-constexpr int64_t kMaxHidden = (int64_t)1 << 24, kMaxHeadRows = (int64_t)1 << 30;
+// (the head's kernels address the rows of a tile within 2 GiB and count tiles of 2^16
+// logits in 32 bits)
+constexpr int64_t kMaxHidden = (int64_t)1 << 22, kMaxHeadRows = (int64_t)1 << 30;
+constexpr int64_t kMaxLogits = (int64_t)1 << 46;
 int check_blocks(int64_t N, int64_t H, int32_t scale_type) {
   if (scale_type != OPD_SCALE_F32 && scale_type != OPD_SCALE_E8M0) return OPD_ERR_DTYPE;
   if (N < 0 || N > INT32_MAX || H < 1 || H > kMaxHidden) return OPD_ERR_SHAPE;
@@ -617,7 +620,9 @@ int opd_head_logits(const void* x, int64_t ldx, const void* x_scales, const void
   if (logits_dtype != OPD_F32 && logits_dtype != OPD_BF16) return OPD_ERR_DTYPE;
   if (int rc = check_blocks(N, H, scale_type)) return rc;
   if (int rc = check_shape(N, V, ld)) return rc;
-  if (V > kMaxHeadRows || ldx < H || ldw < H) return OPD_ERR_SHAPE;
+  if (V > kMaxHeadRows || ldx < H || ldw < H || ldx > kMaxHidden || ldw > kMaxHidden)
+    return OPD_ERR_SHAPE;
+  if (N * V > kMaxLogits) return OPD_ERR_SHAPE;
   if (N == 0) return OPD_OK;
   if (!x || !x_scales || !w || !w_scales || !logits) return OPD_ERR_NULL;
   if (!aligned16(x) || !aligned16(w) || !aligned16(logits)) return OPD_ERR_ALIGN;

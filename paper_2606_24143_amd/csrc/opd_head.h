@@ -17,7 +17,7 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlk = 128;          // columns of a block
 constexpr float kTop = 448.0f;     // the largest e4m3 value
@@ -240,29 +240,10 @@ hipError_t launch_quantize_t(const QuantArgs& a, hipStream_t stream) {
 
 // ---------------------------------------------------------------- product
 
-// 16 bytes of a row from byte h on; bytes at or past H read as 0.  (Only bytes
-// of [0, H) are touched.)
-__device__ __forceinline__ i32x4 load16(const uint8_t* row, int h, int H) {
-  if (h + 16 <= H) return *(const i32x4*)(row + h);
-  i32x4 r = {0, 0, 0, 0};
-#pragma unroll
-  for (int e = 0; e < 16; ++e)
-    if (h + e < H) r[e >> 2] |= (int)((uint32_t)row[h + e] << (8 * (e & 3)));
-  return r;
-}
-
 // 2^(e - 127) (2^-127 is not a normal number; 255 is NaN)
 __device__ __forceinline__ float e8m0_value(uint32_t e) {
   return e == 255u ? __builtin_nanf("") : __uint_as_float(e ? e << 23 : 0x400000u);
 }
-template <bool E8>
-__device__ __forceinline__ float load_scale(const void* s, int64_t at) {
-  if constexpr (E8)
-    return e8m0_value(((const uint8_t*)s)[at]);
-  else
-    return ((const float*)s)[at];
-}
-
 // Four logits of consecutive vocabulary entries v .. v + 3 of one token.
 template <class TO>
 __device__ __forceinline__ void store_logits(void* row, int64_t v, int64_t V, f32x4 z) {
@@ -292,27 +273,13 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// c += w x^T over 64 columns, of which a lane holds 32 of its row of each.
-// The 8-bit instruction cuts each product at 2^-13 of the largest of the 16 it
-// sums at once before they reach the fp32 accumulator (measured: 1.5e-5 of a
-// result of 64 normal products; the 16-bit instructions: 5e-9), far below
-// the rounding of bf16 logits (2^-8) but not that of fp32 ones, so these are
-// made by 16-bit instructions of exactly widened values, at half the rate.
-template <class TO>
-__device__ __forceinline__ f32x16 mma64(i32x8 w, i32x8 x, f32x16 c) {
-  if constexpr (TO::BYTES == 2) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(w[2 * k], w[2 * k + 1]),
-                                                  widen8(x[2 * k], x[2 * k + 1]), c, 0, 0, 0);
-    return c;
-  }
-}
-
-// The product of 16 rows of each over 128 columns, of which a lane holds 32: as the
-// matrix instructions of TO take them.
+// The 8-bit instruction cuts each product at 2^-13 of the largest of the 16 it sums
+// at once before they reach the fp32 accumulator (measured: 1.5e-5 of a result
+// of 64 normal products; the 16-bit instructions: 5e-9), far below the rounding of
+// bf16 logits (2^-8) but not that of fp32 ones, so these are made by 16-bit
+// instructions of exactly widened values, at half the rate.
+// 16 rows over 128 columns, of which a lane holds 32: as the instructions for TO take
+// them; and the product of two.
 template <class TO>
 struct Frag {
   i32x8 v;
@@ -355,74 +322,14 @@ __device__ __forceinline__ void store8_logits(char* row, int64_t v, int64_t V, f
   store_logits<TO>(row, v + 4, V, b);
 }
 
-// Any width: a tile of 128 vocabulary entries by 128 tokens, four waves of 64 by
-// 64, blocks staged one at a time with their ends masked.  For widths the
-// kernels below do not take (no multiple of 16, or one block).
-constexpr int kHeadThreads = 256;
-template <class TO, bool E8>
-__global__ void __launch_bounds__(kHeadThreads) k_head_any(HeadArgs a) {
-  __shared__ __align__(16) uint8_t lds[2][128 * 128];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int64_t vt = blockIdx.x / a.ntiles, nt = blockIdx.x - vt * a.ntiles;
-  const int64_t v0 = vt * 128, n0 = nt * 128;
-  const int wv = (w & 1) * 64, wn = (w >> 1) * 64;
-  f32x16 acc[2][2];
+// What is kept of 16 bytes of a row from byte h on: those before H.
+__device__ __forceinline__ u32x4 keep16(u32x4 x, int h, int H) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  for (int b = 0; b < a.nb; ++b) {
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int r = p * 32 + (tid >> 3), c = tid & 7;
-      const int64_t rv = min(v0 + r, a.V - 1), rn = min(n0 + r, a.N - 1);
-      const int at = r * 128 + ((c ^ (r & 7)) << 4);
-      *(i32x4*)(lds[0] + at) = load16(a.w + rv * a.ldw, b * 128 + c * 16, (int)a.H);
-      *(i32x4*)(lds[1] + at) = load16(a.x + rn * a.ldx, b * 128 + c * 16, (int)a.H);
-    }
-    __syncthreads();
-    auto frag = [&](int m, int row, int t) {
-      const int c = 4 * t + 2 * (lane >> 5);
-      const uint8_t* p = lds[m] + row * 128;
-      const i32x4 lo = *(const i32x4*)(p + ((c ^ (row & 7)) << 4));
-      const i32x4 hi = *(const i32x4*)(p + (((c + 1) ^ (row & 7)) << 4));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    const float sw = load_scale<E8>(a.sw, vt * a.nb + b);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int rn = wn + 32 * j + (lane & 31);
-      const float s = load_scale<E8>(a.sx, min(n0 + rn, a.N - 1) * a.nb + b) * sw;
-      const i32x8 x0 = frag(1, rn, 0), x1 = frag(1, rn, 1);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int rv = wv + 32 * i + (lane & 31);
-        f32x16 p;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = 0.f;
-        p = mma64<TO>(frag(0, rv, 0), x0, p);
-        p = mma64<TO>(frag(0, rv, 1), x1, p);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = fmaf(p[e], s, acc[i][j][e]);
-      }
-    }
-    __syncthreads();
+  for (int d = 0; d < 4; ++d) {
+    const int n = H - h - 4 * d;  // valid bytes from this dword on
+    x[d] = n >= 4 ? x[d] : n > 0 ? x[d] & ((1u << (8 * n)) - 1u) : 0u;
   }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int64_t n = n0 + wn + 32 * j + (lane & 31);
-    if (n >= a.N) continue;
-    void* row = (char*)a.out + n * a.ldo * TO::BYTES;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        store_logits<TO>(row, v0 + wv + 32 * i + 8 * g + 4 * (lane >> 5), a.V,
-                         f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                               acc[i][j][4 * g + 3]});
-  }
+  return x;
 }
 
 __device__ __forceinline__ uint32_t key_x(uint32_t row) { return (row >> 1) & 7u; }
@@ -444,7 +351,7 @@ __device__ __forceinline__ Rsrc rows_rsrc(const void* p, int64_t bytes) {
 // (T > 1): rows are often a multiple of 4 KiB apart, and all reads at one place of
 // them wait for the same part of the memory (127 against 137 us at 32 tokens,
 // V = 151,936, H = 4,096).
-template <class TO, bool E8, int T, int SB, int W>
+template <class TO, bool E8, bool ODD, int T, int SB, int W>
 __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   constexpr bool HW = E8 && TO::BYTES == 2;
   constexpr int SZ = E8 ? 1 : 4, THREADS = 64 * W;
@@ -489,10 +396,11 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
         ps[k] = __builtin_amdgcn_raw_buffer_load_b32(qs, o, 0, 0);
     }
   };
-  auto put_x = [&](int buf) {
+  auto put_x = [&](int buf, int b0) {
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const uint32_t i = (uint32_t)tid + k * THREADS, at = i & (SB * 8 - 1), row = i / (SB * 8);
+      if (ODD) px[k] = keep16(px[k], b0 * kBlk + (int)at * 16, (int)a.H);
       if (PIECES % THREADS == 0 || i < PIECES)
         *(u32x4*)(lx[buf][at >> 3] + row * 128 + (((at & 7u) ^ key_x(row)) << 4)) = px[k];
     }
@@ -520,7 +428,17 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
 #pragma unroll
   for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint32_t fx0 = lr * 128 + ((lk ^ key_x(lr)) << 4);
-  auto multiply = [&](int d, int buf) {
+  auto multiply = [&](int d, int buf, int b) {
+    if (ODD) {
+      const int h = b * kBlk + (int)lk * 16;
+      const u32x4 lo = keep16(__builtin_shufflevector(__builtin_bit_cast(u32x8, bw[d]),
+                                                      __builtin_bit_cast(u32x8, bw[d]), 0, 1, 2, 3),
+                              h, (int)a.H);
+      const u32x4 hi = keep16(__builtin_shufflevector(__builtin_bit_cast(u32x8, bw[d]),
+                                                      __builtin_bit_cast(u32x8, bw[d]), 4, 5, 6, 7),
+                              h + 64, (int)a.H);
+      bw[d] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
     const Frag<TO> head(bw[d]);
 #pragma unroll
     for (int t = 0; t < T; ++t) {
@@ -545,32 +463,29 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   };
   // stages in a cycle that starts elsewhere for each workgroup
   const int stages = (a.nb + SB - 1) / SB;
-  int at_x = T > 1 ? (int)(blockIdx.x % (uint32_t)stages) : 0, at_w = at_x;
-  auto step = [&](int& at) { at = at + 1 == stages ? 0 : at + 1; };
-  ask_x(at_x * SB);
-  step(at_x);
+  int now = T > 1 ? (int)(blockIdx.x % (uint32_t)stages) : 0;  // the stage that is multiplied
+  auto after = [&](int at) { return at + 1 == stages ? 0 : at + 1; };
+  ask_x(now * SB);
 #pragma unroll
-  for (int d = 0; d < SB; ++d) ask_w(d, at_w * SB + d);
-  step(at_w);
-  put_x(0);
-  ask_x(at_x * SB);
-  step(at_x);
+  for (int d = 0; d < SB; ++d) ask_w(d, now * SB + d);
+  put_x(0, now * SB);
+  ask_x(after(now) * SB);
   int buf = 0;
   for (int i = 0; i < stages; ++i, buf ^= 1) {
     __syncthreads();
+    const int next = after(now);
 #pragma unroll
     for (int d = 0; d < SB; ++d) {
-      multiply(d, buf);
-      ask_w(d, at_w * SB + d);
+      multiply(d, buf, now * SB + d);
+      ask_w(d, next * SB + d);
       __builtin_amdgcn_sched_barrier(0);
       if (d == SB - 1) {
-        put_x(buf ^ 1);
-        ask_x(at_x * SB);
+        put_x(buf ^ 1, next * SB);
+        ask_x(after(next) * SB);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    step(at_x);
-    step(at_w);
+    now = next;
   }
 #pragma unroll
   for (int t = 0; t < T; ++t) {
@@ -582,7 +497,9 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
 
 template <class TO, bool E8, int T, int SB, int W>
 hipError_t launch_stream(const HeadArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((k_head_stream<TO, E8, T, SB, W>),
+  const auto kernel = a.H % 16 != 0 ? k_head_stream<TO, E8, true, T, SB, W>
+                                    : k_head_stream<TO, E8, false, T, SB, W>;
+  hipLaunchKernelGGL(kernel,
                      dim3((unsigned)((a.V + 16 * W - 1) / (16 * W))), dim3(64 * W), 0,
                      stream, a);
   return hipGetLastError();
@@ -663,13 +580,13 @@ struct HeadTile {  // where a tile's operands are (wave-uniform)
   }
 };
 
-template <class TO, bool E8>
+template <class TO, bool E8, bool ODD>
 __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
   constexpr bool WIDE = TO::BYTES == 4;  // 16-bit instructions (mma128)
   constexpr bool HW = E8 && !WIDE;       // the instructions apply the scales
   constexpr int JH = HW ? 4 : 2;         // groups of 16 tokens at a time
   constexpr int PF = 2;                  // fragments of the head on the way
-  constexpr int SLICES = 32 / JH, FIRST = HW ? 0 : 1;
+  constexpr int FIRST = HW ? 0 : 1;      // the first slice that moves a piece
   __shared__ __align__(16) uint8_t lds[2][2][256 * 128];  // [stage][head, tokens]
   __shared__ uint32_t lsc[2][kTileN + 2];                 // tokens' scales, then the head's
   const int tid = threadIdx.x, lane = tid & 63;
@@ -713,9 +630,9 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
     if (k == 0) {
       const Rsrc r = rows_rsrc(h.s + b * HeadTile<E8>::SB, h.sbytes - b * HeadTile<E8>::SB);
       if constexpr (E8)
-        psc = __builtin_amdgcn_raw_buffer_load_b8(r, (int)os, 0, 0);
+        psc = __builtin_amdgcn_raw_buffer_load_b8(r, b < a.nb ? (int)os : INT32_MIN, 0, 0);
       else
-        psc = __builtin_amdgcn_raw_buffer_load_b32(r, (int)os, 0, 0);
+        psc = __builtin_amdgcn_raw_buffer_load_b32(r, b < a.nb ? (int)os : INT32_MIN, 0, 0);
     }
   };
   auto put = [&](int buf, int k) {
@@ -749,6 +666,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
     put(0, k);
     ask(cur, 1, k);
   }
+  const int nb = max(a.nb, 2);  // (a second block of zeros, so that two stages are this tile's)
   int buf = 0;
   for (;;) {
     f32x4 acc[8][4];
@@ -756,10 +674,10 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int b = 0; b < a.nb; ++b, buf ^= 1) {
+    for (int b = 0; b < nb; ++b, buf ^= 1) {
       const uint8_t* fw = lds[buf][0] + wv * 128;
       const uint8_t* fx = lds[buf][1] + wn * 128;
-      const bool over = b + 2 >= a.nb;  // stage g + 2 is the next tile's
+      const bool over = b + 2 >= nb;  // stage g + 2 is the next tile's
       HeadTile<E8> from = cur;
       from.w = over ? next.w : cur.w;
       from.x = over ? next.x : cur.x;
@@ -767,8 +685,17 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
       from.wbytes = over ? next.wbytes : cur.wbytes;
       from.xbytes = over ? next.xbytes : cur.xbytes;
       from.sbytes = over ? next.sbytes : cur.sbytes;
-      const int fb = over ? b + 2 - a.nb : b + 2;
+      const int fb = over ? b + 2 - nb : b + 2;
       __syncthreads();  // stage g is in LDS; the other half is free
+      if (ODD && b == a.nb - 1) {
+        // a thread per row cuts what follows H in the piece that holds the row's end
+        // (as pieces pass through registers, it would cost registers that hold sums)
+        const uint32_t row = (uint32_t)tid & 255u, at = ((uint32_t)a.H >> 4) & 7u;
+        const uint32_t key = tid < 256 ? key_w(row) : key_x(row);
+        u32x4* p = (u32x4*)(lds[buf][tid >> 8] + row * 128 + ((at ^ key) << 4));
+        *p = keep16(*p, 0, (int)a.H & 15);
+        __syncthreads();
+      }
       const uint32_t hs = lsc[buf][kTileN + (w & 1)];
 #pragma unroll
       for (int h = 0; h < 4; h += JH) {
@@ -852,39 +779,14 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
 }
 
 template <class TO, bool E8>
-hipError_t launch_head_rows(HeadArgs a, hipStream_t stream) {
-  // (a tile's rows have to lie within the 2 GiB that a buffer's offsets take here)
-  constexpr int64_t kMaxStride = (int64_t)1 << 22;
-  if (a.H % 16 != 0 || a.nb < 2 || a.ldw > kMaxStride || a.ldx > kMaxStride) {
-    a.ntiles = (a.N + 127) / 128;
-    const int64_t tiles = (a.V + 127) / 128 * a.ntiles;
-    hipLaunchKernelGGL((k_head_any<TO, E8>), dim3((unsigned)tiles), dim3(kHeadThreads), 0, stream,
-                       a);
-    return hipGetLastError();
-  }
+hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
   if (a.N <= 128) return launch_few<TO, E8>(a, stream);
   a.ntiles = (a.N + kTileN - 1) / kTileN;
   const int64_t tiles = (a.V + kTileV - 1) / kTileV * a.ntiles;
-  hipLaunchKernelGGL((k_head_tile<TO, E8>), dim3((unsigned)min(tiles, (int64_t)kHeadCus)),
+  const auto kernel = a.H % 16 != 0 ? k_head_tile<TO, E8, true> : k_head_tile<TO, E8, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)min(tiles, (int64_t)kHeadCus)),
                      dim3(kTileThreads), 0, stream, a);
   return hipGetLastError();
-}
-
-// (so many tokens to a launch that its tiles can be counted: all but never less
-// than all)
-template <class TO, bool E8>
-hipError_t launch_head_t(const HeadArgs& a, hipStream_t stream) {
-  const int64_t most = max((int64_t)256, ((int64_t)1 << 38) / a.V / 256 * 256);
-  for (int64_t n = 0; n < a.N; n += most) {
-    HeadArgs b = a;
-    b.N = min(most, a.N - n);
-    b.x = a.x + n * a.ldx;
-    b.sx = (const char*)a.sx + n * a.nb * (E8 ? 1 : 4);
-    b.out = (char*)a.out + n * a.ldo * TO::BYTES;
-    const hipError_t e = launch_head_rows<TO, E8>(b, stream);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
 }
 
 }  // namespace

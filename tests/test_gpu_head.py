@@ -101,7 +101,8 @@ def head_tolerance(mags, z, H, out, x, sx, w, sw):
     (17, 129, 384), (33, 515, 2000), (63, 700, 384), (64, 1030, 512), (65, 256, 257),
     (100, 1537, 768), (128, 384, 128), (129, 260, 1024), (200, 3001, 896), (256, 512, 2048),
     (257, 1025, 272), (300, 2050, 1152), (520, 777, 640),
-    (600, 30011, 272), (16, 13001, 384), (40, 25003, 256), (90, 30000, 640)])
+    (600, 30011, 272), (300, 515, 7), (260, 300, 135), (150, 777, 1001), (31, 4100, 333),
+    (100, 640, 2047), (16, 13001, 384), (40, 25003, 256), (90, 30000, 640)])
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_head_logits(N, V, H, scale, out):
@@ -128,6 +129,29 @@ def test_head_logits(N, V, H, scale, out):
     assert (err <= tol).all()
     assert torch.equal(got, again)
     assert (buf[:, V:] == 777.0).all(), "columns past V are not written"
+
+
+@pytest.mark.parametrize("N,V,H", [(1, 100, 9), (20, 300, 130), (128, 700, 255), (260, 300, 135),
+                                   (300, 1000, 2047), (130, 515, 15)])
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_what_lies_past_a_row_is_not_used(N, V, H, scale, out):
+    g = np.random.default_rng(6)
+    x, sx, _, _ = quantized(g.normal(0, 1, (N, H)).astype(np.float32), 1, scale)
+    w, sw, _, _ = quantized(g.normal(0, 1, (V, H)).astype(np.float32), 128, scale)
+
+    def padded(q, fill, extra):
+        buf = torch.full((q.shape[0], (H + 15) // 16 * 16 + extra), fill, dtype=torch.uint8,
+                         device=DEV)
+        buf[:, :H] = q.contiguous().view(torch.uint8)
+        return buf.view(torch.float8_e4m3fn)[:, :H]
+
+    z = [opd.head_logits(padded(x, f, e), sx, padded(w, f, e), sw, dtype=DT[out])["logits"]
+         for f, e in ((0, 0), (0x7F, 0), (0xFF, 32), (0x38, 16))]
+    torch.cuda.synchronize()
+    assert torch.isfinite(z[0]).all()
+    for other in z[1:]:
+        assert torch.equal(other, z[0])
 
 
 @pytest.mark.parametrize("N", [1, 40, 300])

@@ -168,6 +168,69 @@ def test_bad_arguments_in_the_data_end_their_sequence():
     assert out["accepted"].cpu().tolist()[:10] == [1, 0, 2, 1, 0, 3, 3, 0, 0, 0]
 
 
+def large(certain=False, near=0.2, seed=0):
+    """So many bf16 logits that their exponentials come from a table."""
+    return make(40, 2, 110000, "bf16", certain, near=near, seed=seed)
+
+
+@pytest.mark.parametrize("value", [0.0, 1e-7, 88.0, 300.0, 700.0, -700.0, -30000.0])
+def test_unusual_logits_of_large_batches(value):
+    t = large(seed=16)
+    t["z"][:, 0] += value
+    t["z"][:10, 1, 5] = value
+    t["y"][:, 1] -= value
+    t["y"][5:15, 1, 109990] = value
+    t["z"][20:30, 2, ::2] = value
+    check(t, "large, value %g" % value)
+
+
+@pytest.mark.parametrize("certain", [False, True])
+def test_masked_actions_of_large_batches(certain):
+    t = large(certain, seed=17)
+    g = np.random.default_rng(18)
+    low = torch.finfo(torch.bfloat16).min
+    dead = torch.from_numpy(g.random((40, 3, 110000)) < 0.99)
+    dead[:, :, 17] = False
+    z = t["z"].masked_fill(dead, float("-inf"))
+    z[20:] = torch.where(dead[20:], torch.tensor(low, dtype=z.dtype), t["z"][20:])
+    z[7, 0, :] = float("-inf")
+    z[7, 0, 100001] = 3.0  # one action
+    t["z"] = z
+    if not certain:
+        t["y"][:, :, 50000:] = float("-inf")
+        t["ids"].clamp_(max=49999)
+    check(t, "large, masked actions")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), "none"])
+@pytest.mark.parametrize("where", ["target", "draft"])
+def test_rows_without_a_distribution_in_large_batches(bad, where):
+    t = large(near=0.0, seed=19)
+    x = t["z"] if where == "target" else t["y"]
+    if bad == "none":
+        x[:6, 1] = float("-inf")
+    else:
+        x[:6, 1, 109999] = bad
+    out = check(t, "large, undefined %s" % where)
+    assert (out["accepted"][:6] == 1).all() and (out["ids"][:6, 1] == -1).all()
+
+
+@pytest.mark.parametrize("B,D,V", [(2049, 2, 77), (2500, 3, 300), (9000, 2, 520)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("certain", [False, True])
+def test_many_sequences(B, D, V, dtype, certain):
+    t = make(B, D, V, dtype, certain, True, near=0.3, seed=20)
+    t["mask"] = torch.from_numpy((np.random.default_rng(21).random(B) < 0.8).astype(np.uint8))
+    check(t, "many sequences %d %d %d" % (B, D, V))
+
+
+@pytest.mark.parametrize("B", [1, 5])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("certain", [False, True])
+def test_rows_of_over_a_million(B, dtype, certain):
+    check(make(B, 1, 1100003, dtype, certain, near=0.1, seed=22), "long rows")
+
+
 def test_masked_sequences_are_left_alone():
     t = make(9, 3, 500, "f32", near=0.3, seed=10)
     t["mask"] = torch.tensor([1, 0, 1, 1, 0, 0, 1, 1, 0], dtype=torch.uint8)

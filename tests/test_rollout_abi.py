@@ -58,8 +58,12 @@ def head(x=FAKE, ldx=None, sx=FAKE, w=FAKE, ldw=None, sw=FAKE, scale=0, N=4, V=1
     (dict(V=2 ** 30 + 8), SHAPE),
     (dict(H=0), SHAPE),
     (dict(ld=1000), SHAPE),
+    (dict(H=2 ** 22 + 16), SHAPE),
     (dict(ldx=128), SHAPE),
     (dict(ldw=128), SHAPE),
+    (dict(ldx=2 ** 22 + 16), SHAPE),
+    (dict(ldw=2 ** 22 + 16), SHAPE),
+    (dict(N=2 ** 30, V=2 ** 17, ld=2 ** 17), SHAPE),
     (dict(x=None), NULL),
     (dict(sx=None), NULL),
     (dict(w=None), NULL),
