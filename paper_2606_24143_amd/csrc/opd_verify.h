@@ -401,20 +401,29 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, in
   uint32_t parts = (uint32_t)a.parts, part_groups = a.part_groups;
   const uint32_t groups = (uint32_t)((a.V + 7) >> 3);
   const bool listed = a.B <= kListed;
-  ver_setup<TABLE, kVerThreads>(tab, c.factors);
   uint64_t items;
+  uint32_t all = 0;  // rows of the round
   const uint32_t most = (uint32_t)(pos1 - pos0) * (a.draft ? 2u : 1u);  // rows of a sequence
+  constexpr int PER = kListed / kVerThreads;
+  uint32_t mine[PER], sum = 0;
   if (listed) {
-    constexpr int PER = kListed / kVerThreads;
-    uint32_t mine[PER], sum = 0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int64_t b = (int64_t)tid * PER + k;
-      mine[k] = sum;
+      mine[k] = 0;
       if (b < a.B) {
         const RoundRows r = round_rows(a, ws, b, pos0, pos1);
-        sum += (uint32_t)(r.targets + r.drafts);
+        mine[k] = (uint32_t)(r.targets + r.drafts);
       }
+    }
+  }
+  ver_setup<TABLE, kVerThreads>(tab, c.factors);
+  if (listed) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const uint32_t rows = mine[k];
+      mine[k] = sum;
+      sum += rows;
     }
     uint32_t incl = sum;
 #pragma unroll
@@ -428,22 +437,25 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, in
     for (uint32_t k = 0; k < w; ++k) at += wsum[k];
 #pragma unroll
     for (int k = 0; k < PER; ++k) c.before[tid * PER + k] = at + mine[k];
-    uint32_t all = 0;
 #pragma unroll
     for (int k = 0; k < kVerWaves; ++k) all += wsum[k];
     __syncthreads();
     // as many parts to a row as give the wavefronts the least to do: whole items, and
     // for each kItemCost of a row besides (the first loads and the record)
     constexpr float kItemCost = 0.03f;
-    const uint32_t tiles = (groups + 255) / 256;
-    float best = 1e30f;
-    for (uint32_t p = 1; p <= (uint32_t)a.parts; ++p) {
-      const float cost = (float)((all * p + W - 1) / W) * (1.f / (float)p + kItemCost);
-      if (cost < best) {
-        best = cost;
-        parts = p;
+    const uint32_t tiles = (groups + 255) / 256, p = min(lane + 1, (uint32_t)a.parts);  // (64 at most)
+    float cost = (float)((all * p + W - 1) / W) * (1.f / (float)p + kItemCost);
+    parts = p;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const float x = __shfl_xor(cost, o, 64);
+      const uint32_t xp = (uint32_t)__shfl_xor((int)parts, o, 64);
+      if (x < cost || (x == cost && xp < parts)) {
+        cost = x;
+        parts = xp;
       }
     }
+    parts = (uint32_t)__builtin_amdgcn_readfirstlane((int)parts);
     part_groups = (tiles + parts - 1) / parts * 256;
     parts = (groups + part_groups - 1) / part_groups;
     items = (uint64_t)all * parts;
@@ -462,6 +474,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, in
       const uint32_t part = (uint32_t)(k - u * parts);
       uint32_t r;
       int64_t b;
+      RoundRows rr;
       if (listed) {
         uint32_t lo = 0, hi = (uint32_t)a.B - 1;  // the last sequence with before <= u
         while (lo < hi) {
@@ -469,19 +482,22 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, in
           if (c.before[mid] <= (uint32_t)u) lo = mid;
           else hi = mid - 1;
         }
-        b = lo;
-        r = (uint32_t)u - c.before[lo];
+        const uint32_t from = c.before[lo];
+        const int n = (int)((lo + 1 < (uint32_t)a.B ? c.before[lo + 1] : all) - from);
+        // (a target row without a draft row is the last)
+        rr = a.draft ? RoundRows{(n + 1) / 2, n / 2} : RoundRows{n, 0};
+        b = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
+        r = (uint32_t)u - from;
       } else {
         b = (int64_t)(u / most);
         r = (uint32_t)(u - (uint64_t)b * most);
+        rr = round_rows(a, ws, b, pos0, pos1);
+        if (r >= (uint32_t)(rr.targets + rr.drafts)) continue;
       }
-      b = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)b);
-      r = (uint32_t)__builtin_amdgcn_readfirstlane((int)r);
-      const RoundRows rr = round_rows(a, ws, b, pos0, pos1);
-      if (r >= (uint32_t)(rr.targets + rr.drafts)) continue;  // (not listed)
-      const bool draft = r >= (uint32_t)rr.targets;
-      const int pos = pos0 + (int)(draft ? r - rr.targets : r);
-      if (pos + (int)ws.stop[b] > a.D + 1) continue;  // (refused by now)
+      const bool draft = __builtin_amdgcn_readfirstlane(r >= (uint32_t)rr.targets);
+      const int pos = __builtin_amdgcn_readfirstlane(pos0 + (int)(draft ? r - rr.targets : r));
+      // (refused by now; nothing is while the first items are on their way)
+      if (k >= W && pos + (int)ws.stop[b] > a.D + 1) continue;
       const uint32_t g0 = part * part_groups, g1 = min(g0 + part_groups, groups);
       const int64_t tr = target_row(a, b, pos), dr = a.B * (a.D + 1) + draft_row(a, b, pos);
       const VerRec x = part_record<TI, TABLE>(
@@ -495,7 +511,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, in
         my_tr = tr;
         my_b = (uint32_t)b;
         my_pos = pos;
-        my_pair = a.draft && pos < drafted(a, b);
+        my_pair = pos - pos0 < rr.drafts;
       }
       ++held;
     }
@@ -657,38 +673,37 @@ __device__ __forceinline__ void chunk_masses(const VerifyArgs& a, const DrawRow<
         out[q] = all;
     }
   };
-  uint32_t q = q0 + w * K;
+  uint32_t q = q0;
   if (CG == 64) {
-    for (; q + K <= q1 && (q + K) * 64 <= full; q += kVerWaves * K) {
+    for (; q + K * kVerWaves <= q1 && (q + K * kVerWaves) * 64 <= full; q += K * kVerWaves) {
+      const uint32_t qw = q + w * K;
       Group<TI> z[K], y[K];
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        z[k] = group_load<TI>(d.z, (q + k) * 64 + lane);
-        y[k] = d.mass == kResidual ? group_load<TI>(d.y, (q + k) * 64 + lane) : z[k];
+        z[k] = group_load<TI>(d.z, (qw + k) * 64 + lane);
+        y[k] = d.mass == kResidual ? group_load<TI>(d.y, (qw + k) * 64 + lane) : z[k];
       }
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         double v[8], sum = 0.0;
-        group_masses<TI, TABLE>(d, z[k], y[k], (q + k) * 64 + lane, tab, c2, v);
+        group_masses<TI, TABLE>(d, z[k], y[k], (qw + k) * 64 + lane, tab, c2, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum += v[e];
-        put(q + k, sum);
+        put(qw + k, sum);
       }
     }
   }
-  for (; q < q1; q += kVerWaves * K) {
 #pragma unroll 1
-    for (uint32_t k = q; k < min(q + K, q1); ++k) {
-      double sum = 0.0;
-      const uint32_t c1 = min(k * CG + CG, groups);
-      for (uint32_t g = k * CG; g < c1; g += 64) {
-        double v[8];
-        masses_at<TI, TABLE>(a, d, g + lane, c1, tab, c2, v);
+  for (uint32_t k = q + w; k < q1; k += kVerWaves) {  // the rest one by one
+    double sum = 0.0;
+    const uint32_t c1 = min(k * CG + CG, groups);
+    for (uint32_t g = k * CG; g < c1; g += 64) {
+      double v[8];
+      masses_at<TI, TABLE>(a, d, g + lane, c1, tab, c2, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += v[e];
-      }
-      put(k, sum);
+      for (int e = 0; e < 8; ++e) sum += v[e];
     }
+    put(k, sum);
   }
 }
 
@@ -707,6 +722,9 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
   const int parts = a.draw_parts;
   const double c2 = c2_reg();
   static_assert(kTabBinades * 32 <= kSmpMaxChunks, "the table's factors fit the masses");
+  // (the first item's words are on their way during the setup)
+  int n = drafted(a, blockIdx.x / parts);
+  uint32_t stop = ws.stop[blockIdx.x / parts];
   ver_setup<TABLE, kVerThreads>(tab, c.s);
   for (int64_t k = blockIdx.x; k < a.B * parts; k += gridDim.x) {
     const int64_t b = k / parts;
@@ -714,9 +732,12 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
     int32_t* ids = a.ids_out + b * (a.D + 1);
     float* logp = a.logp ? a.logp + b * (a.D + 1) : nullptr;
     const bool masked = a.mask && a.mask[b] == 0;
-    const int n = drafted(a, b);
+    if (k != blockIdx.x) {
+      n = drafted(a, b);
+      stop = ws.stop[b];
+    }
     // the first token that is not kept
-    const uint32_t st = n < 0 ? 0 : ws.stop[b];
+    const uint32_t st = n < 0 ? 0 : stop;
     const int kept = n < 0 ? 0 : st ? a.D + 1 - (int)st : n;
     const uint32_t test = n < 0 ? (uint32_t)kBad : st ? ws.test[b * (a.D + 1) + kept] : (uint32_t)kKept;
     const float u = a.u[b * (a.D + 1) + a.D];
