@@ -347,16 +347,17 @@ __device__ __forceinline__ Rsrc rows_rsrc(const void* p, int64_t bytes) {
 // Up to 128 tokens the product is a read of the head.  W waves of 16 of its rows
 // each, all tokens (T groups of 16).  The head goes from memory to the matrix
 // instructions' registers, SB blocks ahead; the tokens through LDS, SB blocks a
-// stage, shared by the waves.  Workgroups start at different stages of the rows
-// (T > 1): rows are often a multiple of 4 KiB apart, and all reads at one place of
-// them wait for the same part of the memory (127 against 137 us at 32 tokens,
-// V = 151,936, H = 4,096).
+// stage, shared by the waves.  Workgroups start at different stages of the rows:
+// rows are often a multiple of 4 KiB apart, and all reads at one place of them wait
+// for the same part of the memory (127 against 137 us at 32 tokens, V = 151,936, H =
+// 4,096; 27 against 30 at 16, V = 32,000).  At V = 151,936, H = 4,096 (622 MB): 1 token
+// 112 us (5.6 TB/s), 32 120, 64 135, 128 178; reads alone in this order take 100.  Two
+// groups of rows to a wave, which halve the reads of LDS, gave 139 for 64.
 template <class TO, bool E8, bool ODD, int T, int SB, int W>
 __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   constexpr bool HW = E8 && TO::BYTES == 2;
   constexpr int SZ = E8 ? 1 : 4, THREADS = 64 * W;
   constexpr int ROWS = 16 * T, PIECES = ROWS * SB * 8, PER = (PIECES + THREADS - 1) / THREADS;
-  static_assert(ROWS * SB <= THREADS * 2, "scales");
   constexpr int SPER = (ROWS * SB + THREADS - 1) / THREADS;
   __shared__ __align__(16) uint8_t lx[2][SB][ROWS * 128];
   __shared__ uint32_t lsc[2][SB][ROWS];
@@ -376,8 +377,10 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   u32x4 px[PER];
   uint32_t ps[SPER], hs[SB];
   i32x8 bw[SB];
-  auto ask_x = [&](int b0) {
-    const Rsrc q = rows_rsrc(a.x + (int64_t)b0 * kBlk, xbytes - (int64_t)b0 * kBlk);
+  // (`more`: no stage is read twice, which the last ones would be)
+  auto ask_x = [&](int b0, bool more) {
+    const Rsrc q =
+        rows_rsrc(a.x + (int64_t)b0 * kBlk, more ? xbytes - (int64_t)b0 * kBlk : 0);
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const uint32_t i = (uint32_t)tid + k * THREADS, at = i & (SB * 8 - 1), row = i / (SB * 8);
@@ -385,7 +388,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
       px[k] = __builtin_amdgcn_raw_buffer_load_b128(q, in ? (int)(row * ldx + at * 16) : INT32_MIN,
                                                     0, 0);
     }
-    const Rsrc qs = rows_rsrc((const uint8_t*)a.sx + b0 * SZ, sbytes - b0 * SZ);
+    const Rsrc qs = rows_rsrc((const uint8_t*)a.sx + b0 * SZ, more ? sbytes - b0 * SZ : 0);
 #pragma unroll
     for (int k = 0; k < SPER; ++k) {
       const uint32_t i = (uint32_t)tid + k * THREADS, row = i / SB, b = i & (SB - 1);
@@ -410,15 +413,15 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
       if (row < ROWS) lsc[buf][i & (SB - 1)][row] = ps[k];
     }
   };
-  auto ask_w = [&](int d, int b) {
+  auto ask_w = [&](int d, int b, bool more) {
     const int h = b * kBlk + (int)lk * 16;
     const bool in0 = h < (int)a.H, in1 = h + 64 < (int)a.H;
-    const Rsrc q = rows_rsrc(gw + (int64_t)b * kBlk, wbytes - (int64_t)b * kBlk);
+    const Rsrc q = rows_rsrc(gw + (int64_t)b * kBlk, more ? wbytes - (int64_t)b * kBlk : 0);
     const u32x4 lo = __builtin_amdgcn_raw_buffer_load_b128(q, in0 ? (int)ow : INT32_MIN, 0, 0);
     const u32x4 hi =
         __builtin_amdgcn_raw_buffer_load_b128(q, in1 ? (int)(ow + 64) : INT32_MIN, 0, 0);
     bw[d] = __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    const Rsrc qs = rows_rsrc(gh + b * SZ, b < a.nb ? SZ : 0);
+    const Rsrc qs = rows_rsrc(gh + b * SZ, more && b < a.nb ? SZ : 0);
     if constexpr (E8)
       hs[d] = __builtin_amdgcn_raw_buffer_load_b8(qs, 0, 0, 0);
     else
@@ -463,13 +466,13 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   };
   // stages in a cycle that starts elsewhere for each workgroup
   const int stages = (a.nb + SB - 1) / SB;
-  int now = T > 1 ? (int)(blockIdx.x % (uint32_t)stages) : 0;  // the stage that is multiplied
+  int now = (int)(blockIdx.x % (uint32_t)stages);  // the stage that is multiplied
   auto after = [&](int at) { return at + 1 == stages ? 0 : at + 1; };
-  ask_x(now * SB);
+  ask_x(now * SB, true);
 #pragma unroll
-  for (int d = 0; d < SB; ++d) ask_w(d, now * SB + d);
+  for (int d = 0; d < SB; ++d) ask_w(d, now * SB + d, true);
   put_x(0, now * SB);
-  ask_x(after(now) * SB);
+  ask_x(after(now) * SB, stages > 1);
   int buf = 0;
   for (int i = 0; i < stages; ++i, buf ^= 1) {
     __syncthreads();
@@ -477,11 +480,11 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
 #pragma unroll
     for (int d = 0; d < SB; ++d) {
       multiply(d, buf, now * SB + d);
-      ask_w(d, next * SB + d);
+      ask_w(d, next * SB + d, i + 1 < stages);
       __builtin_amdgcn_sched_barrier(0);
       if (d == SB - 1) {
         put_x(buf ^ 1, next * SB);
-        ask_x(after(next) * SB);
+        ask_x(after(next) * SB, i + 2 < stages);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -499,8 +502,7 @@ template <class TO, bool E8, int T, int SB, int W>
 hipError_t launch_stream(const HeadArgs& a, hipStream_t stream) {
   const auto kernel = a.H % 16 != 0 ? k_head_stream<TO, E8, true, T, SB, W>
                                     : k_head_stream<TO, E8, false, T, SB, W>;
-  hipLaunchKernelGGL(kernel,
-                     dim3((unsigned)((a.V + 16 * W - 1) / (16 * W))), dim3(64 * W), 0,
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((a.V + 16 * W - 1) / (16 * W))), dim3(64 * W), 0,
                      stream, a);
   return hipGetLastError();
 }
