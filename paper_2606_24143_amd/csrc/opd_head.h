@@ -344,8 +344,8 @@ __device__ __forceinline__ Rsrc rows_rsrc(const void* p, int64_t bytes) {
 }
 
 // ---- few tokens
-// Up to 128 tokens the product is a read of the head.  W waves of 16 of its rows
-// each, all tokens (T groups of 16).  The head goes from memory to the matrix
+// Of few tokens the product is a read of the head.  W waves of 16 of its rows each,
+// 128 tokens at most (T groups of 16; of more, blockIdx.y's).  The head goes from memory to the matrix
 // instructions' registers, SB blocks ahead; the tokens through LDS, SB blocks a
 // stage, shared by the waves.  Workgroups start at different stages of the rows:
 // rows are often a multiple of 4 KiB apart, and all reads at one place of them wait
@@ -365,6 +365,11 @@ __global__ void __launch_bounds__(64 * W, 2) k_head_stream(HeadArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t lr = (uint32_t)lane & 15u, lk = (uint32_t)lane >> 4;
   const int64_t v0 = ((int64_t)blockIdx.x * W + w) * 16;
+  const int64_t n0 = (int64_t)blockIdx.y * ROWS;  // the launch's tokens are 16 T at a time
+  a.x += n0 * a.ldx;
+  a.sx = (const char*)a.sx + n0 * a.nb * SZ;
+  a.out = (char*)a.out + n0 * a.ldo * TO::BYTES;
+  a.N = min(a.N - n0, (int64_t)ROWS);
   const uint32_t ldw = (uint32_t)a.ldw, ldx = (uint32_t)a.ldx;
   const int64_t vr = min(v0, a.V - 1);  // (a wave past the last row reads nothing)
   const uint8_t* gw = a.w + vr * a.ldw;
@@ -502,8 +507,10 @@ template <class TO, bool E8, int T, int SB, int W>
 hipError_t launch_stream(const HeadArgs& a, hipStream_t stream) {
   const auto kernel = a.H % 16 != 0 ? k_head_stream<TO, E8, true, T, SB, W>
                                     : k_head_stream<TO, E8, false, T, SB, W>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((a.V + 16 * W - 1) / (16 * W))), dim3(64 * W), 0,
-                     stream, a);
+  hipLaunchKernelGGL(kernel,
+                     dim3((unsigned)((a.V + 16 * W - 1) / (16 * W)),
+                          (unsigned)((a.N + 16 * T - 1) / (16 * T))),
+                     dim3(64 * W), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -780,9 +787,15 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
   }
 }
 
+// Up to 128 tokens, or so few logits that their tiles leave CUs idle, the rows are
+// streamed (for every 128 tokens again).  Streamed / tiled, us, fp32 scales: V = 151,936,
+// H = 4,096, 128 tokens 178 / 214; V = 32,000, H = 4,096, 256 73 / 141, 384 98 / 117, 512
+// 124 / 130 (e8m0 113 / 102), 1,024 229 / 153; V = 50,257, H = 2,048, 256 66 / 83, 384 85 / 80;
+// V = 8,000, H = 4,096, 512 39 / 64, 1,024 65 / 71.
+constexpr int64_t kFewLogits = 14000000;
 template <class TO, bool E8>
 hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
-  if (a.N <= 128) return launch_few<TO, E8>(a, stream);
+  if (a.N <= 128 || a.N * a.V <= kFewLogits) return launch_few<TO, E8>(a, stream);
   a.ntiles = (a.N + kTileN - 1) / kTileN;
   const int64_t tiles = (a.V + kTileV - 1) / kTileV * a.ntiles;
   const auto kernel = a.H % 16 != 0 ? k_head_tile<TO, E8, true> : k_head_tile<TO, E8, false>;

@@ -102,7 +102,9 @@ def head_tolerance(mags, z, H, out, x, sx, w, sw):
     (100, 1537, 768), (128, 384, 128), (129, 260, 1024), (200, 3001, 896), (256, 512, 2048),
     (257, 1025, 272), (300, 2050, 1152), (520, 777, 640),
     (600, 30011, 272), (300, 515, 7), (260, 300, 135), (150, 777, 1001), (31, 4100, 333),
-    (100, 640, 2047), (16, 13001, 384), (40, 25003, 256), (90, 30000, 640)])
+    (100, 640, 2047), (16, 13001, 384), (40, 25003, 256), (90, 30000, 640),
+    (129, 108701, 130), (257, 54501, 200), (1000, 14100, 7), (14001, 1000, 384), (4100, 3500, 2047),
+    (700, 20100, 16), (300, 50001, 1008)])
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_head_logits(N, V, H, scale, out):
@@ -132,7 +134,8 @@ def test_head_logits(N, V, H, scale, out):
 
 
 @pytest.mark.parametrize("N,V,H", [(1, 100, 9), (20, 300, 130), (128, 700, 255), (260, 300, 135),
-                                   (300, 1000, 2047), (130, 515, 15)])
+                                   (300, 1000, 2047), (130, 515, 15), (300, 50001, 135),
+                                   (14100, 1000, 255), (1000, 14100, 2047)])
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_what_lies_past_a_row_is_not_used(N, V, H, scale, out):
@@ -154,7 +157,7 @@ def test_what_lies_past_a_row_is_not_used(N, V, H, scale, out):
         assert torch.equal(other, z[0])
 
 
-@pytest.mark.parametrize("N", [1, 40, 300])
+@pytest.mark.parametrize("N", [1, 40, 300, 50000])
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_head_keeps_nan_to_its_rows(N, scale, out):

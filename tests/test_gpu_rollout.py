@@ -87,11 +87,13 @@ def test_a_rollout_with_drafts_down_to_the_loss():
 
 
 CALLS = {
-    # (the head's kernels: streamed rows, tiles, any width)
+    # (the head's kernels: streamed rows, once and again, tiles, an odd width)
     "few tokens": lambda s: opd.head_logits(s["q"][:9], s["s"][:9], *s["w"])["logits"],
+    "more tokens": lambda s: opd.head_logits(s["q"][:300], s["s"][:300], *s["w"])["logits"],
     "tiles": lambda s: opd.head_logits(s["q"], s["s"], *s["w"])["logits"],
-    "any width": lambda s: opd.head_logits(s["q"][:, :120], s["s"][:, :1].contiguous(),
-                                           s["w"][0][:, :120], s["w"][1][:, :1].contiguous())["logits"],
+    "odd width": lambda s: opd.head_logits(s["q"][:, :120], s["s"][:, :1].contiguous(),
+                                           s["w"][0][:, :120],
+                                           s["w"][1][:, :1].contiguous())["logits"],
     "quantize": lambda s: opd.quantize_blocks(s["x"])["q"].view(torch.uint8),
     "verify": lambda s: opd.verify_drafts(s["z"], s["ids"], s["u"], draft_logits=s["y"])["ids"],
     "verify copied": lambda s: opd.verify_drafts(s["z"], s["ids"], s["u"])["logp"],
@@ -99,7 +101,7 @@ CALLS = {
 
 
 def state(seed):
-    x = model(seed, 200)
+    x = model(seed, 5000)
     q = opd.quantize_blocks(x)
     g = torch.Generator(DEV).manual_seed(seed)
     z = logits(x[:8 * 4], head(seed))
@@ -170,7 +172,7 @@ def test_verify_replayed_from_a_graph():
                    lambda: opd.verify_drafts(other["z"], other["ids"], other["u"]))
 
 
-@pytest.mark.parametrize("N", [9, 200])
+@pytest.mark.parametrize("N", [9, 200, 5000])
 def test_head_replayed_from_a_graph(N):
     s, other = state(6), state(7)
     out = torch.empty(N, 3008, dtype=torch.bfloat16, device=DEV)
