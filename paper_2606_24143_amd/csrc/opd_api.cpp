@@ -301,12 +301,18 @@ VerifyPlan verify_plan(int64_t B, int32_t D, int64_t V, int32_t dtype, bool draf
   int64_t k = (opd::kVerGroups + B - 1) / B;
   if (k > groups / 512) k = groups / 512;
   p.draw_parts = k < 1 ? 1 : (int)k;
-  p.table = B * V >= 4000000;
-  // The first round's positions: about 128 MB.  Every round costs some 15 us besides its
-  // reading (a launch, the table, the tests at its end), so small ones do not pay;
-  // later ones have twice the positions, as fewer sequences are left.
-  constexpr int64_t kRoundBytes = (int64_t)128 << 20;
-  const int64_t round = kRoundBytes / ((draft ? 2 : 1) * B * V * elt_bytes(dtype)) + 1;
+  // Terms of bf16 rows from a table, which costs each workgroup some 3 us: D = 4, with /
+  // without it, us: V = 151,936, B = 8 47 / 46, 16 51 / 50, 26 52 / 59, 40 57 / 71;
+  // V = 32,000, B = 32 36 / 35, 64 39 / 42, 128 51 / 61.
+  p.table = B * V >= 2000000;
+  // The first round's positions: some 32 M elements (fp32 rows, bound by arithmetic, take as
+  // long as bf16 ones).  Every round costs about 12 us besides (a launch, the table,
+  // the tests at its end), so small ones do not pay; later ones have twice the
+  // positions, as fewer sequences are left.  First rounds of 2 / 4 / 6 positions, us: 64
+  // sequences of 5 drafts, bf16 V = 151,936 80 / 86 / 80; of 2 / 3 / 6: 256 of 8 drafts,
+  // fp32 V = 50,257 100 / 96 / 118.
+  constexpr int64_t kRoundElements = (int64_t)32 << 20;
+  const int64_t round = kRoundElements / ((draft ? 2 : 1) * B * V) + 1;
   p.round = (int)(round < D + 1 ? round : D + 1);
   const size_t rows = (size_t)B * (size_t)(2 * D + 1);
   p.ws_bytes = rows * 16 * (1 + (size_t)p.parts) +
