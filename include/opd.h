@@ -6,7 +6,9 @@
  * of V entries, plus the finite teacher-score cache those tokens carry, and
  * returns the per-token loss and its gradient with respect to every logit
  * (Sec. 4.1, "Stage 3: Student update": the learner recomputes log p_theta
- * on the cached actions).  All work runs in HIP kernels on the caller's
+ * on the cached actions).  Further calls make what it reads: rows of logits from
+ * 8-bit hidden states and head weights, draws, verified drafts, supports and
+ * scores.  All work runs in HIP kernels on the caller's
  * stream; nothing is computed on the host.
  *
  * Conventions shared by every entry point
@@ -371,7 +373,8 @@ int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, i
  *   sum_{h in block b} x[n, h] w[v, h], in fp32, rounded once to logits_dtype
  *   (OPD_F32 or OPD_BF16).  For fp32 logits products are exact; for bf16 ones
  *   the matrix cores cut each at 2^-13 of the largest of the 16 that they sum
- *   at once, far below the rounding.  A NaN in a
+ *   at once, far below the rounding.  (fp32 scales are multiplied first, and
+ *   their product should be finite.)  A NaN in a
  *   token's values or scales reaches its own row only, one in the weights its
  *   own vocabulary entries (a scale: those of its block).
  *     x [N, ldx], x_scales [N, nb]; w [V, ldw], w_scales [ceil(V / 128), nb];
@@ -427,7 +430,9 @@ int opd_head_logits(const void* x, int64_t ldx, const void* x_scales, const void
  *   ids            [B, D + 1] int32 out: those, then the drawn token, then -1
  *   logp           [B, D + 1] fp32 out, nullable: log p at these tokens (what
  *                  the MC estimators read as behav_logp), 0 past them
- *   workspace      16-byte aligned, opd_verify_workspace_bytes(...) bytes
+ *   workspace      16-byte aligned, opd_verify_workspace_bytes(...) bytes, of any
+ *                  content; calls (and captured graphs) that may overlap need
+ *                  one each
  * Rows behind the first refusal have no part in the results and may stay unread.
  * Masked sequences get accepted 0, ids -1 and logp 0.  A sequence ends with id -1
  * and logp NaN, in place of the drawn token, at the first position whose

@@ -382,7 +382,7 @@ const char* opd_status_string(int status) {
     case OPD_ERR_ESTIMATOR: return "unknown estimator";
     case OPD_ERR_FLAGS: return "unknown or contradictory flags";
     case OPD_ERR_HIP: return "HIP runtime error";
-    case OPD_ERR_PARAM: return "invalid scalar option or output (clip_eps, coverage_out)";
+    case OPD_ERR_PARAM: return "invalid scalar option or output (clip_eps, coverage_out, block_rows)";
     case OPD_ERR_SCRATCH:
       return "the call needs more scratch than the no-allocation entry point holds";
   }

@@ -10,6 +10,8 @@
 //   top-k   the k largest logits (descending, equal values by lower index),
 //           plus log softmax(z) there;
 //   score   log softmax(z) at given ids.
+// (opd_head.h, included below: the rows of logits themselves from 8-bit operands;
+// opd_verify.h: rollout with drafted tokens.)
 // One 1024-lane workgroup per token row.  A row that fits the registers
 // (bf16 up to 155,648 entries, fp32 up to 77,824) is loaded once and kept
 // there; wider rows are streamed.
