@@ -385,7 +385,7 @@ int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, i
  *   bytes; what is there past H may hold anything.
  *
  * Errors: OPD_ERR_DTYPE (dtype or scale_type), OPD_ERR_SHAPE (N < 0, N >=
- * 2^31, V outside [2, 2^30], H outside [1, 2^22], a row stride below its row's
+ * 2^31, V outside [2, 2^29], H outside [1, 2^22], a row stride below its row's
  * length; in opd_head_logits also ldx or ldw above 2^22, N * V above 2^46),
  * OPD_ERR_PARAM (block_rows not 1 or 128), OPD_ERR_ALIGN, OPD_ERR_NULL,
  * OPD_ERR_HIP.  N == 0 is a no-op returning OPD_OK.

@@ -256,9 +256,9 @@ bool row_fits(int64_t nvec, int32_t dtype) {
 }
 
 // Arguments shared by the blockwise calls.
-// (the head's kernels address the rows of a tile within 2 GiB and count tiles of 2^16
-// logits in 32 bits)
-constexpr int64_t kMaxHidden = (int64_t)1 << 22, kMaxHeadRows = (int64_t)1 << 30;
+// (the head's kernels address the rows of a tile within 2 GiB, count tiles of 2^16
+// logits in 32 bits, and have four work-items to a row of the head)
+constexpr int64_t kMaxHidden = (int64_t)1 << 22, kMaxHeadRows = (int64_t)1 << 29;
 constexpr int64_t kMaxLogits = (int64_t)1 << 46;
 int check_blocks(int64_t N, int64_t H, int32_t scale_type) {
   if (scale_type != OPD_SCALE_F32 && scale_type != OPD_SCALE_E8M0) return OPD_ERR_DTYPE;

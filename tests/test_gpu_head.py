@@ -189,6 +189,30 @@ def test_head_keeps_nan_to_its_rows(N, scale, out):
     assert torch.equal(got[~bad], want[~bad])
 
 
+@pytest.mark.parametrize("H", [100, 135, 272, 400])
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_edges_of_tiles(H, scale, out):
+    """A token's logits are the same in a tile that it shares with any number of
+    others, and an entry's in one that the vocabulary ends in anywhere."""
+    N, V = 512, 54784  # (tiles of 256 by 256 from 257 tokens and 54,500 entries on)
+    g = np.random.default_rng(9)
+    x, sx, _, _ = quantized(g.normal(0, 1, (N, H)).astype(np.float32), 1, scale)
+    w, sw, _, _ = quantized(g.normal(0, 1, (V, H)).astype(np.float32), 128, scale)
+    want = opd.head_logits(x, sx, w, sw, dtype=DT[out])["logits"]
+    buf = torch.empty(N, V, dtype=DT[out], device=DEV)
+    for n in range(257, 513):
+        buf.fill_(777.0)
+        got = opd.head_logits(x[:n], sx[:n], w, sw, dtype=DT[out], out=buf[:n])["logits"]
+        assert torch.equal(got, want[:n]) and (buf[n:] == 777.0).all(), n
+    for v in range(V - 256, V):
+        buf.fill_(777.0)
+        opd.head_logits(x[:257], sx[:257], w[:v], sw[:(v + 127) // 128], dtype=DT[out],
+                        out=buf[:257])
+        assert torch.equal(buf[:257, :v], want[:257, :v]) and (buf[:257, v:] == 777.0).all(), v
+    assert torch.isfinite(want).all()
+
+
 def test_no_rows():
     w, sw, _, _ = quantized(np.ones((64, 128), np.float32), 128, "f32")
     x = torch.empty(0, 128, dtype=torch.float8_e4m3fn, device=DEV)

@@ -55,6 +55,7 @@ def head(x=FAKE, ldx=None, sx=FAKE, w=FAKE, ldw=None, sw=FAKE, scale=0, N=4, V=1
     (dict(N=2 ** 31), SHAPE),
     (dict(V=1), SHAPE),
     (dict(V=2 ** 31), SHAPE),
+    (dict(V=2 ** 29 + 8, ld=2 ** 29 + 8), SHAPE),
     (dict(V=2 ** 30 + 8), SHAPE),
     (dict(H=0), SHAPE),
     (dict(ld=1000), SHAPE),
