@@ -222,6 +222,19 @@ def test_no_rows():
     assert q["q"].shape == (0, 128) and q["scales"].shape == (0, 1)
 
 
+@pytest.mark.parametrize("rows", [1, 128])
+def test_rows_past_4_gib(rows):
+    """Offsets that pass 32 bits in the rows and in the values."""
+    N, H = (1 << 22) + 128 + 5, 1024
+    x = torch.zeros(N, H, dtype=torch.bfloat16, device=DEV)
+    x[-133:] = torch.randn(133, H, device=DEV, generator=torch.Generator(DEV).manual_seed(4))
+    out = opd.quantize_blocks(x, block_rows=rows)
+    alone = opd.quantize_blocks(x[-133:], block_rows=rows)
+    assert torch.equal(out["q"][-133:].view(torch.uint8), alone["q"].view(torch.uint8))
+    assert torch.equal(out["scales"][-alone["scales"].shape[0]:], alone["scales"])
+    assert (out["q"][:-133].view(torch.uint8) == 0).all()
+
+
 def test_logits_past_4_gib():
     """Rows whose offsets pass 32 bits, in the weights' rows and in the logits."""
     N, V, H = 1100, 1 << 21, 128
