@@ -714,7 +714,7 @@ __device__ __forceinline__ void chunk_masses(const VerifyArgs& a, const DrawRow<
 
 // A sequence's tokens: the kept ones, then the draw.  The row that it is drawn from
 // (for a residual, the draft's too) is read again, as its masses need both rows'
-// sums: 250 MB in 66 us at 512 sequences of 8 drafts, V = 151,936; 24 us at 64 of 5,
+// sums: 250 MB in 66-82 us at 512 sequences of 8 drafts, V = 151,936; 24 us at 64 of 5,
 // of which the table is 4 and the last workgroup of a sequence 6.  Item k: part k % draw_parts of
 // the row that sequence k / draw_parts is drawn from; whoever ends a sequence's
 // last part draws.
