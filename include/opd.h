@@ -411,10 +411,14 @@ int opd_head_logits(const void* x, int64_t ldx, const void* x_scales, const void
  *
  * The draw is by inversion in index order at u[D]: the first index at which the
  * cumulative mass exceeds u[D] times the whole.  Tests and draw are evaluated in
- * double precision, so they are those of exact arithmetic unless a uniform lies
- * within about 1e-13 of a border.  Where a token is refused and rounding leaves
- * no residual at all (p and q are equal to double precision but for it), the
- * draw is from p.
+ * double precision, wherever the logits lie (a row of the type's lowest value is
+ * uniform), so they are those of exact arithmetic unless u[i] q_i(x_i) and
+ * p_i(x_i) differ by less than about 1e-13 of p_i(x_i), or u[D] times the whole
+ * lies within about 1e-13 of a cumulative mass.  (Masses of a residual are not
+ * divided by its sum; the sums' part of the 1e-13 is a bound at V = 150,000 and
+ * grows with V; probabilities below about 1e-280 may count as 0.)  Where a token
+ * is refused and rounding leaves no residual at all (p and q are equal to double
+ * precision but for it), the draw is from p.
  *
  *   target_logits  [B * (D + 1), ld], sequence b's rows b (D + 1) .. b (D + 1) + D
  *   draft_logits   [B * D, draft_ld], nullable, of the same dtype: NULL means

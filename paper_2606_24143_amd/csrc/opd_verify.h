@@ -7,9 +7,10 @@
 // q_{n-1}.  Token x_i is kept while u_i q_i(x_i) < p_i(x_i).  At the first that is
 // not, one token is drawn from max(p_i - q_i, 0) over its sum; if all are kept,
 // from p_n.  So the tokens that come out follow the target, and their log-probs
-// under it are the cache's behav_logp.  All in double precision: the decisions
-// and the draw are those of exact arithmetic unless a uniform lies within about
-// 1e-13 of a border.
+// under it are the cache's behav_logp.  All in double precision, relative to a
+// row's maximum where its logits lie far from 0: the decisions and the draw are
+// those of exact arithmetic unless u q and p differ by less than about 1e-13 of p,
+// or the draw's uniform lies as near to a cumulative mass.
 //
 // k_verify_rows sums the rows, k_verify_draw draws.  Rows past a sequence's first
 // refusal have no part in the result, and they are an eighth to three quarters of
@@ -35,10 +36,13 @@ enum Test : uint32_t { kUntested = 0, kKept = 1, kRefused = 2, kBad = 3 };
 struct VerRec {
   double m, s;
 };
-// A row: its log-sum-exp (NaN: no distribution), and the largest m of its parts.
+// A row sums to exp(m + l): m the largest of its parts', l NaN without a
+// distribution.  Kept apart, since far from 0 the sum m + l is m: log p(z) is (z - m)
+// - l, of a difference exact to 2^-53 of itself.
 struct VerRow {
-  double L, m;
+  double l, m;
 };
+__device__ __forceinline__ double log_p(float z, const VerRow& r) { return ((double)z - r.m) - r.l; }
 
 // LDS of the terms: the 512 powers of the exponential, and exp(z) of each bf16 z.
 template <bool TABLE>
@@ -343,20 +347,22 @@ __device__ __forceinline__ VerRow row_of_parts(const VerRec* r, int parts, const
   for (int o = 32; o >= 1; o >>= 1) m = fmax(m, __shfl_xor(m, o, 64));
   if (m == (double)kNegInf) return VerRow{__builtin_nan(""), m};
   const double s = wave_sum_f64(x.s * (x.m == m ? 1.0 : exp_neg(x.m - m, tab)));
-  return VerRow{m + log(s), m};
+  return VerRow{log(s), m};
 }
 
 // The test of token i of sequence b, its rows summed (one lane).
 template <class TI>
-__device__ __forceinline__ uint32_t test_token(const VerifyArgs& a, int64_t b, int i, double L,
-                                               double Lq, const double* tab) {
+__device__ __forceinline__ uint32_t test_token(const VerifyArgs& a, int64_t b, int i,
+                                               const VerRow& rt, const VerRow& rd,
+                                               const double* tab) {
   const int32_t x = a.ids[b * a.D + i];
   const float u = a.u[b * (a.D + 1) + i];
-  if ((uint64_t)(uint32_t)x >= (uint64_t)a.V || !(L == L) || !(Lq == Lq) || !(u >= 0.f && u < 1.f))
+  if ((uint64_t)(uint32_t)x >= (uint64_t)a.V || !(rt.l == rt.l) || !(rd.l == rd.l) ||
+      !(u >= 0.f && u < 1.f))
     return kBad;
-  const double p = exp_neg((double)load_elem<TI>(target_ptr<TI>(a, b, i), x) - L, tab);
+  const double p = exp_neg(log_p(load_elem<TI>(target_ptr<TI>(a, b, i), x), rt), tab);
   const double q =
-      a.draft ? exp_neg((double)load_elem<TI>(draft_ptr<TI>(a, b, i), x) - Lq, tab) : 1.0;
+      a.draft ? exp_neg(log_p(load_elem<TI>(draft_ptr<TI>(a, b, i), x), rd), tab) : 1.0;
   return (double)u * q < p ? kKept : kRefused;
 }
 
@@ -541,7 +547,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_rows(VerifyArgs a, in
         ws.row[tr] = rt;
         if (pair) ws.row[dr] = rd;
         if (pos < drafted(a, b)) {
-          const uint32_t t = test_token<TI>(a, b, pos, rt.L, rd.L, tab.p);
+          const uint32_t t = test_token<TI>(a, b, pos, rt, rd, tab.p);
           ws.test[tr] = t;
           // (D + 1 - the first refusal, or 0)
           if (t != kKept)
@@ -562,11 +568,12 @@ template <class TI>
 struct DrawRow {
   const char* z;
   const char* y;     // kResidual
-  double L, Lq;
-  double ps, qs;     // exp(-L), exp(-Lq)
+  double ps, qs;     // exp(-l) of both
+  const VerRow* far;  // the target's and the draft's where not direct (in LDS: rare, and
+                      // the registers are full)
   int64_t x;         // kWithout: the refused token
   int mass;
-  bool direct;       // from exp(z) (as the rows were summed), else from exp(z - L)
+  bool direct;       // from exp(z) (as the rows were summed), else from exp(log p)
 };
 
 // The masses of a lane's group, in index order.
@@ -591,8 +598,8 @@ __device__ __forceinline__ void group_masses(const DrawRow<TI>& d, const Group<T
     group_values<TI>(y, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      double v = exp_reduced((double)f[e] - d.L, tab.p, c2);
-      if (d.mass == kResidual) v = fmax(v - exp_reduced((double)h[e] - d.Lq, tab.p, c2), 0.0);
+      double v = exp_reduced(log_p(f[e], d.far[0]), tab.p, c2);
+      if (d.mass == kResidual) v = fmax(v - exp_reduced(log_p(h[e], d.far[1]), tab.p, c2), 0.0);
       w[e] = v;
     }
   }
@@ -616,6 +623,7 @@ struct DrawLds {
   double s[kSmpMaxChunks];  // chunk masses
   double p[kVerThreads];    // inclusive prefix of the runs
   double wt[kVerWaves];
+  VerRow far[2];
   uint32_t word;
 };
 
@@ -763,14 +771,20 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
           d.y = draft_ptr<TI>(a, b, kept);
         }
       }
-      d.L = rt.L;
-      d.Lq = rd.L;
-      d.ps = exp(-rt.L);
-      d.qs = exp(-rd.L);
+      d.ps = exp(-rt.l);
+      d.qs = exp(-rd.l);
       // (both rows summed as exp(z): no logit at or past kVerTop, and no tiny sum)
       d.direct = rt.m == 0.0 && rd.m == 0.0;
+      d.far = c.far;
+      if (!d.direct) {  // (the same in every lane; the item before is done with c)
+        if (tid == 0) {
+          c.far[0] = rt;
+          c.far[1] = rd;
+        }
+        __syncthreads();
+      }
     }
-    const bool draws = rt.L == rt.L && u >= 0.f && u < 1.f;
+    const bool draws = rt.l == rt.l && u >= 0.f && u < 1.f;
     if (parts > 1) {
       if (draws) {
         const uint32_t per = (nchunk + parts - 1) / parts;
@@ -793,8 +807,8 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
       const int32_t x = mine ? a.ids[b * a.D + i] : -1;
       if (i != kept || masked || !draws) ids[i] = x;
       if (logp && (i != kept || masked || !draws))
-        logp[i] = mine ? (float)((double)load_elem<TI>(target_ptr<TI>(a, b, i), x) -
-                                 ws.row[target_row(a, b, i)].L)
+        logp[i] = mine ? (float)log_p(load_elem<TI>(target_ptr<TI>(a, b, i), x),
+                                      ws.row[target_row(a, b, i)])
                        : (i == kept && !masked ? __builtin_nanf("") : 0.f);
     }
     if (tid == 0) a.accepted[b] = kept;
@@ -825,7 +839,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
       // p(x) < q(x) leaves a residual; where rounding hides it the draw is from p
       if (S > 0.0 || d.mass == kTarget) break;
       d.mass = kTarget;
-      d.direct = rt.m == 0.0;
+      d.direct = ws.row[target_row(a, b, kept)].m == 0.0;
       mine = true;
     }
     if (w == 0) {
@@ -835,8 +849,8 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
       if (lane == 0) {
         ids[kept] = (int32_t)id;
         if (logp)
-          logp[kept] =
-              id >= 0 ? (float)((double)load_elem<TI>(d.z, id) - d.L) : __builtin_nanf("");
+          logp[kept] = id >= 0 ? (float)log_p(load_elem<TI>(d.z, id),
+                                                ws.row[target_row(a, b, kept)]) : __builtin_nanf("");
       }
     }
     __syncthreads();  // (the masses are used until here)
