@@ -364,7 +364,8 @@ int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, i
  *   largest magnitude in the block, the scale s is max(a / 448, 2^-126) in fp32,
  *   or the least power of two that is not below a / 448 (2^-127 at least), and
  *   q = x / s, divided in fp32 and rounded to the nearest e4m3 value, ties to
- *   even.  A block that holds a NaN or an infinity gets a NaN scale and values.
+ *   even; what rounds to zero keeps its sign.  A block that holds a NaN or an
+ *   infinity gets a NaN scale and values (0x7F).
  *     x [N, ldx] OPD_F32 or OPD_BF16; q [N, ldq] bytes, columns [H, ldq) are not
  *     written; scales [ceil(N / block_rows), nb].
  *   x and q are 16-byte aligned, ldx * element_size and ldq multiples of 16.

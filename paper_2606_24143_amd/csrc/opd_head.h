@@ -99,15 +99,16 @@ __device__ __forceinline__ Scale block_scale(uint32_t top) {
 // inverse, by their exact remainders: the first leaves less than a step, from which
 // the second gives the rounded quotient (Markstein, IBM J. Res. Dev. 34(1), 1990).
 // Five instructions for a division's eleven; where the remainders of such values
-// could underflow (s below 2^-60) it divides.
+// could underflow (s below 2^-60) it divides.  (The remainders are q s - f, which is
+// +0 where f is -0: taken from q it leaves -0.  f - q s, added, would leave +0.)
 constexpr float kSmallScale = 8.6736174e-19f;  // 2^-60
 template <bool E8>
 __device__ __forceinline__ float quotient(float f, const Scale& sc, bool small) {
   if constexpr (E8) return f * sc.inv;
   if (small) return f / sc.s;
   float q = f * sc.inv;
-  q = fmaf(fmaf(-q, sc.s, f), sc.inv, q);
-  return fmaf(fmaf(-q, sc.s, f), sc.inv, q);
+  q = fmaf(-fmaf(q, sc.s, -f), sc.inv, q);
+  return fmaf(-fmaf(q, sc.s, -f), sc.inv, q);
 }
 
 // The nearest e4m3 values of f / s, eight to a lane, packed.
