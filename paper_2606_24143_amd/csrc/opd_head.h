@@ -107,8 +107,8 @@ __device__ __forceinline__ float quotient(float f, const Scale& sc, bool small) 
   if constexpr (E8) return f * sc.inv;
   if (small) return f / sc.s;
   float q = f * sc.inv;
-  q = fmaf(-fmaf(q, sc.s, -f), sc.inv, q);
-  return fmaf(-fmaf(q, sc.s, -f), sc.inv, q);
+  q = fmaf(fmaf(q, sc.s, -f), -sc.inv, q);
+  return fmaf(fmaf(q, sc.s, -f), -sc.inv, q);
 }
 
 // The nearest e4m3 values of f / s, eight to a lane, packed.
