@@ -681,8 +681,6 @@ int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32
   a.ld = ld;
   a.ldd = draft_ld;
   a.D = D;
-  a.nvec = nvec_of(V, dtype);
-  a.tail = (int)(V - (a.nvec - 1) * elems_per_vec(dtype));
   a.ids = draft_ids;
   a.lens = draft_lens;
   a.u = uniforms;

@@ -97,8 +97,6 @@ struct VerifyArgs {
   const void* draft;      // [B D, ldd]; NULL: drafts that are certain
   int64_t B, V, ld, ldd;
   int D;
-  int64_t nvec;           // 4-element vectors per row covering [0, V)
-  int tail;               // valid elements in the last vector
   const int32_t* ids;     // [B, D]
   const int32_t* lens;    // [B] nullable
   const float* u;         // [B, D + 1]
@@ -107,7 +105,8 @@ struct VerifyArgs {
   int32_t* ids_out;       // [B, D + 1]
   float* logp;            // [B, D + 1] nullable
   void* ws;               // opd_verify_workspace_bytes (laid out by ver_ws)
-  int parts;              // of a row, each summed by one workgroup
+  int parts;              // of a row, each summed by one wavefront: the most it has, and the
+                          // stride of its records
   uint32_t part_groups;   // groups of 8 elements in a part
   int draw_parts;         // of the row that a sequence's last token is drawn from
   int nchunk, chunk_steps;  // its chunks, of 512 chunk_steps elements

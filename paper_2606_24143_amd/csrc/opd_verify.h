@@ -14,7 +14,7 @@
 //
 // k_verify_rows sums the rows, k_verify_draw draws.  Rows past a sequence's first
 // refusal have no part in the result, and they are an eighth to three quarters of
-// all rows.  So the positions are summed in rounds, a launch each (verify_round): a
+// all rows.  So the positions are summed in rounds, a launch each (launch_verify_t): a
 // round leaves out the sequences that the rounds before it ended.
 #pragma once
 
