@@ -569,8 +569,8 @@ struct DrawRow {
   const char* z;
   const char* y;     // kResidual
   double ps, qs;     // exp(-l) of both
-  const VerRow* far;  // the target's and the draft's where not direct (in LDS: rare, and
-                      // the registers are full)
+  const VerRow* far;  // the target's and the draft's, in LDS: read where not direct (rare,
+                      // and the registers are full) and for the drawn token's log-prob
   int64_t x;         // kWithout: the refused token
   int mass;
   bool direct;       // from exp(z) (as the rows were summed), else from exp(log p)
@@ -776,13 +776,11 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
       // (both rows summed as exp(z): no logit at or past kVerTop, and no tiny sum)
       d.direct = rt.m == 0.0 && rd.m == 0.0;
       d.far = c.far;
-      if (!d.direct) {  // (the same in every lane; the item before is done with c)
-        if (tid == 0) {
-          c.far[0] = rt;
-          c.far[1] = rd;
-        }
-        __syncthreads();
+      if (tid == 0) {  // (the item before is done with c)
+        c.far[0] = rt;
+        c.far[1] = rd;
       }
+      if (!d.direct) __syncthreads();  // (the same in every lane)
     }
     const bool draws = rt.l == rt.l && u >= 0.f && u < 1.f;
     if (parts > 1) {
@@ -839,7 +837,7 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
       // p(x) < q(x) leaves a residual; where rounding hides it the draw is from p
       if (S > 0.0 || d.mass == kTarget) break;
       d.mass = kTarget;
-      d.direct = ws.row[target_row(a, b, kept)].m == 0.0;
+      d.direct = c.far[0].m == 0.0;
       mine = true;
     }
     if (w == 0) {
@@ -849,8 +847,8 @@ __global__ void __launch_bounds__(kVerThreads, 4) k_verify_draw(VerifyArgs a) {
       if (lane == 0) {
         ids[kept] = (int32_t)id;
         if (logp)
-          logp[kept] = id >= 0 ? (float)log_p(load_elem<TI>(d.z, id),
-                                                ws.row[target_row(a, b, kept)]) : __builtin_nanf("");
+          logp[kept] = id >= 0 ? (float)log_p(load_elem<TI>(d.z, id), c.far[0])
+                               : __builtin_nanf("");
       }
     }
     __syncthreads();  // (the masses are used until here)
