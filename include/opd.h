@@ -374,10 +374,13 @@ int opd_score_actions(const void* logits, int32_t dtype, int64_t N, int64_t V, i
  *   sum_{h in block b} x[n, h] w[v, h], in fp32, rounded once to logits_dtype
  *   (OPD_F32 or OPD_BF16).  For fp32 logits products are exact; for bf16 ones
  *   the matrix cores cut each at 2^-13 of the largest of the 16 that they sum
- *   at once, far below the rounding.  (Two blocks' scales are multiplied first;
- *   their product should be finite in fp32.)  A NaN in a
- *   token's values or scales reaches its own row only, one in the weights its
- *   own vocabulary entries (a scale: those of its block).
+ *   at once, at most 2^-6 of a block's largest product in all.  Of hidden states
+ *   with a few channels far larger than the others that is 7e-5 of a logit, where
+ *   the rounding to bf16 is 1.7e-3; where larger products cancel it is more, and
+ *   such logits are better asked for in fp32.  (Two blocks' scales are multiplied
+ *   first; their product should be finite in fp32.)  A NaN in a token's values
+ *   or scales reaches its own row only, one in the weights its own vocabulary
+ *   entries (a scale: those of its block).
  *     x [N, ldx], x_scales [N, nb]; w [V, ldw], w_scales [ceil(V / 128), nb];
  *     logits [N, ld], as every call here reads them; columns [V, ld) are not
  *     written.

@@ -535,9 +535,12 @@ def head_logits(hidden: torch.Tensor, hidden_scales: torch.Tensor, weight: torch
                 stream=None) -> dict:
     """Logits of N tokens from their hidden states ([N, H] float8_e4m3fn, scales
     [N, ceil(H / 128)]) and an output head ([V, H] float8_e4m3fn, scales
-    [ceil(V / 128), ceil(H / 128)]), both as quantize_blocks gives them.  Returns
-    {"logits" [N, V]}, a view of an [N, ld] buffer (`out`, if given) as the other
-    calls take it."""
+    [ceil(V / 128), ceil(H / 128)]), both as quantize_blocks gives them.  Sums are
+    fp32; products are exact for dtype=torch.float32, while for bfloat16 logits the
+    matrix cores cut each at 2^-13 of the largest of the 16 summed with it (about
+    7e-5 of a logit, where rounding it to bfloat16 costs 1.7e-3; see opd_head_logits).
+    Returns {"logits" [N, V]}, a view of an [N, ld] buffer (`out`, if given) as the
+    other calls take it."""
     e4m3 = (torch.float8_e4m3fn,)
     for t, name in ((hidden, "hidden"), (weight, "weight")):
         _rowmajor(t, name)
