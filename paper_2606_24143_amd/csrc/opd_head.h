@@ -285,7 +285,10 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
 // far larger than the others, lie 1.6589e-3 of their norm from the exact logits, and
 // exact products rounded to bf16 1.6588e-3 (they differ in one logit of 80, by a
 // step).  It is not below that of fp32 ones, so these are made by 16-bit instructions
-// of exactly widened values, at half the rate.
+// of exactly widened values, at half the rate.  (bf16 logits from these as well, V =
+// 151,936, H = 4,096, fp32 scales, us: 1 token 116 / 117, 32 119 / 121, 64 135 / 150, 128
+// 179 / 235.  All take the 8-bit ones, so that a token's logits do not depend on how
+// many are asked for with it by more than the order of sums.)
 // 16 rows over 128 columns, of which a lane holds 32: as the instructions for TO take
 // them; and the product of two.
 template <class TO>
