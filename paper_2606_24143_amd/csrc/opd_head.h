@@ -803,10 +803,22 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_head_tile(HeadArgs a) {
 }
 
 // Up to 128 tokens, or so few logits that their tiles leave CUs idle, the rows are
-// streamed (for every 128 tokens again).  Streamed / tiled, us, fp32 scales: V = 151,936,
-// H = 4,096, 128 tokens 178 / 214; V = 32,000, H = 4,096, 256 73 / 141, 384 98 / 117, 512
-// 124 / 130 (e8m0 113 / 102), 1,024 229 / 153; V = 50,257, H = 2,048, 256 66 / 83, 384 85 / 80;
-// V = 8,000, H = 4,096, 512 39 / 64, 1,024 65 / 71.
+// streamed (for every 128 tokens again).  Streamed / tiled at H = 4,096, us:
+//                              bf16 logits,           fp32 logits,
+//   tokens x V                 fp32 scales  e8m0      fp32 scales
+//   512 x 8,000    (4.1 M)      39 / 61      33 / 50     58 / 119
+//   1,024 x 8,000  (8.2 M)      68 / 75      59 / 57    101 / 127
+//   256 x 32,000   (8.2 M)      69 / 140     64 / 104   104 / 229
+//   384 x 32,000   (12.3 M)    103 / 122     92 / 100   145 / 225
+//   256 x 50,257   (12.9 M)    123 / 142    111 / 110   172 / 227
+//   512 x 32,000   (16.4 M)    127 / 132    117 / 106   191 / 239
+//   2,048 x 8,000  (16.4 M)    123 / 78     113 / 61    181 / 135
+//   384 x 50,257   (19.3 M)    154 / 132    137 / 108   221 / 235
+//   136 x 151,936  (20.7 M)    305 / 204    293 / 177   419 / 345
+//   1,024 x 32,000 (32.8 M)    236 / 156    216 / 124   352 / 260
+// and the same to either side at H = 512, 2,048 and 8,192.  One bound for all loses up to
+// a seventh for bf16 logits (e8m0, 1,024 x 8,000 at H = 8,192), and for fp32 ones up to a third
+// where 14 to 20 million are of few tokens (512 x 32,000 at H = 512: 36 / 49).
 constexpr int64_t kFewLogits = 14000000;
 template <class TO, bool E8>
 hipError_t launch_head_t(HeadArgs a, hipStream_t stream) {
