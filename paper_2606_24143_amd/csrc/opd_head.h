@@ -530,6 +530,10 @@ hipError_t launch_stream(const HeadArgs& a, hipStream_t stream) {
 // 32,000 x 2,048 - / 13.4 / 15.1; 32 tokens, 4,000 x 4,096 10.5 / 11.6 / 19.6;
 // 16,000 x 2,048 9.1 / 9.1 / 12.0; 32,000 x 4,096 34.2 / 30.5 / 28.4; 64 tokens, 4,000 18.8 /
 // 17.5 / 23.5; 16,000 x 2,048 14.3 / 11.5 / 14.4; 64,000 x 4,096 95.0 / 69.8 / 61.3.
+// Both scales and both types of logits agree to a tenth, and so do widths: 4 / 8 waves, 32
+// tokens x 128,256 at H = 2,048 57 / 58, 5,120 135 / 123, 7,168 179 / 164, 16,384 441 / 358;
+// not 8,192, 203 / 265 (32,000 entries 53 / 71), for a reason that is not known.  Between the
+// bounds up to a quarter is lost (32 tokens x 12,000 x 4,096, fp32 logits 19.6 / 15.8 / 21.3).
 template <class TO, bool E8>
 hipError_t launch_few(const HeadArgs& a, hipStream_t stream) {
   const bool narrow = a.V < 12288, wide = a.V >= 24576;
