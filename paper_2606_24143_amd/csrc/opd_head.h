@@ -564,10 +564,10 @@ hipError_t launch_few(const HeadArgs& a, hipStream_t stream) {
 // consecutive entries of one token, and its scales one per 16 tokens; the head's
 // scale is the wave's.  e8m0 scales go to the instructions; fp32 ones multiply
 // each block's product as it is added to the sum, which costs the vector unit
-// half the matrix cores' time.  At that size e8m0 scales take 2.15-2.29 ms (2.3
-// PFLOP/s; the matrix cores are busy for 61% of it), fp32 ones 2.63-2.79 (50%): what is
+// half the matrix cores' time.  At that size e8m0 scales take 2.11-2.36 ms (2.3
+// PFLOP/s; the matrix cores are busy for 61% of it), fp32 ones 2.55-2.74 (50%): what is
 // left is the barrier of a stage, at which no other workgroup fills the CU.  fp32
-// logits: 4.7 ms; 1,111 tokens, V = 50,257, H = 2,000 270-285 us (0.8 PFLOP/s at the
+// logits: 4.7 ms; 1,111 tokens, V = 50,257, H = 2,000 252-277 us (0.8 PFLOP/s at the
 // 16-bit instructions' rate; 985 tiles on 256 CUs are four rounds).
 //
 // LDS rows are 128 bytes, 16-byte pieces at piece ^ key(row): with the keys below

@@ -392,9 +392,9 @@ __device__ __forceinline__ RoundRows round_rows(const VerifyArgs& a, const VerWs
 // those of rows that are not needed are left out.  Who ends a position's last part
 // makes its test.
 //
-// bf16 rows are bound by HBM (294 MB, the first position of 512 sequences at V =
-// 151,936: 62 us, of which reading 53, 5.5 TB/s), fp32 ones by the exponentials in
-// double precision (103 MB in 38 us).  Besides, a launch takes about 12 us: the table 4,
+// bf16 rows are bound by HBM (295 MB, the first position of 512 sequences at V =
+// 151,936: 64 us, of which reading 53, 5.5 TB/s), fp32 ones by the exponentials in
+// double precision (154 MB, the first three of 256 at V = 50,257: 39 us).  Besides, a launch takes about 12 us: the table 4,
 // counting 1, the first loads, and at its end the counters and the tests 3 each.
 constexpr int kListed = 2048;
 template <class TI, bool TABLE>
@@ -723,8 +723,10 @@ __device__ __forceinline__ void chunk_masses(const VerifyArgs& a, const DrawRow<
 
 // A sequence's tokens: the kept ones, then the draw.  The row that it is drawn from
 // (for a residual, the draft's too) is read again, as its masses need both rows'
-// sums: 250 MB in 66-82 us at 512 sequences of 8 drafts, V = 151,936; 24 us at 64 of 5,
-// of which the table is 4 and the last workgroup of a sequence 6.  Item k: part k % draw_parts of
+// sums: 237 MB in 65 us at 512 sequences of 8 drafts, V = 151,936 (3.6 TB/s: a
+// workgroup to a sequence, whose loads of a step do not overlap the sums of the step
+// before); 23 us at 64 of 5, of which the table is 4 and the last workgroup of a
+// sequence 6.  Item k: part k % draw_parts of
 // the row that sequence k / draw_parts is drawn from; whoever ends a sequence's
 // last part draws.
 template <class TI, bool TABLE>
