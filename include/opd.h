@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define OPD_VERSION 6
+#define OPD_VERSION 7
 /* Largest cached support size k, and largest sample count M. */
 #define OPD_K_MAX 256
 
@@ -461,6 +461,127 @@ int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32
 
 /* Workspace bytes of opd_verify_drafts (0 for invalid arguments). */
 size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype);
+
+/*
+ * Token embeddings: rows of a vocabulary-sized table (often the output head's
+ * too) for the tokens that Stages 1 to 3 run the model on, and the gradient that the
+ * learner's update gives the table.
+ *
+ * opd_embed_tokens: out[n, :] = scale * table[ids[n], :], in fp32, rounded once.
+ * opd_embed_grads: dtable[v, :] = scale * sum of dy[n, :] over the tokens n with
+ *   ids[n] == v, summed in fp32 in the order of the tokens (an entry of more than 64
+ *   tokens: in parts of 64 places of the sorted batch, then over the parts).  Every row of
+ *   dtable is written, zeros among them; with accumulate = 1 the sums are added to what
+ *   it holds, and the rows of entries without a token stay as they are, unread.
+ *     table [V, ld], dtable [V, ldo], dy [N, ldy], out [N, ldo]: OPD_F32 or OPD_BF16, in
+ *     any combination, 16-byte aligned rows; columns past H are not written.
+ *     ids [N] int32.  -1 (what opd_verify_drafts writes past a sequence's last token)
+ *     gives a row of zeros and has no part in the gradient; any other id outside
+ *     [0, V) gives a row of NaN and has no part in the gradient.
+ *     workspace: opd_embed_workspace_bytes(N, V, H) bytes (0 for few tokens: may be
+ *     NULL), 16-byte aligned, of any content; calls (and captured graphs) that may
+ *     overlap need one each.
+ * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N, V >= 2^31, V < 1, H outside [1, 2^22], a
+ * row stride below H), OPD_ERR_PARAM (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL,
+ * OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0 looks nothing up; the gradient is then zeros.
+ */
+int opd_embed_tokens(const void* table, int32_t dtype, int64_t V, int64_t H, int64_t ld,
+                     const int32_t* ids, int64_t N, float scale, void* out, int32_t out_dtype,
+                     int64_t ldo, void* stream);
+int opd_embed_grads(const void* dy, int32_t dtype, int64_t N, int64_t H, int64_t ldy,
+                    const int32_t* ids, int64_t V, float scale, void* dtable, int32_t out_dtype,
+                    int64_t ldo, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                    void* stream);
+size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that they share:
+ * the output head of opd_head_logits, whose rows of logits they change for each
+ * student or teacher, or any other.  Token n has adapter g = adapter_ids[n]:
+ *   t = x[n] a_g^T  (r numbers),  out[n] = y[n] + s_g t b_g
+ * and the gradients of a loss, from dy = dloss/dout (of logits: what opd_loss_fwd_bwd
+ * returns):
+ *   u = dy[n] b_g^T,  dx[n] = dx_shared[n] + s_g u a_g,
+ *   da_g = s_g sum_n u_n^T x[n],  db_g = s_g sum_n t_n^T dy[n]   (over its tokens)
+ *     x [N, ldx], a [G, r, lda], b [G, r, ldb]: dtype.  (Both matrices are held as r
+ *     rows of the long axis.)  y, out [N, ..], dy [N, lddy]: y_dtype, which is dtype or
+ *     OPD_F32.  out may be y.  dx_shared (the shared projection's gradient; nullable: 0)
+ *     and dx (nullable: not wanted) [N, ..]: dtype; they may be one.  da [G, r, ldda],
+ *     db [G, r, lddb]: OPD_F32; adapters without a token get zeros.
+ *     scales [G] fp32, nullable (1).
+ *     adapter_ids [N] int32: -1 for a token without an adapter (out is y, dx is dx_shared);
+ *     any other id outside [0, G) gives a row of NaN in out and dx, and no part in da and db.
+ *     low_out [N, r] fp32, nullable: t, which opd_adapter_grads takes as low (nullable: it
+ *     makes t again) for the same x and a.  Rows of tokens without an adapter are 0.
+ *     workspace: opd_adapter_workspace_bytes(...) bytes, 16-byte aligned, of any
+ *     content; calls (and captured graphs) that may overlap need one each.
+ * Sums are fp32, each result is rounded once.  bf16 operands are multiplied exactly; t
+ * and u enter the second product to 2^-17 of themselves where its result is bf16, to
+ * 2^-25 where it is fp32.  A NaN or an infinity in a token's x (dy) or in its adapter reaches
+ * its own row, and its adapter's da and db; no other's.
+ * All rows are 16-byte aligned; what lies past a row's end is neither read nor written.
+ * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N > 2^24, H or O outside [1, 2^22], a row stride
+ * below its row's length, strides of in-place rows that differ, or a call whose launches
+ * would pass 2^32 work-items), OPD_ERR_SUPPORT (G outside [1, OPD_ADAPTERS_MAX], r outside
+ * [1, OPD_RANK_MAX]), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0
+ * adds nothing; the gradients are then zeros.
+ */
+#define OPD_ADAPTERS_MAX 1000
+#define OPD_RANK_MAX 128
+int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x, int32_t dtype,
+                     int64_t ldx, const void* a, int64_t lda, const void* b, int64_t ldb,
+                     const float* scales, const int32_t* adapter_ids, int64_t N, int64_t H,
+                     int64_t O, int32_t G, int32_t r, void* out, int64_t ldo, float* low_out,
+                     void* workspace, size_t workspace_bytes, void* stream);
+int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void* x, int32_t dtype,
+                      int64_t ldx, const void* a, int64_t lda, const void* b, int64_t ldb,
+                      const float* scales, const int32_t* adapter_ids, int64_t N, int64_t H,
+                      int64_t O, int32_t G, int32_t r, const float* low, const void* dx_shared,
+                      int64_t ldds, void* dx, int64_t lddx, float* da, int64_t ldda, float* db,
+                      int64_t lddb, void* workspace, size_t workspace_bytes, void* stream);
+size_t opd_adapter_workspace_bytes(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r,
+                                   int32_t dtype, int32_t y_dtype, int32_t backward);
+
+/*
+ * Beam search beside the draws: the continuations that a group of W beams goes on with,
+ * and the beams' states in their new order.
+ *
+ * opd_beam_select: rows b W .. b W + W - 1 of the logits are group b's beams, with
+ *   scores [B, W].  Candidate (w, v) has score scores[b, w] + log softmax(row)[v]; the k
+ *   largest are returned in descending order, ties to the lower beam, then the lower token.
+ *   Scores are made and compared in double precision from fp32 logarithms' sums
+ *   good to about 1e-8, so the order is that of exact arithmetic unless two beams' scores
+ *   differ by about as little.
+ *     finished [B, W] uint8, nullable: a finished beam (not 0) is one candidate, with its
+ *     own score and id -1; its row is not read.  A beam of score -inf (one that does not
+ *     exist yet) and a row without a finite logit have no candidates (a masked logit, -inf,
+ *     is none either), and a beam of score -inf is not read.
+ *     out_scores, parents, ids [B, k]: the scores in fp32, the beams [0, W), the tokens.
+ *     Where a group has fewer candidates, the rest get score -inf, parent -1 and id -1.
+ *     A group with a score that is NaN or +inf, or a row (that is read) with a NaN or a +inf
+ *     logit, gets NaN, -1 and -1 throughout.
+ *     workspace: opd_beam_workspace_bytes(B, W, V, dtype) bytes, 16-byte aligned, of any
+ *     content; calls (and captured graphs) that may overlap need one each.
+ * opd_reorder_beams: state j of group b becomes a copy of the group's state
+ *   parents[b, j], for j < k; one whose parent is outside [0, W) becomes zeros.  A state is
+ *   `outer` slices of inner_bytes bytes, outer_stride bytes apart; states lie `stride`
+ *   bytes apart, b W + w of them before the state of beam w of group b (in out: b k + j).
+ *   Any element type.  out may be states (k == W, the same strides): the states
+ *   are then moved in place, and those that are their own parent stay.  It may not
+ *   overlap them otherwise.
+ * Errors: OPD_ERR_DTYPE, OPD_ERR_SUPPORT (W or k outside [1, OPD_BEAM_MAX]), OPD_ERR_SHAPE,
+ * OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  B == 0 is a no-op returning
+ * OPD_OK.
+ */
+#define OPD_BEAM_MAX 64
+int opd_beam_select(const void* logits, int32_t dtype, int64_t B, int32_t W, int64_t V, int64_t ld,
+                    const float* scores, const uint8_t* finished, int32_t k, float* out_scores,
+                    int32_t* parents, int32_t* ids, void* workspace, size_t workspace_bytes,
+                    void* stream);
+size_t opd_beam_workspace_bytes(int64_t B, int32_t W, int64_t V, int32_t dtype);
+int opd_reorder_beams(const void* states, int64_t B, int32_t W, int64_t outer, int64_t inner_bytes,
+                      int64_t stride, int64_t outer_stride, const int32_t* parents, int32_t k,
+                      void* out, int64_t out_stride, int64_t out_outer_stride, void* stream);
 
 /*
  * Diagnostics of the Monte-Carlo estimator: the importance-ratio tail that

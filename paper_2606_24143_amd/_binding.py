@@ -40,7 +40,10 @@ EXPORTS = ("opd_loss_fwd_bwd", "opd_loss_fwd_bwd_noalloc", "opd_noalloc_scratch_
            "opd_workspace_bytes", "opd_validate_cache", "opd_sample_actions",
            "opd_topk_support", "opd_score_actions", "opd_mc_diag_workspace_bytes",
            "opd_mc_diagnostics", "opd_quantize_blocks", "opd_head_logits", "opd_verify_drafts",
-           "opd_verify_workspace_bytes", "opd_status_string", "opd_version")
+           "opd_verify_workspace_bytes", "opd_embed_tokens", "opd_embed_grads",
+           "opd_embed_workspace_bytes", "opd_add_adapters", "opd_adapter_grads",
+           "opd_adapter_workspace_bytes", "opd_beam_select", "opd_beam_workspace_bytes",
+           "opd_reorder_beams", "opd_status_string", "opd_version")
 
 
 class OpdError(RuntimeError):
@@ -114,6 +117,29 @@ def lib():
         L.opd_verify_drafts.argtypes = [P, P, i32, i64, i32, i64, i64, i64, P, P, P, P, P, P, P, P,
                                         ctypes.c_size_t, P]
         L.opd_verify_drafts.restype = ctypes.c_int
+        f32, size = ctypes.c_float, ctypes.c_size_t
+        L.opd_embed_tokens.argtypes = [P, i32, i64, i64, i64, P, i64, f32, P, i32, i64, P]
+        L.opd_embed_tokens.restype = ctypes.c_int
+        L.opd_embed_grads.argtypes = [P, i32, i64, i64, i64, P, i64, f32, P, i32, i64, i32, P,
+                                      size, P]
+        L.opd_embed_grads.restype = ctypes.c_int
+        L.opd_embed_workspace_bytes.argtypes = [i64, i64, i64]
+        L.opd_embed_workspace_bytes.restype = size
+        L.opd_add_adapters.argtypes = [P, i32, i64, P, i32, i64, P, i64, P, i64, P, P, i64, i64,
+                                       i64, i32, i32, P, i64, P, P, size, P]
+        L.opd_add_adapters.restype = ctypes.c_int
+        L.opd_adapter_grads.argtypes = [P, i32, i64, P, i32, i64, P, i64, P, i64, P, P, i64, i64,
+                                        i64, i32, i32, P, P, i64, P, i64, P, i64, P, i64, P, size,
+                                        P]
+        L.opd_adapter_grads.restype = ctypes.c_int
+        L.opd_adapter_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32]
+        L.opd_adapter_workspace_bytes.restype = size
+        L.opd_beam_select.argtypes = [P, i32, i64, i32, i64, i64, P, P, i32, P, P, P, P, size, P]
+        L.opd_beam_select.restype = ctypes.c_int
+        L.opd_beam_workspace_bytes.argtypes = [i64, i32, i64, i32]
+        L.opd_beam_workspace_bytes.restype = size
+        L.opd_reorder_beams.argtypes = [P, i64, i32, i64, i64, i64, i64, P, i32, P, i64, i64, P]
+        L.opd_reorder_beams.restype = ctypes.c_int
         L.opd_status_string.argtypes = [ctypes.c_int]
         L.opd_status_string.restype = ctypes.c_char_p
         L.opd_version.restype = ctypes.c_int
@@ -631,6 +657,357 @@ def verify_drafts(target_logits: torch.Tensor, draft_ids: torch.Tensor, uniforms
     if logp is not None:
         out["logp"] = logp
     return out
+
+
+# ---------------------------------------------------------------- token embeddings
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _need_float_rows(t, name: str) -> int:
+    """t: [n, m] float32 or bfloat16 with 16-byte aligned rows; its row stride."""
+    _rowmajor(t, name)
+    if t.dtype not in _FLOATS:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    return _need_stride(t, name)
+
+
+def _need_out(out, name: str, dtype, N: int, M: int, device) -> int:
+    """out: [N, M] of `dtype` with 16-byte aligned rows; its row stride."""
+    if not isinstance(out, torch.Tensor):
+        raise ValueError("%s must be a torch tensor" % name)
+    _rowmajor(out, name)
+    if out.dtype != dtype or tuple(out.shape) != (N, M) or out.device != device:
+        raise ValueError("%s must be [%d, %d] %s on %s, got %s %s on %s" %
+                         (name, N, M, dtype, device, tuple(out.shape), out.dtype, out.device))
+    return _need_stride(out, name)
+
+
+def _padded(M: int, dtype) -> int:
+    """M elements, up to a multiple of 16 bytes."""
+    each = 4 if dtype == torch.float32 else 8
+    return _blocks(M, each) * each
+
+
+def _need_workspace(workspace, dev):
+    if workspace is not None:
+        _need(workspace, "workspace", (torch.uint8,), (workspace.numel(),), dev)
+
+
+def _workspace(workspace, nbytes: int, dev):
+    if workspace is None and nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    return workspace, 0 if workspace is None else workspace.numel()
+
+
+def embed_tokens(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, dtype=None,
+                 out=None, stream=None) -> dict:
+    """scale * table[ids] ([V, H] float32 or bfloat16 by [N] int32) in `dtype`
+    (the table's, unless given).  An id of -1 gives a row of zeros, any other outside [0, V) a
+    row of NaN.  Returns {"hidden" [N, H]}, a view of rows a multiple of 16 bytes
+    apart (or `out`)."""
+    ld = _need_float_rows(table, "table")
+    V, H = table.shape
+    dev = table.device
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids must be a contiguous [N] int32 tensor")
+    N = ids.shape[0]
+    _need(ids, "ids", (torch.int32,), (N,), dev)
+    dtype = table.dtype if dtype is None else dtype
+    if dtype not in _FLOATS:
+        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+    if out is not None:
+        ldo = _need_out(out, "out", dtype, N, H, dev)
+    _need_gpu(table, "table")
+    with _On(dev, stream) as s:
+        if out is None:
+            ldo = _padded(H, dtype)
+            out = torch.empty((N, ldo), dtype=dtype, device=dev)[:, :H]
+        rc = lib().opd_embed_tokens(_at(table), _dt(table), V, H, ld, _at(ids), N, scale, _at(out),
+                                    _dt(out), ldo, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_embed_tokens")
+    return {"hidden": out}
+
+
+def embed_grads(grad: torch.Tensor, ids: torch.Tensor, V: int, *, scale: float = 1.0,
+                dtype=torch.float32, out=None, accumulate: bool = False, workspace=None,
+                stream=None) -> dict:
+    """The table's gradient from that of embed_tokens' rows ([N, H] float32 or
+    bfloat16): scale times the sum over each entry's tokens, in their order.  Every row is
+    written, unless accumulate=True, which adds to `out` and leaves the rows of entries without
+    a token alone.  Ids outside [0, V) have no part.  Returns {"dtable" [V, H]} in
+    `dtype`."""
+    ldy = _need_float_rows(grad, "grad")
+    N, H = grad.shape
+    dev = grad.device
+    _need(ids, "ids", (torch.int32,), (N,), dev)
+    if not 1 <= V < 2 ** 31:
+        raise ValueError("V must be in [1, 2^31), got %d" % V)
+    if dtype not in _FLOATS:
+        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+    if out is not None:
+        ldo = _need_out(out, "out", dtype, V, H, dev)
+    elif accumulate:
+        raise ValueError("accumulate=True needs the gradient to add to (out)")
+    _need_workspace(workspace, dev)
+    _need_gpu(grad, "grad")
+    with _On(dev, stream) as s:
+        if out is None:
+            ldo = _padded(H, dtype)
+            out = torch.empty((V, ldo), dtype=dtype, device=dev)[:, :H]
+        ws, nbytes = _workspace(workspace, int(lib().opd_embed_workspace_bytes(N, V, H)), dev)
+        rc = lib().opd_embed_grads(_at(grad), _dt(grad), N, H, ldy, _at(ids), V, scale, _at(out),
+                                   _dt(out), ldo, 1 if accumulate else 0, _at(ws), nbytes, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_embed_grads")
+    return {"dtable": out}
+
+
+# ---------------------------------------------------------------- low-rank adapters
+
+def _need_adapters(w, name: str, x: torch.Tensor) -> int:
+    """w: [G, r, M] of x's type whose rows lie one row stride apart throughout; that."""
+    if not isinstance(w, torch.Tensor) or w.dim() != 3:
+        raise ValueError("%s must be a [G, r, M] tensor" % name)
+    if w.dtype != x.dtype or w.device != x.device:
+        raise ValueError("%s must be %s on %s, got %s on %s" %
+                         (name, x.dtype, x.device, w.dtype, w.device))
+    G, r, M = w.shape
+    each = 16 // w.element_size()
+    # (the stride of an axis of one element says nothing)
+    ld = w.stride(1) if r > 1 else w.stride(0) if G > 1 else _blocks(M, each) * each
+    if (M > 1 and w.stride(2) != 1) or (r > 1 and G > 1 and w.stride(0) != r * ld) or ld < M or \
+            ld % each != 0 or w.data_ptr() % 16 != 0:
+        raise ValueError("%s must have 16-byte aligned rows, one row stride apart" % name)
+    return ld
+
+
+def _adapter_call(x, a, b, adapter_ids, scales, wide, name: str):
+    """The checks that the calls on adapters share; wide: y or dy."""
+    ldx = _need_float_rows(x, "x")
+    N, H = x.shape
+    dev = x.device
+    lda, ldb = _need_adapters(a, "a", x), _need_adapters(b, "b", x)
+    G, r, O = b.shape
+    if tuple(a.shape) != (G, r, H):
+        raise ValueError("a must have shape %s, got %s" % ((G, r, H), tuple(a.shape)))
+    ldw = _need_float_rows(wide, name)
+    if tuple(wide.shape) != (N, O) or wide.device != dev:
+        raise ValueError("%s must have shape %s on %s, got %s on %s" %
+                         (name, (N, O), dev, tuple(wide.shape), wide.device))
+    if wide.dtype not in (x.dtype, torch.float32):
+        raise ValueError("%s must be float32 or %s, got %s" % (name, x.dtype, wide.dtype))
+    _need(adapter_ids, "adapter_ids", (torch.int32,), (N,), dev)
+    if scales is not None:
+        _need(scales, "scales", (torch.float32,), (G,), dev)
+    return N, H, O, G, r, ldx, lda, ldb, ldw, dev
+
+
+def add_adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                 adapter_ids: torch.Tensor, *, scales=None, out=None, want_low: bool = False,
+                 workspace=None, stream=None) -> dict:
+    """y + scales[g] * (x @ a[g].T) @ b[g] for N tokens of adapters g = adapter_ids
+    ([N] int32; -1: none) beside a shared projection y [N, O] (head_logits' rows of
+    logits, or any other).  x [N, H], a [G, r, H] and b [G, r, O] are float32 or bfloat16, y
+    that or float32.  Returns {"out" [N, O]} (`out`, if given, which may be y), and "low"
+    [N, r] float32, x @ a[g].T, for adapter_grads when want_low."""
+    N, H, O, G, r, ldx, lda, ldb, ldy, dev = _adapter_call(x, a, b, adapter_ids, scales, y, "y")
+    if out is not None:
+        ldo = _need_out(out, "out", y.dtype, N, O, dev)
+        if out is not y and _overlap(out, y) and (out.data_ptr() != y.data_ptr() or ldo != ldy):
+            raise ValueError("out must be y or not overlap it")
+    _need_workspace(workspace, dev)
+    _need_gpu(x, "x")
+    dt, ydt = _dt(x), _dt(y)
+    with _On(dev, stream) as s:
+        if out is None:
+            ldo = _padded(O, y.dtype)
+            out = torch.empty((N, ldo), dtype=y.dtype, device=dev)[:, :O]
+        low = torch.empty((N, r), dtype=torch.float32, device=dev) if want_low else None
+        ws, nbytes = _workspace(workspace, int(lib().opd_adapter_workspace_bytes(
+            N, H, O, G, r, dt, ydt, 0)), dev)
+        rc = lib().opd_add_adapters(_at(y), ydt, ldy, _at(x), dt, ldx, _at(a), lda, _at(b), ldb,
+                                    _at(scales), _at(adapter_ids), N, H, O, G, r, _at(out), ldo,
+                                    _at(low), _at(ws), nbytes, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_add_adapters")
+    return {"out": out} if low is None else {"out": out, "low": low}
+
+
+def adapter_grads(dy: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                  adapter_ids: torch.Tensor, *, scales=None, low=None, dx=None,
+                  want_dx: bool = True, workspace=None, stream=None) -> dict:
+    """Gradients of add_adapters from that of its result, dy [N, O] (of logits:
+    loss_fwd_bwd's "dlogits").  low: what add_adapters returned with want_low for the same x
+    and a; dx [N, H]: the shared projection's gradient, which the adapters' is added to.
+    Returns {"da" [G, r, H], "db" [G, r, O] (float32; zeros for adapters without a token),
+    "dx" [N, H] in x's type unless want_dx=False}."""
+    N, H, O, G, r, ldx, lda, ldb, lddy, dev = _adapter_call(x, a, b, adapter_ids, scales, dy, "dy")
+    if low is not None:
+        _need(low, "low", (torch.float32,), (N, r), dev)
+    ldds = 0
+    if dx is not None:
+        if not want_dx:
+            raise ValueError("dx is given but not wanted")
+        ldds = _need_out(dx, "dx", x.dtype, N, H, dev)
+    _need_workspace(workspace, dev)
+    _need_gpu(x, "x")
+    dt, ydt = _dt(x), _dt(dy)
+    f32 = torch.float32
+    with _On(dev, stream) as s:
+        ldda, lddb, lddx = _padded(H, f32), _padded(O, f32), _padded(H, x.dtype)
+        da = torch.empty((G, r, ldda), dtype=f32, device=dev)
+        db = torch.empty((G, r, lddb), dtype=f32, device=dev)
+        to = torch.empty((N, lddx), dtype=x.dtype, device=dev) if want_dx else None
+        ws, nbytes = _workspace(workspace, int(lib().opd_adapter_workspace_bytes(
+            N, H, O, G, r, dt, ydt, 1)), dev)
+        rc = lib().opd_adapter_grads(_at(dy), ydt, lddy, _at(x), dt, ldx, _at(a), lda, _at(b), ldb,
+                                     _at(scales), _at(adapter_ids), N, H, O, G, r, _at(low),
+                                     _at(dx), ldds, _at(to), lddx, _at(da), ldda, _at(db), lddb,
+                                     _at(ws), nbytes, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_adapter_grads")
+    res = {"da": da[:, :, :H], "db": db[:, :, :O]}
+    if want_dx:
+        res["dx"] = to[:, :H]
+    return res
+
+
+# ---------------------------------------------------------------- beams
+
+BEAM_MAX = 64
+
+
+def _span(t: torch.Tensor):
+    """[first, last) byte of what a tensor's elements cover."""
+    if t.numel() == 0:
+        return t.data_ptr(), t.data_ptr()
+    last = sum((n - 1) * st for n, st in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+
+
+def _overlap(t: torch.Tensor, u: torch.Tensor) -> bool:
+    (a, b), (c, d) = _span(t), _span(u)
+    return t.device == u.device and a < d and c < b
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, *, k: Optional[int] = None,
+                finished=None, workspace=None, stream=None) -> dict:
+    """The k (W, unless given) best continuations of each group of W beams: logits
+    [B * W, V], scores [B, W] float32, finished [B, W] (or None): beams that have ended
+    and stand as they are.  Returns {"scores" [B, k] float32, "parents" [B, k] int32 (beams),
+    "ids" [B, k] int32 (tokens; -1 for a beam that has ended, and, with parent -1 and score
+    -inf, where there are no more)}, in descending order, ties to the lower beam, then
+    the lower token; see opd_beam_select."""
+    R, V, ld, dt = _row_call(logits)
+    dev = logits.device
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2:
+        raise ValueError("scores must be a contiguous [B, W] float32 tensor")
+    B, W = scores.shape
+    if not 1 <= W <= BEAM_MAX or R != B * W:
+        raise ValueError("logits must have B * W rows, W up to %d, got %d for B = %d, W = %d" %
+                         (BEAM_MAX, R, B, W))
+    k = W if k is None else k
+    if not 1 <= k <= BEAM_MAX:
+        raise ValueError("k must be in [1, %d], got %d" % (BEAM_MAX, k))
+    _need(scores, "scores", (torch.float32,), (B, W), dev)
+    if finished is not None:
+        _need(finished, "finished", _MASK_DTYPES, (B, W), dev)
+    _need_workspace(workspace, dev)
+    if R == 1:
+        ld = _padded(V, logits.dtype)
+    _need_gpu(logits, "logits")
+    with _On(dev, stream) as s:
+        res = {"scores": torch.empty((B, k), dtype=torch.float32, device=dev),
+               "parents": torch.empty((B, k), dtype=torch.int32, device=dev),
+               "ids": torch.empty((B, k), dtype=torch.int32, device=dev)}
+        ws, nbytes = _workspace(workspace, int(lib().opd_beam_workspace_bytes(B, W, V, dt)), dev)
+        rc = lib().opd_beam_select(_at(logits), dt, B, W, V, ld, _at(scores), _at(finished), k,
+                                   _at(res["scores"]), _at(res["parents"]), _at(res["ids"]),
+                                   _at(ws), nbytes, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_beam_select")
+    return res
+
+
+def _slices(t: torch.Tensor, name: str):
+    """(outer, inner bytes, stride, outer stride) of the states along t's first axis:
+    each `outer` slices of contiguous bytes, evenly apart."""
+    size = t.element_size()
+    inner, axes = 1, [(n, st) for n, st in zip(t.shape[1:], t.stride()[1:]) if n != 1]
+    while axes and axes[-1][1] == inner:
+        inner *= axes.pop()[0]
+    outer, apart = 1, inner
+    if axes:
+        outer, apart = axes.pop()
+        for n, st in reversed(axes):
+            if st != outer * apart:
+                raise ValueError("%s must hold states of evenly spaced, contiguous slices" % name)
+            outer *= n
+    if min([apart] + [st for st in t.stride()]) < 0 or (outer > 1 and apart < inner) or \
+            (t.shape[0] > 1 and t.stride(0) < (outer - 1) * apart + inner):
+        raise ValueError("%s must hold states that do not overlap" % name)
+    return outer, inner * size, t.stride(0) * size, apart * size
+
+
+def reorder_beams(states: torch.Tensor, parents: torch.Tensor, *, out=None, stream=None) -> dict:
+    """The beams' states in the order that beam_select returned: states [B * W, ...] of
+    any type, parents [B, k] int32 in [0, W) (zeros for any other).  out: another tensor
+    [B * k, ...], or `states` itself (k == W): moved in place.  A state may be strided (a
+    cache cut at its length) if its contiguous slices lie evenly apart.  Returns {"states"
+    [B * k, ...]}."""
+    if not isinstance(states, torch.Tensor) or states.dim() < 1:
+        raise ValueError("states must be a [B * W, ...] tensor")
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 2:
+        raise ValueError("parents must be a contiguous [B, k] int32 tensor")
+    B, k = parents.shape
+    dev = states.device
+    _need(parents, "parents", (torch.int32,), (B, k), dev)
+    if not 1 <= k <= BEAM_MAX:
+        raise ValueError("k must be in [1, %d], got %d" % (BEAM_MAX, k))
+    if B and (states.shape[0] % B != 0 or not 1 <= states.shape[0] // B <= BEAM_MAX):
+        raise ValueError("states must hold B * W states, W up to %d, got %d for B = %d" %
+                         (BEAM_MAX, states.shape[0], B))
+    W = states.shape[0] // B if B else k
+    outer, inner, stride, apart = _slices(states, "states")
+    shape = (B * k,) + tuple(states.shape[1:])
+    if out is not None:
+        if not isinstance(out, torch.Tensor) or out.dtype != states.dtype or \
+                tuple(out.shape) != shape or out.device != dev:
+            raise ValueError("out must be %s %s on %s" % (shape, states.dtype, dev))
+        to_outer, to_inner, to_stride, to_apart = _slices(out, "out")
+        if _overlap(out, states) and (out.data_ptr() != states.data_ptr() or k != W or
+                                      out.stride() != states.stride()):
+            raise ValueError("out must be states, with k == W, or not overlap it")
+    _need_gpu(states, "states")
+    with _On(dev, stream) as s:
+        if out is None:
+            # (rows a multiple of 16 bytes apart)
+            n = states[0].numel() if B else 0
+            pad = _blocks(max(n, 1) * states.element_size(), 16) * 16
+            buf = torch.empty((B * k, pad), dtype=torch.uint8, device=dev).view(states.dtype)
+            out = buf[:, :n].unflatten(1, shape[1:]) if len(shape) > 1 else buf[:, 0]
+            to_outer, to_inner, to_stride, to_apart = _slices(out, "out")
+        if to_inner != inner and B:
+            # slices of both: the shorter ones
+            outer, inner, apart, to_apart = _common(outer, inner, apart, to_outer, to_inner,
+                                                    to_apart)
+        rc = lib().opd_reorder_beams(_at(states), B, W, outer, inner, stride, apart, _at(parents),
+                                     k, _at(out), to_stride, to_apart, s)
+    if rc != 0:
+        raise OpdError(rc, "opd_reorder_beams")
+    return {"states": out}
+
+
+def _common(outer, inner, apart, to_outer, to_inner, to_apart):
+    """Slices of one length for two layouts of a state, one of which is contiguous
+    where the other is cut."""
+    if inner < to_inner and to_outer == 1:
+        return outer, inner, apart, inner
+    if to_inner < inner and outer == 1:
+        return to_outer, to_inner, to_inner, to_apart
+    raise ValueError("out must have states' slices, or contiguous states")
 
 
 # ---------------------------------------------------------------- MC diagnostics

@@ -6,6 +6,7 @@
 
 #include "../../include/opd.h"
 #include "opd_internal.h"
+#include "opd_model.h"
 
 namespace {
 
@@ -321,6 +322,144 @@ VerifyPlan verify_plan(int64_t B, int32_t D, int64_t V, int32_t dtype, bool draf
   p.ws_bytes = rows * 16 * (1 + (size_t)p.parts) +
                (p.draw_parts > 1 ? (size_t)B * p.nchunk * 8 : 0) +
                (size_t)B * (2 * (size_t)(D + 1) + 2) * 4;
+  return p;
+}
+
+// Arguments shared by the calls on rows of an embedding table.
+int check_embed(int32_t dtype, int32_t other, int64_t N, int64_t V, int64_t H) {
+  if ((dtype != OPD_F32 && dtype != OPD_BF16) || (other != OPD_F32 && other != OPD_BF16))
+    return OPD_ERR_DTYPE;
+  if (N < 0 || N > INT32_MAX || V < 1 || V > INT32_MAX || H < 1 || H > kMaxHidden)
+    return OPD_ERR_SHAPE;
+  return OPD_OK;
+}
+bool rows_aligned(const void* p, int64_t ld, int32_t dtype) {
+  return aligned16(p) && (ld * elt_bytes(dtype)) % 16 == 0;
+}
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Workspace of opd_embed_grads: first places, sorted tokens, sums of tiles.
+struct EmbedLayout {
+  size_t perm, partial, total;
+  int64_t hp;
+};
+// Up to so many tokens are looked for by each entry's wavefront itself.
+constexpr int64_t kEmbedUnsorted = 256;
+EmbedLayout embed_layout(int64_t N, int64_t V, int64_t H) {
+  EmbedLayout l{};
+  l.hp = (H + 3) / 4 * 4;
+  if (N <= kEmbedUnsorted) return l;
+  l.perm = up256((size_t)(V + 1) * 4);
+  l.partial = l.perm + up256((size_t)N * 4);
+  l.total = l.partial + up256((size_t)((N + 63) / 64) * 2 * (size_t)l.hp * 4);
+  return l;
+}
+// Entries to a workgroup that sorts: as many workgroups as the GPU has CUs, up to 1,024 entries.
+int embed_keys(int64_t V) {
+  int keys = 64;
+  while (keys < 1024 && (int64_t)keys * 256 < V) keys *= 2;
+  return keys;
+}
+
+// Arguments shared by the calls on adapters.
+constexpr int64_t kMaxAdaptTokens = (int64_t)1 << 24;
+int check_adapters(int32_t dtype, int32_t y_dtype, int64_t N, int64_t H, int64_t O, int32_t G,
+                   int32_t r) {
+  if (dtype != OPD_F32 && dtype != OPD_BF16) return OPD_ERR_DTYPE;
+  if (y_dtype != OPD_F32 && y_dtype != dtype) return OPD_ERR_DTYPE;
+  if (N < 0 || N > kMaxAdaptTokens || H < 1 || H > kMaxHidden || O < 1 || O > kMaxHidden)
+    return OPD_ERR_SHAPE;
+  if (G < 1 || G > OPD_ADAPTERS_MAX || r < 1 || r > OPD_RANK_MAX) return OPD_ERR_SUPPORT;
+  return OPD_OK;
+}
+// Workspace of the calls on adapters, and how their products are split.
+struct AdaptLayout {
+  int64_t max_tiles, ldt;
+  int64_t span_x, span_y;      // of the long axes, parts
+  int splits_x, splits_y;
+  int outer_x, outer_y;        // parts of an adapter's tokens
+  size_t start, tiles, t, u, outer, total;
+};
+// Parts of a long axis of D columns: about 1,024 workgroups of 16 tokens, each
+// with 1,024 columns at least.
+void split_axis(int64_t groups, int64_t D, int64_t* span, int* splits) {
+  int64_t s = 1024 / groups, most = D / 1024;
+  if (s > most) s = most;
+  if (s < 1) s = 1;
+  *span = ((D + s - 1) / s + 511) / 512 * 512;
+  *splits = (int)((D + *span - 1) / *span);
+}
+AdaptLayout adapt_layout(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r, int32_t dtype,
+                         int32_t y_dtype, bool backward) {
+  AdaptLayout l{};
+  const int64_t keys = (int64_t)G + 2 < N ? (int64_t)G + 2 : N;
+  l.max_tiles = N / opd::kAdTile + keys;
+  l.ldt = (r + 3) / 4 * 4;
+  const int64_t groups = N / 16 + (keys + 1) / 2 + 1;
+  split_axis(groups, H, &l.span_x, &l.splits_x);
+  split_axis(groups, O, &l.span_y, &l.splits_y);
+  size_t at = up256((size_t)N * 4);  // perm
+  l.start = at;
+  at += up256((size_t)(G + 3) * 4);
+  l.tiles = at;
+  at += up256((size_t)l.max_tiles * sizeof(opd::AdTile));
+  l.t = at;
+  at += up256((size_t)l.splits_x * N * l.ldt * 4);
+  l.u = at;
+  if (backward) {
+    at += up256((size_t)l.splits_y * N * l.ldt * 4);
+    l.outer = at;
+    const int64_t used = G < N ? G : N;
+    auto parts = [&](int64_t D, int32_t dt) {
+      const int64_t span = dt == OPD_BF16 ? 512 : 256;
+      int64_t s = 1024 / (((D + span - 1) / span) * (used > 0 ? used : 1));
+      if (s > N / 128) s = N / 128;
+      if (s > 64) s = 64;
+      return (int)(s < 1 ? 1 : s);
+    };
+    l.outer_x = parts(H, dtype);
+    l.outer_y = parts(O, y_dtype);
+    const size_t gr = (size_t)G * (size_t)r * 4;
+    const size_t px = l.outer_x > 1 ? (size_t)l.outer_x * gr * (size_t)((H + 3) / 4 * 4) : 0;
+    const size_t py = l.outer_y > 1 ? (size_t)l.outer_y * gr * (size_t)((O + 3) / 4 * 4) : 0;
+    at += up256(px > py ? px : py);
+  }
+  l.total = at;
+  return l;
+}
+// (a launch has fewer than 2^32 work-items)
+bool adapt_fits(const AdaptLayout& l, int64_t D, int32_t G) {
+  const int64_t chunks = (D + 255) / 256;
+  return l.max_tiles * chunks * 256 <= kMaxGridLanes && (int64_t)G * 64 * chunks <= INT32_MAX &&
+         (int64_t)G * chunks * 512 <= kMaxGridLanes &&
+         l.max_tiles * 4 * 512 * (l.splits_x > l.splits_y ? l.splits_x : l.splits_y) <=
+             kMaxGridLanes;
+}
+
+// How rows of logits are cut for the selection of beams.
+int check_beams(int32_t dtype, int64_t B, int32_t W, int64_t V, int64_t ld) {
+  if (dtype != OPD_F32 && dtype != OPD_BF16) return OPD_ERR_DTYPE;
+  if (W < 1 || W > OPD_BEAM_MAX) return OPD_ERR_SUPPORT;
+  if (int rc = check_shape(B, V, ld)) return rc;
+  if (B > INT32_MAX / opd::kBeamMax / 16) return OPD_ERR_SHAPE;
+  return OPD_OK;
+}
+struct BeamPlan {
+  int slots;
+  int64_t parts;
+  size_t cands, total;
+};
+// Parts of up to 8 vectors of 16 bytes a lane, fewer where the rows are few: 1,024
+// workgroups.
+BeamPlan beam_plan(int64_t rows, int64_t V, int32_t dtype) {
+  BeamPlan p{8, 0, 0, 0};
+  for (;; p.slots /= 2) {
+    const int64_t part = 256 * (16 / elt_bytes(dtype)) * (int64_t)p.slots;
+    p.parts = (V + part - 1) / part;
+    if (p.slots == 1 || rows * p.parts >= 1024) break;
+  }
+  p.cands = up256((size_t)rows * (size_t)p.parts * sizeof(opd::BeamRec));
+  p.total = p.cands + (size_t)rows * (size_t)p.parts * opd::kBeamMax * 8;
   return p;
 }
 
@@ -701,6 +840,235 @@ int opd_verify_drafts(const void* target_logits, const void* draft_logits, int32
   a.table = p.table;
   a.round = p.round;
   const hipError_t err = opd::launch_verify(a, dtype, (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+int opd_embed_tokens(const void* table, int32_t dtype, int64_t V, int64_t H, int64_t ld,
+                     const int32_t* ids, int64_t N, float scale, void* out, int32_t out_dtype,
+                     int64_t ldo, void* stream) {
+  if (int rc = check_embed(dtype, out_dtype, N, V, H)) return rc;
+  if (ld < H || ldo < H) return OPD_ERR_SHAPE;
+  if (N == 0) return OPD_OK;
+  if (!table || !ids || !out) return OPD_ERR_NULL;
+  if (!rows_aligned(table, ld, dtype) || !rows_aligned(out, ldo, out_dtype)) return OPD_ERR_ALIGN;
+  opd::EmbedArgs a{};
+  a.table = table;
+  a.V = V;
+  a.H = H;
+  a.ld = ld;
+  a.ids = ids;
+  a.N = N;
+  a.scale = scale;
+  a.out = out;
+  a.ldo = ldo;
+  const hipError_t err = opd::launch_embed(a, dtype, out_dtype, (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H) {
+  if (check_embed(OPD_F32, OPD_F32, N, V, H) != OPD_OK) return 0;
+  return embed_layout(N, V, H).total;
+}
+
+int opd_embed_grads(const void* dy, int32_t dtype, int64_t N, int64_t H, int64_t ldy,
+                    const int32_t* ids, int64_t V, float scale, void* dtable, int32_t out_dtype,
+                    int64_t ldo, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+  if (int rc = check_embed(dtype, out_dtype, N, V, H)) return rc;
+  if (ldy < H || ldo < H) return OPD_ERR_SHAPE;
+  if (accumulate != 0 && accumulate != 1) return OPD_ERR_PARAM;
+  if (!dtable || (N > 0 && (!dy || !ids))) return OPD_ERR_NULL;
+  if (!rows_aligned(dtable, ldo, out_dtype) || (N > 0 && !rows_aligned(dy, ldy, dtype)))
+    return OPD_ERR_ALIGN;
+  const EmbedLayout l = embed_layout(N, V, H);
+  if (l.total > 0 && (!workspace || workspace_bytes < l.total || !aligned16(workspace)))
+    return OPD_ERR_WORKSPACE;
+  if (N == 0 && accumulate) return OPD_OK;
+  opd::EmbedGradArgs a{};
+  a.dy = dy;
+  a.V = V;
+  a.H = H;
+  a.ldy = ldy;
+  a.ids = ids;
+  a.N = N;
+  a.scale = scale;
+  a.accumulate = accumulate;
+  a.out = dtable;
+  a.ldo = ldo;
+  a.keys = embed_keys(V);
+  char* ws = (char*)workspace;
+  if (l.total > 0) {
+    a.start = (int32_t*)ws;
+    a.perm = (int32_t*)(ws + l.perm);
+    a.partial = (float*)(ws + l.partial);
+  }
+  a.hp = l.hp;
+  const hipError_t err = opd::launch_embed_grad(a, dtype, out_dtype, (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+size_t opd_adapter_workspace_bytes(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r,
+                                   int32_t dtype, int32_t y_dtype, int32_t backward) {
+  if (check_adapters(dtype, y_dtype, N, H, O, G, r) != OPD_OK) return 0;
+  return adapt_layout(N, H, O, G, r, dtype, y_dtype, backward != 0).total;
+}
+
+int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x, int32_t dtype,
+                     int64_t ldx, const void* a, int64_t lda, const void* b, int64_t ldb,
+                     const float* scales, const int32_t* adapter_ids, int64_t N, int64_t H,
+                     int64_t O, int32_t G, int32_t r, void* out, int64_t ldo, float* low_out,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_adapters(dtype, y_dtype, N, H, O, G, r)) return rc;
+  if (ldy < O || ldx < H || lda < H || ldb < O || ldo < O) return OPD_ERR_SHAPE;
+  if (N == 0) return OPD_OK;
+  if (!y || !x || !a || !b || !adapter_ids || !out) return OPD_ERR_NULL;
+  if (!rows_aligned(y, ldy, y_dtype) || !rows_aligned(out, ldo, y_dtype) ||
+      !rows_aligned(x, ldx, dtype) || !rows_aligned(a, lda, dtype) || !rows_aligned(b, ldb, dtype))
+    return OPD_ERR_ALIGN;
+  if (y == out && ldy != ldo) return OPD_ERR_SHAPE;
+  const AdaptLayout l = adapt_layout(N, H, O, G, r, dtype, y_dtype, false);
+  if (!adapt_fits(l, O, G)) return OPD_ERR_SHAPE;
+  if (!workspace || workspace_bytes < l.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  const hipStream_t st = (hipStream_t)stream;
+  const opd::AdaptArgs plan{adapter_ids, N, G, (int32_t*)ws, (int32_t*)(ws + l.start),
+                            (opd::AdTile*)(ws + l.tiles), l.max_tiles};
+  hipError_t err = opd::launch_adapt_plan(plan, st);
+  if (err != hipSuccess) return OPD_ERR_HIP;
+  const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
+                       l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
+  err = opd::launch_low(t, dtype, dtype, st);
+  if (err != hipSuccess) return OPD_ERR_HIP;
+  const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r,
+                          opd::LowRef{t.out, t.ldo, t.stride, t.splits, r}, scales, b, ldb, O, y,
+                          ldy, out, ldo, low_out};
+  err = opd::launch_expand(e, dtype, y_dtype, st);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void* x, int32_t dtype,
+                      int64_t ldx, const void* a, int64_t lda, const void* b, int64_t ldb,
+                      const float* scales, const int32_t* adapter_ids, int64_t N, int64_t H,
+                      int64_t O, int32_t G, int32_t r, const float* low, const void* dx_shared,
+                      int64_t ldds, void* dx, int64_t lddx, float* da, int64_t ldda, float* db,
+                      int64_t lddb, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_adapters(dtype, y_dtype, N, H, O, G, r)) return rc;
+  if (lddy < O || ldx < H || lda < H || ldb < O || ldda < H || lddb < O || (dx && lddx < H) ||
+      (dx_shared && ldds < H))
+    return OPD_ERR_SHAPE;
+  if (!da || !db || !a || !b) return OPD_ERR_NULL;
+  if (N > 0 && (!dy || !x || !adapter_ids || (dx_shared && !dx))) return OPD_ERR_NULL;
+  if (!rows_aligned(a, lda, dtype) || !rows_aligned(b, ldb, dtype) ||
+      !rows_aligned(da, ldda, OPD_F32) || !rows_aligned(db, lddb, OPD_F32))
+    return OPD_ERR_ALIGN;
+  if (N > 0 && (!rows_aligned(dy, lddy, y_dtype) || !rows_aligned(x, ldx, dtype) ||
+                (dx && !rows_aligned(dx, lddx, dtype)) ||
+                (dx_shared && !rows_aligned(dx_shared, ldds, dtype))))
+    return OPD_ERR_ALIGN;
+  if (dx && dx == dx_shared && lddx != ldds) return OPD_ERR_SHAPE;
+  const AdaptLayout l = adapt_layout(N, H, O, G, r, dtype, y_dtype, true);
+  if (!adapt_fits(l, H > O ? H : O, G)) return OPD_ERR_SHAPE;
+  if (!workspace || workspace_bytes < l.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  const hipStream_t st = (hipStream_t)stream;
+  const opd::AdaptArgs plan{adapter_ids, N, G, (int32_t*)ws, (int32_t*)(ws + l.start),
+                            (opd::AdTile*)(ws + l.tiles), l.max_tiles};
+  hipError_t err = opd::launch_adapt_plan(plan, st);
+  if (err != hipSuccess) return OPD_ERR_HIP;
+  opd::LowRef tref{low, r, 0, 1, r};
+  if (N > 0) {
+    if (!low) {
+      const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
+                           l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
+      err = opd::launch_low(t, dtype, dtype, st);
+      if (err != hipSuccess) return OPD_ERR_HIP;
+      tref = opd::LowRef{t.out, t.ldo, t.stride, t.splits, r};
+    }
+  }
+  const opd::LowArgs u{plan.tiles, plan.perm, l.max_tiles, G, r, dy, b, lddy, ldb, O,
+                       l.splits_y, l.span_y, N * l.ldt, (float*)(ws + l.u), l.ldt};
+  const opd::LowRef uref{u.out, u.ldo, u.stride, u.splits, r};
+  if (N > 0) {
+    err = opd::launch_low(u, y_dtype, dtype, st);
+    if (err != hipSuccess) return OPD_ERR_HIP;
+  }
+  const int64_t hp = (H + 3) / 4 * 4, op = (O + 3) / 4 * 4, gr = (int64_t)G * r;
+  const opd::OuterArgs oa{plan.perm, plan.start, G, r, uref, scales, x, ldx, H, l.outer_x, gr * hp,
+                          (float*)(ws + l.outer), hp};
+  err = opd::launch_outer(oa, dtype, da, ldda, st);
+  if (err != hipSuccess) return OPD_ERR_HIP;
+  const opd::OuterArgs ob{plan.perm, plan.start, G, r, tref, scales, dy, lddy, O, l.outer_y,
+                          gr * op, (float*)(ws + l.outer), op};
+  err = opd::launch_outer(ob, y_dtype, db, lddb, st);
+  if (err != hipSuccess) return OPD_ERR_HIP;
+  if (!dx || N == 0) return OPD_OK;
+  const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r, uref, scales, a, lda, H,
+                          dx_shared, ldds, dx, lddx, nullptr};
+  err = opd::launch_expand(e, dtype, dtype, st);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+size_t opd_beam_workspace_bytes(int64_t B, int32_t W, int64_t V, int32_t dtype) {
+  if (check_beams(dtype, B, W, V, V) != OPD_OK || B == 0) return 0;
+  return beam_plan(B * W, V, dtype).total;
+}
+
+int opd_beam_select(const void* logits, int32_t dtype, int64_t B, int32_t W, int64_t V, int64_t ld,
+                    const float* scores, const uint8_t* finished, int32_t k, float* out_scores,
+                    int32_t* parents, int32_t* ids, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+  if (int rc = check_beams(dtype, B, W, V, ld)) return rc;
+  if (k < 1 || k > OPD_BEAM_MAX) return OPD_ERR_SUPPORT;
+  if (B == 0) return OPD_OK;
+  if (!logits || !scores || !out_scores || !parents || !ids) return OPD_ERR_NULL;
+  if (!rows_aligned(logits, ld, dtype)) return OPD_ERR_ALIGN;
+  const BeamPlan p = beam_plan(B * W, V, dtype);
+  if (!workspace || workspace_bytes < p.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
+  opd::BeamArgs a{};
+  a.logits = logits;
+  a.B = B;
+  a.V = V;
+  a.ld = ld;
+  a.W = W;
+  a.k = k;
+  a.scores = scores;
+  a.finished = finished;
+  a.slots = p.slots;
+  a.parts = (uint32_t)p.parts;
+  a.recs = workspace;
+  a.cands = (uint64_t*)((char*)workspace + p.cands);
+  a.out_scores = out_scores;
+  a.parents = parents;
+  a.ids = ids;
+  const hipError_t err = opd::launch_beam(a, dtype, (hipStream_t)stream);
+  return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
+}
+
+int opd_reorder_beams(const void* states, int64_t B, int32_t W, int64_t outer, int64_t inner_bytes,
+                      int64_t stride, int64_t outer_stride, const int32_t* parents, int32_t k,
+                      void* out, int64_t out_stride, int64_t out_outer_stride, void* stream) {
+  if (W < 1 || W > OPD_BEAM_MAX || k < 1 || k > OPD_BEAM_MAX) return OPD_ERR_SUPPORT;
+  constexpr int64_t most = (int64_t)1 << 40;
+  if (B < 0 || B > INT32_MAX || outer < 0 || outer > INT32_MAX || inner_bytes < 0 ||
+      inner_bytes > most)
+    return OPD_ERR_SHAPE;
+  // (slices of a state do not overlap each other, nor do states of `out`)
+  if (B > 0 && outer > 0 && inner_bytes > 0 &&
+      (stride < 0 || out_stride < 0 || (outer > 1 && (outer_stride < inner_bytes ||
+                                                      out_outer_stride < inner_bytes))))
+    return OPD_ERR_SHAPE;
+  if (B == 0 || outer == 0 || inner_bytes == 0) return OPD_OK;
+  if (!states || !parents || !out) return OPD_ERR_NULL;
+  const bool in_place = states == out;
+  if (in_place && (k != W || stride != out_stride || (outer > 1 && outer_stride != out_outer_stride)))
+    return OPD_ERR_SHAPE;
+  uint64_t all = (uint64_t)(uintptr_t)states | (uint64_t)(uintptr_t)out | (uint64_t)stride |
+                 (uint64_t)out_stride;
+  if (outer > 1) all |= (uint64_t)outer_stride | (uint64_t)out_outer_stride;
+  const int unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
+  const opd::ReorderArgs a{states, B, W, k, outer, inner_bytes, stride, outer_stride, parents, out,
+                           out_stride, out_outer_stride, in_place ? 1 : 0, 0, 0, 0};
+  const hipError_t err = opd::launch_reorder(a, unit, (hipStream_t)stream);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }
 

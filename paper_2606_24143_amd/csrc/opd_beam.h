@@ -1,0 +1,503 @@
+// Beam search beside the draws (included by opd_cache_kernels.hip only, whose sort
+// keys it uses): of W beams' rows of logits, the k best
+// continuations of a group, and the beams' states in their new order.
+//   select   score(w, v) = scores[w] + (z[w, v] - log sum_j exp(z[w, j])),
+//            the k largest of the group, ties to the lower beam, then the lower
+//            token; a finished beam is a candidate as it stands
+//   reorder  state[j] = state[parent[j]], in place or to another buffer
+// Scores are compared in double precision (sums of exponentials are good to
+// about 1e-8: fp32 terms with the rounding of their argument put back, doubles from
+// a lane's vector on), so beams that are nearly as good keep their order.
+#pragma once
+
+#include "opd_device.h"
+#include "opd_model.h"
+
+namespace opd {
+namespace {
+
+constexpr int kBeamThreads = 256;
+constexpr int kBeamWaves = kBeamThreads / 64;
+
+// The 64 largest of two descending lists, descending.
+__device__ __forceinline__ uint32_t beam_merge_desc(uint32_t a, uint32_t b_reversed) {
+  const int lane = threadIdx.x & 63;
+  uint32_t v = max(a, b_reversed);
+#pragma unroll
+  for (int stride = 32; stride > 0; stride >>= 1) {
+    const uint32_t pv = (uint32_t)__shfl_xor((int)v, stride, 64);
+    v = (lane & stride) == 0 ? max(v, pv) : min(v, pv);
+  }
+  return v;
+}
+
+// exp(f - m), m the maximum: the argument of the power of two is a rounded
+// product, whose rounding (and that of log2 e) goes into the result afterwards.
+__device__ __forceinline__ float beam_term(float f, float m) {
+  constexpr float hi = 1.44269504f, lo = 1.92596299e-8f, ln2 = 0.693147181f;
+  const float d = f - m;
+  const float p = d * hi;
+  const float r = fmaf(d, lo, fmaf(d, hi, -p));
+  const float e = fast_exp2(p);
+  // (d = -inf: p is -inf, r NaN, the term 0)
+  return p < -150.f ? 0.f : fmaf(e * ln2, r, e);
+}
+
+// Candidates of a part at most: all elements of fewer than k lanes (those above the
+// bound), and a wavefront's equal to it besides.
+template <class TI, int S>
+constexpr uint32_t beam_cap(int k) {
+  return (uint32_t)((k - 1) * S * (16 / TI::BYTES) + 64 * (16 / TI::BYTES) + k);
+}
+
+struct BeamLds {
+  uint32_t top[kBeamWaves][64];
+  float max[kBeamWaves];
+  double sum[kBeamWaves];
+  uint32_t n;
+};
+
+// One workgroup to a row's part of 256 * E * S elements, which stays in registers:
+// its maximum, its sum of exponentials, and its candidates: what is not below
+// the k-th largest of the lanes' maxima, so k of them at least are among the best k,
+// and none else can be.  Bound by HBM and the vector unit alike (about 14 instructions
+// an element).
+template <class TI, int S>
+__global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
+  constexpr int E = 16 / TI::BYTES;
+  constexpr int kSpan = kBeamThreads * E;  // elements of a slot
+  __shared__ BeamLds sh;
+  extern __shared__ uint64_t beam_cand[];  // beam_cap
+  uint64_t* const cand = beam_cand;
+  const uint32_t cap = beam_cap<TI, S>(a.k);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t row = a.row0 + blockIdx.x / a.parts;
+  const uint32_t part = blockIdx.x % a.parts;
+  if ((a.finished && a.finished[row]) || a.scores[row] == kNegInf) return;
+  const char* z = (const char*)a.logits + row * a.ld * TI::BYTES;
+  const int64_t v0 = (int64_t)part * (kSpan * S) + tid * E;
+  if (tid == 0) sh.n = 0;
+
+  u32x4 x[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const int64_t v = v0 + s * kSpan;
+    if (v + E <= a.V) {
+      x[s] = __builtin_nontemporal_load((const u32x4*)(z + v * TI::BYTES));
+    } else {
+      constexpr uint32_t none = TI::BYTES == 2 ? 0xFF80FF80u : 0xFF800000u;
+      x[s] = u32x4{none, none, none, none};
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (v + e >= a.V) continue;
+        if constexpr (TI::BYTES == 2) {
+          const uint32_t b = ((const uint16_t*)z)[v + e];
+          x[s][e / 2] = e & 1 ? (x[s][e / 2] & 0xFFFFu) | b << 16 : (x[s][e / 2] & 0xFFFF0000u) | b;
+        } else {
+          x[s][e] = ((const uint32_t*)z)[v + e];
+        }
+      }
+    }
+  }
+  auto value = [&](int s, int e) -> float {
+    if constexpr (TI::BYTES == 2)
+      return __uint_as_float(e & 1 ? x[s][e / 2] & 0xFFFF0000u : x[s][e / 2] << 16);
+    else
+      return __uint_as_float(x[s][e]);
+  };
+  float mine = kNegInf;  // (a NaN shows in the sum)
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) mine = fmaxf(mine, value(s, e));
+  }
+  // the lanes' maxima, sorted: their k-th bounds the candidates from below
+  const uint32_t sorted = wave_sort_desc(order_key(__float_as_uint(mine)));
+  sh.top[w][lane] = sorted;
+  if (lane == 0) sh.max[w] = key_value(sorted);
+  __syncthreads();
+  float m = sh.max[0];
+#pragma unroll
+  for (int i = 1; i < kBeamWaves; ++i) m = fmaxf(m, sh.max[i]);
+  const uint32_t ab = beam_merge_desc(sh.top[0][lane], sh.top[1][63 - lane]);
+  const uint32_t cd = beam_merge_desc(sh.top[2][lane], sh.top[3][63 - lane]);
+  const uint32_t all = beam_merge_desc(ab, (uint32_t)__shfl((int)cd, 63 - lane, 64));
+  const uint32_t bound = (uint32_t)__builtin_amdgcn_readlane((int)all, a.k - 1);
+  const float least = fmaxf(key_value(bound), -3.4028234663852886e38f);  // -inf has no mass
+
+  const float off = m == kNegInf ? 0.f : m;
+  double sum = 0.0;
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    float t[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) t[e] = beam_term(value(s, e), off);
+    if constexpr (E == 8)
+      sum += (double)(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
+    else
+      sum += (double)((t[0] + t[1]) + (t[2] + t[3]));
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) sh.sum[w] = sum;
+
+  const bool some = mine >= least;
+  if (__ballot(some)) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (some && value(s, e) >= least) {
+          const uint32_t at = atomicAdd(&sh.n, 1u);
+          const uint32_t v = (uint32_t)(v0 + s * kSpan + e);
+          if (at < cap) cand[at] = (uint64_t)order_key(__float_as_uint(value(s, e))) << 32 | (uint32_t)~v;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  uint32_t n = sh.n;
+  if (n > cap) {
+    // Many that are equal to the bound: those above it (in fewer than k lanes), then the
+    // equal ones slot by slot, whose tokens ascend, until there are enough.
+    __syncthreads();
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    for (int equal = 0; equal < 2; ++equal) {
+#pragma unroll 1
+      for (int s = 0; s < S; ++s) {
+        // (the slot's vector, without indexing the registers)
+        u32x4 y = x[0];
+#pragma unroll
+        for (int i = 1; i < S; ++i) y = s == i ? x[i] : y;
+        float f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if constexpr (TI::BYTES == 2)
+            f[e] = __uint_as_float(e & 1 ? y[e / 2] & 0xFFFF0000u : y[e / 2] << 16);
+          else
+            f[e] = __uint_as_float(y[e]);
+        }
+        // (lanes in turn waves: a slot's tokens ascend with the lanes)
+#pragma unroll 1
+        for (int turn = 0; turn < kBeamWaves; ++turn) {
+          const uint32_t have = sh.n;
+          __syncthreads();
+          if (turn == w && (!equal || have < (uint32_t)a.k)) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              if (equal ? f[e] == least : f[e] > least) {
+                const uint32_t at = atomicAdd(&sh.n, 1u);
+                const uint32_t v = (uint32_t)(v0 + s * kSpan + e);
+                if (at < cap) cand[at] = (uint64_t)order_key(__float_as_uint(f[e])) << 32 | (uint32_t)~v;
+              }
+            }
+          }
+          __syncthreads();
+        }
+      }
+    }
+    n = sh.n;
+  }
+  BeamRec* rec = (BeamRec*)a.recs + (row * a.parts + part);
+  uint64_t* out = a.cands + (row * a.parts + part) * (int64_t)kBeamMax;
+  if (n > (uint32_t)kBeamMax) {
+    // more than a record holds: the k largest, each at its rank
+    for (uint32_t i = tid; i < n; i += kBeamThreads) {
+      const uint64_t c = cand[i];
+      uint32_t rank = 0;
+      for (uint32_t o = 0; o < n; ++o) rank += cand[o] > c ? 1u : 0u;
+      if (rank < (uint32_t)a.k) out[rank] = c;
+    }
+    n = a.k;
+  } else if (tid < (int)n) {
+    out[tid] = cand[tid];
+  }
+  if (tid == 0) {
+    double t = sh.sum[0];
+#pragma unroll
+    for (int i = 1; i < kBeamWaves; ++i) t += sh.sum[i];
+    // (s NaN: a NaN or an infinity among the logits)
+    *rec = BeamRec{t, m, n};
+  }
+}
+
+// What a beam's candidates are scored with.
+enum BeamKind : uint32_t { kBeamLive = 0, kBeamDone = 1, kBeamDead = 2, kBeamBad = 3 };
+struct BeamRow {
+  double l, score;  // log of the sum relative to the maximum; the beam's score
+  float m;
+  uint32_t kind;
+};
+
+constexpr int kMergeThreads = 1024;
+constexpr int kMergeWaves = kMergeThreads / 64;
+struct MergeLds {
+  BeamRow row[kBeamMax];
+  double best[kMergeWaves];
+  uint64_t at[kMergeWaves];
+  uint32_t bad;
+};
+
+// a before b: a larger score, or an equal one at a lower beam, or token.
+__device__ __forceinline__ bool beam_before(double sa, uint64_t a, double sb, uint64_t b) {
+  return sa > sb || (sa == sb && a < b);
+}
+
+// One workgroup to a group: its rows' sums from their parts', then the k best of
+// the parts' candidates, one after the other.
+__global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
+  __shared__ MergeLds sh;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t b = blockIdx.x;
+  const int W = a.W, k = a.k;
+  if (tid == 0) sh.bad = 0;
+  __syncthreads();
+  for (int w = wave; w < W; w += kMergeWaves) {
+    const int64_t row = b * W + w;
+    BeamRow r;
+    const float score = a.scores[row];
+    r.score = (double)score;
+    r.l = 0.0;
+    r.m = 0.f;
+    r.kind = kBeamLive;
+    if (!(score < __builtin_huge_valf())) {
+      r.kind = kBeamBad;
+    } else if (score == kNegInf) {
+      r.kind = kBeamDead;
+    } else if (a.finished && a.finished[row]) {
+      r.kind = kBeamDone;
+    } else {
+      const BeamRec* rec = (const BeamRec*)a.recs + row * a.parts;
+      float m = kNegInf;
+      for (uint32_t p = lane; p < a.parts; p += 64) m = fmaxf(m, rec[p].m);
+      m = wave_max(m);
+      double s = 0.0;
+      for (uint32_t p = lane; p < a.parts; p += 64) {
+        // (an empty part has sum 0, one with a NaN or an infinity NaN)
+        const double d = rec[p].m == kNegInf ? 0.0 : (double)rec[p].m - (double)m;
+        s += rec[p].s * exp(d);
+      }
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+      r.m = m;
+      if (!(s < __builtin_huge_val()))
+        r.kind = kBeamBad;
+      else if (m == kNegInf)
+        r.kind = kBeamDead;  // no finite logit
+      else
+        r.l = log(s);
+    }
+    if (lane == 0) {
+      sh.row[w] = r;
+      if (r.kind == kBeamBad) atomicOr(&sh.bad, 1u);
+    }
+  }
+  __syncthreads();
+  float* scores = a.out_scores + b * k;
+  int32_t* parents = a.parents + b * k;
+  int32_t* ids = a.ids + b * k;
+  if (sh.bad) {
+    if (tid < k) {
+      scores[tid] = __builtin_nanf("");
+      parents[tid] = -1;
+      ids[tid] = -1;
+    }
+    return;
+  }
+  double last = __builtin_huge_val();
+  uint64_t last_at = 0;
+  for (int j = 0; j < k; ++j) {
+    double best = -__builtin_huge_val();
+    uint64_t at = ~0ull;
+    auto offer = [&](double s, uint64_t i) {
+      if (s > -__builtin_huge_val() && (j == 0 || beam_before(last, last_at, s, i)) &&
+          beam_before(s, i, best, at)) {
+        best = s;
+        at = i;
+      }
+    };
+    for (int w = wave; w < W; w += kMergeWaves) {
+      const BeamRow r = sh.row[w];
+      if (r.kind == kBeamDone) offer(r.score, (uint64_t)w << 32);
+      if (r.kind != kBeamLive) continue;
+      const BeamRec* rec = (const BeamRec*)a.recs + (b * W + w) * a.parts;
+      const uint64_t* cand = a.cands + (b * W + w) * (int64_t)a.parts * kBeamMax;
+      for (uint32_t p = 0; p < a.parts; ++p) {
+        if (lane >= (int)rec[p].n) continue;
+        const uint64_t c = cand[(int64_t)p * kBeamMax + lane];
+        const double logp = ((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l;
+        offer(r.score + logp, (uint64_t)w << 32 | (uint32_t)~(uint32_t)c);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      const double s = __shfl_xor(best, o, 64);
+      const uint64_t i = (uint64_t)__shfl_xor((unsigned long long)at, o, 64);
+      if (beam_before(s, i, best, at)) {
+        best = s;
+        at = i;
+      }
+    }
+    __syncthreads();
+    if (lane == 0) {
+      sh.best[wave] = best;
+      sh.at[wave] = at;
+    }
+    __syncthreads();
+    best = sh.best[0];
+    at = sh.at[0];
+    for (int i = 1; i < kMergeWaves; ++i) {
+      if (beam_before(sh.best[i], sh.at[i], best, at)) {
+        best = sh.best[i];
+        at = sh.at[i];
+      }
+    }
+    const bool none = best == -__builtin_huge_val();
+    if (tid == 0) {
+      const int w = none ? -1 : (int)(at >> 32);
+      scores[j] = (float)best;
+      parents[j] = w;
+      ids[j] = none || sh.row[w].kind == kBeamDone ? -1 : (int32_t)(uint32_t)at;
+    }
+    if (none) {
+      for (int i = j + 1 + tid; i < k; i += kMergeThreads) {
+        scores[i] = kNegInf;
+        parents[i] = -1;
+        ids[i] = -1;
+      }
+      return;
+    }
+    last = best;
+    last_at = at;
+  }
+}
+
+// ---------------------------------------------------------------- reordering
+
+constexpr int kMoveThreads = 256;
+template <int U>
+struct Unit {
+  typedef std::conditional_t<U == 16, u32x4, std::conditional_t<U == 4, uint32_t, uint8_t>> T;
+};
+
+// A lane moves one unit of U bytes (less at a row's end) of each of its group's
+// states: it reads all of them before it writes, so the states may be moved in
+// place; no other lane has that unit.  A beam that stays where it is is neither read nor
+// written there.  KM: most beams.
+template <int U, int KM>
+__global__ void __launch_bounds__(kMoveThreads) k_reorder(ReorderArgs a) {
+  typedef typename Unit<U>::T T;
+  const int64_t span = a.span0 + blockIdx.x % a.spans;
+  const int64_t bo = a.item0 + blockIdx.x / a.spans;  // group and outer slice
+  const int64_t b = bo / a.outer, o = bo % a.outer;
+  const int64_t c = (span * kMoveThreads + threadIdx.x) * U;
+  if (c >= a.inner) return;
+  const char* from = (const char*)a.states + b * a.W * a.stride + o * a.outer_stride + c;
+  char* to = (char*)a.out + b * a.k * a.out_stride + o * a.out_outer_stride + c;
+  const int32_t* parents = a.parents + b * a.k;
+  const bool whole = c + U <= a.inner;
+  T x[KM];
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    if (j >= a.k) continue;
+    const int32_t p = parents[j];
+    x[j] = T{};
+    if ((uint32_t)p >= (uint32_t)a.W || (a.in_place && p == j)) continue;
+    if (whole) {
+      x[j] = *(const T*)(from + p * a.stride);
+    } else if constexpr (U > 1) {
+      const uint8_t* q = (const uint8_t*)from + p * a.stride;
+      union {
+        T t;
+        uint8_t u[U];
+      } v = {};
+      for (int i = 0; i < U; ++i)
+        if (c + i < a.inner) v.u[i] = q[i];
+      x[j] = v.t;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    if (j >= a.k) continue;
+    if (a.in_place && parents[j] == j) continue;
+    if (whole) {
+      *(T*)(to + j * a.out_stride) = x[j];
+    } else if constexpr (U > 1) {
+      uint8_t* q = (uint8_t*)to + j * a.out_stride;
+      union {
+        T t;
+        uint8_t u[U];
+      } v;
+      v.t = x[j];
+      for (int i = 0; i < U; ++i)
+        if (c + i < a.inner) q[i] = v.u[i];
+    }
+  }
+}
+
+template <int U, int KM>
+hipError_t reorder_u(ReorderArgs a, hipStream_t st) {
+  // launches of fewer than 2^32 work-items: some items whole, or an item in parts
+  constexpr int64_t most = ((int64_t)1 << 32) / kMoveThreads - 1;
+  const int64_t spans = (a.inner + (int64_t)U * kMoveThreads - 1) / ((int64_t)U * kMoveThreads);
+  const int64_t items = a.B * a.outer;
+  const int64_t per = spans < most ? most / spans : 1;
+  for (int64_t i = 0; i < items; i += per) {
+    const int64_t n = items - i < per ? items - i : per;
+    a.item0 = i;
+    for (int64_t s0 = 0; s0 < spans; s0 += most) {
+      a.span0 = s0;
+      a.spans = (uint32_t)(spans - s0 < most ? spans - s0 : most);
+      hipLaunchKernelGGL((k_reorder<U, KM>), dim3((unsigned)(n * a.spans)), dim3(kMoveThreads), 0,
+                         st, a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+template <class TI, int S>
+hipError_t beam_s(BeamArgs a, hipStream_t st) {
+  const int64_t rows = a.B * a.W;
+  const int64_t most = (((int64_t)1 << 32) / kBeamThreads - 1) / a.parts;
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    const int64_t n = rows - r0 < most ? rows - r0 : most;
+    a.row0 = r0;
+    const size_t lds = beam_cap<TI, S>(a.k) * sizeof(uint64_t);
+    hipLaunchKernelGGL((k_beam_rows<TI, S>), dim3((unsigned)(n * a.parts)), dim3(kBeamThreads), lds,
+                       st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+template <class TI>
+hipError_t beam_t(const BeamArgs& a, hipStream_t st) {
+  return a.slots == 1   ? beam_s<TI, 1>(a, st)
+         : a.slots == 2 ? beam_s<TI, 2>(a, st)
+         : a.slots == 4 ? beam_s<TI, 4>(a, st)
+                        : beam_s<TI, 8>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_beam(const BeamArgs& a, int in_dt, hipStream_t st) {
+  const hipError_t e = in_dt == BF16 ? beam_t<InBf16>(a, st) : beam_t<InF32>(a, st);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.B), dim3(kMergeThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_reorder(const ReorderArgs& a, int unit, hipStream_t st) {
+  if (unit == 16 && a.k <= 4) return reorder_u<16, 4>(a, st);
+  if (unit == 16 && a.k <= 8) return reorder_u<16, 8>(a, st);
+  if (unit == 16 && a.k <= 16) return reorder_u<16, 16>(a, st);
+  if (unit >= 4) return reorder_u<4, kBeamMax>(a, st);
+  return reorder_u<1, kBeamMax>(a, st);
+}
+
+}  // namespace opd

@@ -11,7 +11,8 @@
 //           plus log softmax(z) there;
 //   score   log softmax(z) at given ids.
 // (opd_head.h, included below: the rows of logits themselves from 8-bit operands;
-// opd_verify.h: rollout with drafted tokens.)
+// opd_verify.h: rollout with drafted tokens; opd_embed.h, opd_adapter.h and
+// opd_beam.h: token embeddings, low-rank adapters, and beams.)
 // One 1024-lane workgroup per token row.  A row that fits the registers
 // (bf16 up to 155,648 entries, fp32 up to 77,824) is loaded once and kept
 // there; wider rows are streamed.
@@ -2134,3 +2135,6 @@ hipError_t launch_cache(const CacheArgs& a, CacheOp op, int in_dt, bool resident
 
 #include "opd_head.h"
 #include "opd_verify.h"
+#include "opd_embed.h"
+#include "opd_adapter.h"
+#include "opd_beam.h"

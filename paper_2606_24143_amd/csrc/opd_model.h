@@ -1,0 +1,149 @@
+// Internal interface between the C-ABI layer (opd_model_api.cpp) and the kernels around
+// the rows of logits: token embeddings, adapters, beams.  Not installed.
+#pragma once
+
+#include "opd_internal.h"
+
+namespace opd {
+
+// Token embeddings (opd_embed_tokens, opd_embed_grads).  Launches go over rows (tokens,
+// entries, tiles) times chunks of columns.
+struct EmbedArgs {
+  const void* table;      // [V, ld]
+  int64_t V, H, ld;
+  const int32_t* ids;     // [N]
+  int64_t N;
+  float scale;
+  void* out;              // [N, ldo]
+  int64_t ldo;
+  int64_t row0;           // (the launch sets these)
+  uint32_t units, chunks;
+};
+struct EmbedGradArgs {
+  const void* dy;         // [N, ldy]
+  int64_t V, H, ldy;
+  const int32_t* ids;     // [N]
+  int64_t N;
+  float scale;
+  int accumulate;
+  void* out;              // [V, ldo]
+  int64_t ldo;
+  int keys;               // entries that a workgroup sorts
+  int32_t* start;         // [V + 1]; NULL: tokens are not sorted (few)
+  int32_t* perm;          // [N]
+  float* partial;         // [ceil(N / 64), 2, hp]
+  int64_t hp;
+  int64_t row0;           // (the launch sets these)
+  uint32_t units, chunks;
+};
+hipError_t launch_embed(const EmbedArgs& a, int in_dt, int out_dt, hipStream_t stream);
+hipError_t launch_embed_grad(const EmbedGradArgs& a, int in_dt, int out_dt, hipStream_t stream);
+
+// Low-rank adapters (opd_add_adapters, opd_adapter_grads).
+constexpr int kAdTile = 64;  // tokens of one adapter in a tile, at most
+struct AdTile {
+  int32_t key, pos, count, unused;  // adapter (G: none, G + 1: bad id), place of its first token
+};
+struct AdaptArgs {
+  const int32_t* ids;     // [N]
+  int64_t N;
+  int G;
+  int32_t* perm;          // [N] tokens by adapter
+  int32_t* start;         // [G + 3] first places
+  AdTile* tiles;          // [max_tiles]
+  int64_t max_tiles;
+};
+// tokens times the rows of an adapter: out[n, 0 .. r)
+struct LowArgs {
+  const AdTile* tiles;
+  const int32_t* perm;
+  int64_t max_tiles;
+  int G, r;
+  const void* x;          // [N, ldx]
+  const void* w;          // [G, r, ldw]
+  int64_t ldx, ldw, D;
+  int splits;             // parts of the long axis, of `span` columns, `stride` floats apart
+  int64_t span, stride;
+  float* out;             // [splits][N, ldo]
+  int64_t ldo;
+};
+// what they are, to the kernels that read them
+struct LowRef {
+  const float* p;
+  int64_t ld, stride;
+  int splits, r;
+};
+// out = base + scale * low * w
+struct ExpandArgs {
+  const AdTile* tiles;
+  const int32_t* perm;
+  int64_t max_tiles;
+  int G, r;
+  LowRef low;
+  const float* scales;    // [G] nullable
+  const void* w;          // [G, r, ldw]
+  int64_t ldw, D;
+  const void* base;       // [N, ldb] nullable
+  int64_t ldb;
+  void* out;              // [N, ldo]
+  int64_t ldo;
+  float* low_out;         // [N, r] nullable
+};
+// out[g] = scale * sum over the adapter's tokens of low^T x
+struct OuterArgs {
+  const int32_t* perm;
+  const int32_t* start;
+  int G, r;
+  LowRef low;
+  const float* scales;
+  const void* x;          // [N, ldx]
+  int64_t ldx, D;
+  int splits;             // parts of the tokens, `stride` floats apart
+  int64_t stride;
+  float* out;             // [splits][G, r, ldo]
+  int64_t ldo;
+};
+hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t stream);
+hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t stream);
+hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t stream);
+hipError_t launch_outer(const OuterArgs& a, int x_dt, float* out, int64_t ldo, hipStream_t stream);
+
+// Beam selection and reordering (opd_beam_select, opd_reorder_beams).
+constexpr int kBeamMax = 64;
+struct BeamRec {
+  double s;               // sum of exp(z - m)
+  float m;
+  uint32_t n;             // candidates
+};
+struct BeamArgs {
+  const void* logits;     // [B W, ld]
+  int64_t B, V, ld;
+  int W, k;
+  const float* scores;    // [B, W]
+  const uint8_t* finished;  // [B, W] nullable
+  int slots;              // vectors of 16 bytes per lane: a part is 256 times that
+  uint32_t parts;         // of a row
+  void* recs;             // [B W, parts] BeamRec
+  uint64_t* cands;        // [B W, parts, kBeamMax] (order key of the logit, ~token)
+  float* out_scores;      // [B, k]
+  int32_t* parents;
+  int32_t* ids;
+  int64_t row0;           // (the launch sets it)
+};
+struct ReorderArgs {
+  const void* states;     // [B W] states of `outer` slices of `inner` bytes
+  int64_t B;
+  int W, k;
+  int64_t outer, inner, stride, outer_stride;  // bytes
+  const int32_t* parents; // [B, k]
+  void* out;              // [B k]
+  int64_t out_stride, out_outer_stride;
+  int in_place;
+  int64_t item0, span0;   // (the launch sets these)
+  uint32_t spans;
+};
+hipError_t launch_beam(const BeamArgs& a, int in_dt, hipStream_t stream);
+// unit: 16, 4 or 1 bytes, which divide every address and stride
+hipError_t launch_reorder(const ReorderArgs& a, int unit, hipStream_t stream);
+
+}  // namespace opd
