@@ -519,9 +519,10 @@ size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
  * and u enter the second product to 2^-17 of themselves where its result is bf16, to
  * 2^-25 where it is fp32.  A NaN or an infinity in a token's x (dy) or in its adapter reaches
  * its own row, and its adapter's da and db; no other's.
- * All rows are 16-byte aligned; what lies past a row's end is neither read nor written.
+ * All rows are 16-byte aligned, and read up to the next multiple of 16 bytes; what is there
+ * past their end may hold anything, and is not written.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N > 2^24, H or O outside [1, 2^22], a row stride
- * below its row's length, strides of in-place rows that differ, or a call whose launches
+ * below its row's length (or one of a or b above 2^22), strides of in-place rows that differ, or a call whose launches
  * would pass 2^32 work-items), OPD_ERR_SUPPORT (G outside [1, OPD_ADAPTERS_MAX], r outside
  * [1, OPD_RANK_MAX]), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0
  * adds nothing; the gradients are then zeros.

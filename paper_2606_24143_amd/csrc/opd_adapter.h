@@ -27,9 +27,10 @@ typedef __bf16 BFrag __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------- tokens by adapter
 
+constexpr int kAdKeys = 1024;
 struct PlanLds {
-  GroupLds group;
-  uint32_t tile[kGroupKeys + 1];
+  GroupLds<kAdKeys> group;
+  uint32_t tile[kAdKeys + 1];
 };
 
 // One workgroup: tokens sorted by adapter (key G: none, G + 1: an id outside [0, G)),
@@ -89,34 +90,36 @@ __global__ void __launch_bounds__(kGroupThreads) k_adapt_plan(AdaptArgs a) {
 
 // ---------------------------------------------------------------- loads
 
-template <class T>
-using Elem = std::conditional_t<T::BYTES == 2, uint16_t, uint32_t>;
-
-// Eight (bf16) or four (fp32) consecutive elements of a row, 16 bytes; those at or
-// past `end` are 0.
+// 16 bytes of a row from column c on, which is a multiple of theirs; 0 from `end` on.  (Of
+// 16 that the row ends in, those past it are read too: they lie in the same 16.)
 template <class T>
 __device__ __forceinline__ u32x4 load16(const char* row, int64_t c, int64_t end) {
-  constexpr int E = 16 / T::BYTES;
-  if (c + E <= end) return *(const u32x4*)(row + c * T::BYTES);
   u32x4 r = {0, 0, 0, 0};
-  if (c < end) {
+  if (c < end) r = *(const u32x4*)(row + c * T::BYTES);
+  return r;
+}
+// Columns at or past `end` of those from c on become 0.
+template <class T>
+__device__ __forceinline__ u32x4 cut16(u32x4 r, int64_t c, int64_t end) {
+  constexpr int E = 16 / T::BYTES;
+  const int valid = end - c > E ? E : end - c < 0 ? 0 : (int)(end - c);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      if (c + e >= end) continue;
-      const uint32_t b = ((const Elem<T>*)row)[c + e];
-      if constexpr (T::BYTES == 2)
-        r[e / 2] |= b << (16 * (e & 1));
-      else
-        r[e] = b;
+  for (int d = 0; d < 4; ++d) {
+    if constexpr (T::BYTES == 2) {
+      const uint32_t keep =
+          (2 * d < valid ? 0x0000FFFFu : 0u) | (2 * d + 1 < valid ? 0xFFFF0000u : 0u);
+      r[d] &= keep;
+    } else {
+      r[d] = d < valid ? r[d] : 0u;
     }
   }
   return r;
 }
-// Four consecutive elements widened to fp32.
+// Four elements widened to fp32; the same.
 template <class T>
 __device__ __forceinline__ f32x4 load4_wide(const char* row, int64_t c, int64_t end) {
   f32x4 f = {0.f, 0.f, 0.f, 0.f};
-  if (c + 4 <= end) {
+  if (c < end) {
     if constexpr (T::BYTES == 2) {
       const u32x2 x = *(const u32x2*)(row + c * 2);
 #pragma unroll
@@ -127,11 +130,12 @@ __device__ __forceinline__ f32x4 load4_wide(const char* row, int64_t c, int64_t 
     } else {
       f = *(const f32x4*)(row + c * 4);
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < end) f[e] = load_elem<T>(row, c + e);
   }
+  return f;
+}
+__device__ __forceinline__ f32x4 cut4(f32x4 f, int64_t c, int64_t end) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = c + e < end ? f[e] : 0.f;
   return f;
 }
 
@@ -150,6 +154,12 @@ __device__ __forceinline__ void transpose8(const u32x4 (&in)[8], u32x4 (&out)[8]
 __device__ __forceinline__ f32x4 mma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(BFrag, a),
                                                  __builtin_bit_cast(BFrag, b), c, 0, 0, 0);
+}
+// (16 ranks: a lane's four)
+__device__ __forceinline__ f32x4 mma_bf16_16(u32x2 a, u32x2 b, f32x4 c) {
+  typedef short S4 __attribute__((ext_vector_type(4)));
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(S4, a),
+                                                   __builtin_bit_cast(S4, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ f32x4 mma_f32(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -182,79 +192,144 @@ __device__ __forceinline__ float low_value(const LowRef& t, int64_t token, int c
 
 // ---------------------------------------------------------------- tokens times the rows
 
-// One workgroup to 16 tokens of an adapter and a part of the long axis: its waves
-// take steps of 64 (bf16) or 32 (fp32) columns in turn, and their sums are added in
-// order.  RT: ranks / 16.
+// One workgroup to 16 MT tokens of an adapter and a part of the long axis: its waves
+// take steps of 64 (bf16) or 32 (fp32) columns in turn, the next one on its way meanwhile,
+// and their sums are added in order.  RT: ranks / 16.
 constexpr int kLowThreads = 512;
 constexpr int kLowWaves = kLowThreads / 64;
-template <class TX, class TW, int RT>
+template <class TX, class TW, int RT, int MT>
 __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
   constexpr bool BF = TX::BYTES == 2 && TW::BYTES == 2;
   constexpr int STEP = BF ? 64 : 32;
-  __shared__ float sums[kLowWaves][16][RT * 16 + 1];
-  const int sub = blockIdx.x % (kAdTile / 16);
-  const AdTile tile = a.tiles[blockIdx.x / (kAdTile / 16)];
-  if (sub * 16 >= tile.count || tile.key >= a.G) return;
+  typedef std::conditional_t<BF, u32x4, f32x4> V;
+  __shared__ float sums[kLowWaves][16 * MT][RT * 16 + 1];
+  constexpr int SUBS = kAdTile / (16 * MT);
+  const int sub = blockIdx.x % SUBS * (16 * MT);
+  const AdTile tile = a.tiles[blockIdx.x / SUBS];
+  if (sub >= tile.count || tile.key >= a.G) return;
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int count = min(16, tile.count - sub * 16);
-  const int32_t* perm = a.perm + tile.pos + sub * 16;
-  const char* x = (const char*)a.x + (int64_t)perm[min(m, count - 1)] * a.ldx * TX::BYTES;
-  const char* w = (const char*)a.w + ((int64_t)tile.key * a.r + m) * a.ldw * TW::BYTES;
-  f32x4 acc[RT];
+  const int count = min(16 * MT, tile.count - sub);
+  const int32_t* perm = a.perm + tile.pos + sub;
+  const char* x[MT];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < MT; ++i)
+    x[i] = (const char*)a.x + (int64_t)perm[min(16 * i + m, count - 1)] * a.ldx * TX::BYTES;
+  const char* w = (const char*)a.w + ((int64_t)tile.key * a.r + m) * a.ldw * TW::BYTES;
+  f32x4 acc[MT][RT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   const int64_t d0 = (int64_t)blockIdx.y * a.span;
   const int64_t d1 = d0 + a.span < a.D ? d0 + a.span : a.D;
-  for (int64_t d = d0 + wave * STEP; d < d1; d += kLowWaves * STEP) {
-    if constexpr (BF) {
-      // (columns d + 16 q .. + 16 of both, 32 bytes a lane: two instructions' worth)
-      const int64_t c = d + 16 * q;
-      u32x4 xv[2], wv[RT][2];
+  // Two instructions' worth of both operands: columns d + 16 q .. + 16 (bf16) or d + 8 q ..
+  // + 8, 32 consecutive bytes of a lane's rows.
+  struct Step {
+    V x[MT][2], w[RT][2];
+  };
+  auto load = [&](Step& s, int64_t d) {
+    const int64_t c = d + STEP / 4 * q;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) xv[i] = load16<TX>(x, c + 8 * i, d1);
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          wv[t][i] = u32x4{0, 0, 0, 0};
-          if (16 * t + m < a.r)
-            wv[t][i] = load16<TW>(w + (int64_t)t * 16 * a.ldw * TW::BYTES, c + 8 * i, d1);
-        }
+      for (int i = 0; i < MT; ++i) {
+        if constexpr (BF)
+          s.x[i][h] = load16<TX>(x[i], c + 8 * h, d1);
+        else
+          s.x[i][h] = load4_wide<TX>(x[i], c + 4 * h, d1);
       }
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) acc[t] = mma_bf16(xv[i], wv[t][i], acc[t]);
-      }
-    } else {
-      const int64_t c = d + 8 * q;
-      f32x4 xv[2], wv[RT][2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) xv[i] = load4_wide<TX>(x, c + 4 * i, d1);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          wv[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (16 * t + m < a.r)
-            wv[t][i] = load4_wide<TW>(w + (int64_t)t * 16 * a.ldw * TW::BYTES, c + 4 * i, d1);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma unroll
-          for (int t = 0; t < RT; ++t) acc[t] = mma_f32(xv[i][e], wv[t][i][e], acc[t]);
+        s.w[t][h] = V{0, 0, 0, 0};
+        if (16 * t + m < a.r) {
+          const char* row = w + (int64_t)t * 16 * a.ldw * TW::BYTES;
+          if constexpr (BF)
+            s.w[t][h] = load16<TW>(row, c + 8 * h, d1);
+          else
+            s.w[t][h] = load4_wide<TW>(row, c + 4 * h, d1);
         }
       }
     }
+  };
+  auto add = [&](Step& s, int64_t d) {
+    if (d >= d1) return;
+    if (d + STEP > d1) {  // (what lies past the row's end may be anything)
+      const int64_t c = d + STEP / 4 * q;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if constexpr (BF)
+            s.x[i][h] = cut16<TX>(s.x[i][h], c + 8 * h, d1);
+          else
+            s.x[i][h] = cut4(s.x[i][h], c + 4 * h, d1);
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          if constexpr (BF)
+            s.w[t][h] = cut16<TW>(s.w[t][h], c + 8 * h, d1);
+          else
+            s.w[t][h] = cut4(s.w[t][h], c + 4 * h, d1);
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if constexpr (BF) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) acc[i][t] = mma_bf16(s.x[i][h], s.w[t][h], acc[i][t]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+              acc[i][t] = mma_f32(s.x[i][h][e], s.w[t][h][e], acc[i][t]);
+          }
+        }
+      }
+    }
+  };
+  // The rows lie a multiple of the memory channels' period apart, as a rule: workgroups that
+  // ran along them side by side would all ask the same channels.  So each starts at
+  // another step, and goes round.
+  constexpr int NEXT = kLowWaves * STEP;
+  const int steps = (int)((d1 - d0 + NEXT - 1) / NEXT);
+  int at = (int)(blockIdx.x % (uint32_t)steps);
+  auto column = [&]() {
+    const int64_t d = d0 + (int64_t)at * NEXT + wave * STEP;
+    at = at + 1 == steps ? 0 : at + 1;
+    return d;
+  };
+  {
+    Step s, t;
+    int64_t ds = column(), dt = 0;
+    load(s, ds);
+    int left = steps;
+#pragma unroll 1
+    for (; left > 2; left -= 2) {
+      load(t, dt = column());
+      add(s, ds);
+      load(s, ds = column());
+      add(t, dt);
+    }
+    if (left == 2) load(t, dt = column());
+    add(s, ds);
+    if (left == 2) add(t, dt);
   }
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
+  for (int i = 0; i < MT; ++i) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sums[wave][4 * q + i][16 * t + m] = acc[t][i];
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[wave][16 * i + 4 * q + e][16 * t + m] = acc[i][t][e];
+    }
   }
   __syncthreads();
   float* out = a.out + (int64_t)blockIdx.y * a.stride;
@@ -276,25 +351,30 @@ __device__ __forceinline__ int piece(int m) { return (m & 3) * 4 + (m >> 2); }
 constexpr int kExpThreads = 256;
 constexpr int kExpWaves = kExpThreads / 64;
 
-// E values of a row of the result, and back.
-template <class T, int E>
-__device__ __forceinline__ void load_values(const char* row, int64_t c, int64_t end, float (&f)[E]) {
+// The first `valid` elements of a vector of a row.
+template <class T>
+__device__ __forceinline__ void store_end(char* p, u32x4 x, int64_t valid) {
+  constexpr int S = 16 / T::BYTES;
+  if (valid >= S) {
+    *(u32x4*)p = x;
+    return;
+  }
 #pragma unroll
-  for (int v = 0; v < E / 4; ++v) {
-    const f32x4 x = load4_wide<T>(row, c + 4 * v, end);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[4 * v + e] = x[e];
+  for (int e = 0; e < S; ++e) {
+    if (e >= valid) continue;
+    if constexpr (T::BYTES == 2)
+      ((uint16_t*)p)[e] = (uint16_t)(x[e / 2] >> (16 * (e & 1)));
+    else
+      ((uint32_t*)p)[e] = x[e];
   }
 }
 template <class T, int E>
 __device__ __forceinline__ void store_values(char* row, int64_t c, int64_t end, const float (&f)[E]) {
   if (c + E <= end) {
     if constexpr (T::BYTES == 2) {
-      if constexpr (E == 8)
-        *(u32x4*)(row + c * 2) = u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
-                                       pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-      else
-        *(u32x2*)(row + c * 2) = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+      static_assert(E == 8, "16 bytes");
+      *(u32x4*)(row + c * 2) = u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
+                                     pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
     } else {
 #pragma unroll
       for (int v = 0; v < E / 4; ++v)
@@ -313,59 +393,62 @@ __device__ __forceinline__ void store_values(char* row, int64_t c, int64_t end, 
   }
 }
 
-// One workgroup to a tile of up to kAdTile tokens of an adapter and 4 waves' columns
-// (128 each, or 64 of fp32 rows): a wave keeps its columns of the adapter in
-// registers and passes over the tokens, 16 at a time.  The shared projection's values
-// are what the sums start from.  RB: ranks / 32.
-template <class TW, class TY, int RB>
-__global__ void __launch_bounds__(kExpThreads) k_expand(ExpandArgs a) {
+// One workgroup to a tile of up to kAdTile tokens of an adapter and every a.per-th group of
+// 4 waves' columns (128 each, or 64 of fp32 rows): a wave keeps its columns of the
+// adapter in registers and passes over the tokens, 16 at a time.  The shared projection's
+// values are what the sums start from, and become the results in place.  The next 16
+// tokens' are on their way meanwhile, and, up to 16 ranks, the next columns of the adapter.
+// KL: ranks of a lane's operand (bf16: 4 or 8); RB: of 4 KL ranks each.
+template <class TW, class TY, int KL, int RB>
+__global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(ExpandArgs a) {
   constexpr bool BF = TW::BYTES == 2;
   constexpr int E = BF ? 8 : 4;          // columns of a piece
+  constexpr int S = 16 / TY::BYTES;      // of a vector of the result
   constexpr int TERMS = TY::BYTES == 2 ? 2 : 3;
-  constexpr int KP = BF ? RB * 32 + 8 : RB * 32 + 4;  // (padded: lanes of a read spread over the banks)
+  constexpr int K = 4 * KL * RB;         // ranks
+  constexpr int KP = BF ? K + 8 : K + 4; // (padded: lanes of a read spread over the banks)
+  constexpr int WV = KL * RB;            // 16-byte vectors of the adapter to a lane
+  constexpr bool AHEAD = WV <= 4;
   __shared__ __align__(16) uint16_t part[BF ? TERMS : 1][BF ? kAdTile : 1][KP];
   __shared__ float wide[BF ? 1 : kAdTile][BF ? 1 : KP];
-  const AdTile tile = a.tiles[blockIdx.x];
+  __shared__ int32_t tokens[kAdTile];
+  // (columns first: workgroups side by side read whole rows)
+  const uint32_t chunk = blockIdx.x % a.per;
+  const AdTile tile = a.tiles[blockIdx.x / a.per];
   if (tile.count == 0) return;
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t* perm = a.perm + tile.pos;
-  const int64_t c0 = ((int64_t)blockIdx.y * kExpWaves + wave) * (16 * E);
   const bool live = tile.key < a.G;
   if (!live && tile.key == a.G && a.base == a.out) return;  // in place: as it is
-  // this wave's columns of the adapter, ranks along a lane
-  u32x4 wb[BF ? RB : 1][8];
-  f32x4 wf[BF ? 1 : RB * 8];
-  if (live) {
-    const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES;
+  const int64_t span = kExpWaves * 16 * E;
+  int64_t c0 = (int64_t)chunk * span + wave * (16 * E);
+  const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES;
+  const uint32_t ldw = (uint32_t)a.ldw * TW::BYTES;
+  // a wave's columns of the adapter, as they lie: ranks KL q + i of each 4 KL (fp32: 4 i + q)
+  auto load_w = [&](int64_t c0, u32x4 (&v)[WV]) {
     const int64_t c = c0 + piece(m) * E;
-    if constexpr (BF) {
 #pragma unroll
-      for (int k = 0; k < RB; ++k) {
-        u32x4 v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int rank = 32 * k + 8 * q + i;
-          v[i] = u32x4{0, 0, 0, 0};
-          if (rank < a.r) v[i] = load16<TW>(w + (int64_t)rank * a.ldw * 2, c, a.D);
-        }
-        transpose8(v, wb[k]);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < RB * 8; ++k) {
-        const int rank = 4 * k + q;
-        wf[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (rank < a.r) wf[k] = load4_wide<TW>(w + (int64_t)rank * a.ldw * 4, c, a.D);
-      }
+    for (int k = 0; k < WV; ++k) {
+      const int rank = BF ? 4 * KL * (k / KL) + KL * q + k % KL : 4 * k + q;
+      v[k] = u32x4{0, 0, 0, 0};
+      if (rank < a.r && c < a.D)
+        v[k] = *(const u32x4*)(w + ((uint32_t)rank * ldw + (uint32_t)c * TW::BYTES));
     }
+  };
+  u32x4 v[WV];
+  if (AHEAD && live) load_w(c0, v);
+  if ((int)threadIdx.x < kAdTile)
+    tokens[threadIdx.x] = perm[min((int)threadIdx.x, tile.count - 1)];
+  if (live) {
     const float scale = a.scales ? a.scales[tile.key] : 1.f;
-    for (int i = threadIdx.x; i < kAdTile * RB * 32; i += kExpThreads) {
-      const int n = i / (RB * 32), k = i % (RB * 32);
+    for (int i = threadIdx.x; i < kAdTile * K; i += kExpThreads) {
+      const int n = i / K, k = i % K;
       float f = 0.f;
-      if (n < tile.count) {
-        f = low_value(a.low, perm[n], k);
-        if (a.low_out && blockIdx.y == 0 && k < a.r) a.low_out[(int64_t)perm[n] * a.r + k] = f;
+      if (n < tile.count && k < a.r) {
+        const int64_t token = perm[n];
+        f = low_value(a.low, token, k);
+        if (a.low_out && chunk == 0) a.low_out[token * a.r + k] = f;
         f *= scale;
       }
       if constexpr (BF) {
@@ -377,74 +460,183 @@ __global__ void __launch_bounds__(kExpThreads) k_expand(ExpandArgs a) {
         wide[n][k] = f;
       }
     }
-  } else if (a.low_out && blockIdx.y == 0) {
+  } else if (a.low_out && chunk == 0) {
     for (int i = threadIdx.x; i < tile.count * a.r; i += kExpThreads)
       a.low_out[(int64_t)perm[i / a.r] * a.r + i % a.r] =
           tile.key == a.G ? 0.f : __builtin_nanf("");
   }
   __syncthreads();
-#pragma unroll 1
-  for (int n0 = 0; n0 < tile.count; n0 += 16) {
-    const bool mine = n0 + m < tile.count;
-    const int64_t token = perm[mine ? n0 + m : tile.count - 1];
-    // pieces 4 i + q of the wave's columns
-    float y[4][E];
+  // pieces 4 i + q of the wave's columns, of token n0 + m
+  const bool read = a.base && tile.key <= a.G;
+  auto load_y = [&](int64_t c0, int n0, u32x4 (&y)[4][E / S]) {
+    const char* row = (const char*)a.base + (int64_t)tokens[n0 + m] * a.ldb * TY::BYTES +
+                      (c0 + q * E) * TY::BYTES;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[i][e] = tile.key == a.G + 1 ? __builtin_nanf("") : 0.f;
-      const int64_t c = c0 + (4 * i + q) * E;
-      if (a.base && tile.key <= a.G && c < a.D)
-        load_values<TY, E>((const char*)a.base + token * a.ldb * TY::BYTES, c, a.D, y[i]);
+      for (int h = 0; h < E / S; ++h) {
+        y[i][h] = u32x4{0, 0, 0, 0};
+        if (c0 + (4 * i + q) * E + S * h < a.D)
+          y[i][h] = *(const u32x4*)(row + (4 * i * E + S * h) * TY::BYTES);
+      }
     }
+  };
+  u32x4 next[4][E / S];
+  if (read) {
+    load_y(c0, 0, next);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int h = 0; h < E / S; ++h) next[i][h] = u32x4{0, 0, 0, 0};
+    }
+  }
+#pragma unroll 1
+  for (;;) {
+    const int64_t c1 = c0 + a.per * span;
+    // the operand: for column j of a piece, a lane's KL ranks
+    uint32_t wb[RB][BF ? 8 : 1][BF ? KL / 2 : 1];
+    f32x4 wf[BF ? 1 : WV];
     if (live) {
+      if (!AHEAD) load_w(c0, v);
+      if constexpr (BF) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        f32x4 acc = {y[0][j], y[1][j], y[2][j], y[3][j]};
-        if constexpr (BF) {
+        for (int k = 0; k < RB; ++k) {
 #pragma unroll
-          for (int k = 0; k < RB; ++k) {
+          for (int j = 0; j < 8; ++j) {
 #pragma unroll
-            for (int t = TERMS - 1; t >= 0; --t)
-              acc = mma_bf16(wb[k][j], *(const u32x4*)&part[t][n0 + m][32 * k + 8 * q], acc);
+            for (int d = 0; d < KL / 2; ++d)
+              wb[k][j][d] = __builtin_amdgcn_perm(v[KL * k + 2 * d + 1][j / 2],
+                                                  v[KL * k + 2 * d][j / 2],
+                                                  j & 1 ? 0x07060302u : 0x05040100u);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < WV; ++k) wf[k] = __builtin_bit_cast(f32x4, v[k]);
+      }
+      if (AHEAD && c1 < a.D) load_w(c1, v);
+    }
+    const bool whole = c0 + 16 * E <= a.D;
+#pragma unroll 1
+    for (int n0 = 0; n0 < tile.count; n0 += 16) {
+      u32x4 y[4][E / S];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int h = 0; h < E / S; ++h) y[i][h] = next[i][h];
+      }
+      if (read) {
+        if (n0 + 16 < tile.count)
+          load_y(c0, n0 + 16, next);
+        else if (c1 < a.D)
+          load_y(c1, 0, next);
+      }
+      if (live) {
+        auto product = [&](int j, f32x4 acc) {
+          if constexpr (BF) {
+#pragma unroll
+            for (int k = 0; k < RB; ++k) {
+#pragma unroll
+              for (int t = TERMS - 1; t >= 0; --t) {
+                const uint16_t* low = &part[t][n0 + m][4 * KL * k + KL * q];
+                if constexpr (KL == 8) {
+                  acc = mma_bf16(u32x4{wb[k][j][0], wb[k][j][1], wb[k][j][2], wb[k][j][3]},
+                                 *(const u32x4*)low, acc);
+                } else {
+                  acc = mma_bf16_16(u32x2{wb[k][j][0], wb[k][j][1]}, *(const u32x2*)low, acc);
+                }
+              }
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < WV; ++k) acc = mma_f32(wf[k][j], wide[n0 + m][4 * k + q], acc);
+          }
+          return acc;
+        };
+        if constexpr (TY::BYTES == 2) {
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            f32x4 lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              lo[i] = __uint_as_float(y[i][0][d] << 16);
+              hi[i] = __uint_as_float(y[i][0][d] & 0xFFFF0000u);
+            }
+            lo = product(2 * d, lo);
+            hi = product(2 * d + 1, hi);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i][0][d] = pack_bf16x2(lo[i], hi[i]);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < RB * 8; ++k) acc = mma_f32(wf[k][j], wide[n0 + m][4 * k + q], acc);
-        }
+          for (int j = 0; j < E; ++j) {
+            f32x4 acc;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i][j] = acc[i];
+            for (int i = 0; i < 4; ++i) acc[i] = __uint_as_float(y[i][j / 4][j % 4]);
+            acc = product(j, acc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i][j / 4][j % 4] = __float_as_uint(acc[i]);
+          }
+        }
+      } else if (tile.key > a.G) {
+        constexpr uint32_t nan = TY::BYTES == 2 ? 0x7FC07FC0u : 0x7FC00000u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+          for (int h = 0; h < E / S; ++h) y[i][h] = u32x4{nan, nan, nan, nan};
+        }
+      }
+      if (n0 + m < tile.count) {
+        char* row = (char*)a.out + (int64_t)tokens[n0 + m] * a.ldo * TY::BYTES +
+                    (c0 + q * E) * TY::BYTES;
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int h = 0; h < E / S; ++h)
+              *(u32x4*)(row + (4 * i * E + S * h) * TY::BYTES) = y[i][h];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int h = 0; h < E / S; ++h)
+              store_end<TY>(row + (4 * i * E + S * h) * TY::BYTES, y[i][h],
+                            a.D - (c0 + (4 * i + q) * E + S * h));
+          }
+        }
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t c = c0 + (4 * i + q) * E;
-      if (mine && c < a.D)
-        store_values<TY, E>((char*)a.out + token * a.ldo * TY::BYTES, c, a.D, y[i]);
-    }
+    if (c1 >= a.D) return;
+    c0 = c1;
   }
 }
 
 // ---------------------------------------------------------------- summed over an adapter's tokens
 
-// One workgroup to an adapter, up to 64 ranks, 4 waves' columns, and every `splits`-th
-// block of 32 tokens.  A lane loads eight tokens' 16 bytes and transposes them.
-constexpr int kOutThreads = 256;
+// One workgroup to an adapter, up to 64 ranks and a wave's columns (128, or 64 of fp32
+// rows): its waves take blocks of 32 tokens in turn (with those of the other `splits`),
+// and their sums are added in order.  A lane loads eight tokens' 16 bytes and
+// transposes them; the block's r numbers come straight into the layout of the
+// second operand.  The next block's rows are on their way meanwhile.
+constexpr int kOutThreads = 512;
 constexpr int kOutWaves = kOutThreads / 64;
 template <class TX, int RT>
 __global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
   constexpr bool BF = TX::BYTES == 2;
   constexpr int E = BF ? 8 : 4;
   constexpr int TERMS = 3;
-  constexpr int KP = BF ? 32 + 8 : 32 + 1;
-  __shared__ __align__(16) uint16_t part[BF ? TERMS : 1][BF ? RT * 16 : 1][KP];
-  __shared__ float wide[BF ? 1 : RT * 16][BF ? 1 : KP];
+  constexpr int C = 16 * E;
+  __shared__ float sums[kOutWaves][16][C + 4];
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.x % a.splits;
-  const int g = blockIdx.x / a.splits;
-  const int r0 = blockIdx.z * (RT * 16);
-  const int64_t c0 = ((int64_t)blockIdx.y * kOutWaves + wave) * (16 * E);
+  // (columns first: workgroups side by side read whole rows)
+  const uint32_t item = blockIdx.x / a.chunks;
+  const int split = item % a.splits;
+  const int g = item / a.splits;
+  const int r0 = blockIdx.y * (RT * 16);
+  const int64_t c0 = (int64_t)(blockIdx.x % a.chunks) * C;
   const int32_t s = a.start[g], count = a.start[g + 1] - s;
   const int64_t c = c0 + piece(m) * E;
   const float scale = a.scales ? a.scales[g] : 1.f;
@@ -454,75 +646,109 @@ __global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-#pragma unroll 1
-  for (int32_t n0 = split * 32; n0 < count; n0 += a.splits * 32) {
-    const int32_t* perm = a.perm + s + n0;
-    const int here = min(32, count - n0);
-    __syncthreads();
-    for (int i = threadIdx.x; i < RT * 16 * 32; i += kOutThreads) {
-      const int n = i / (RT * 16), k = i % (RT * 16);
-      const float f = n < here ? scale * low_value(a.low, perm[n], r0 + k) : 0.f;
-      if constexpr (BF) {
-        uint16_t p[TERMS];
-        split_bf16<TERMS>(f, p);
+  // token of a lane's i-th row: 8 q + i of the block (fp32: 4 i + q)
+  auto at = [&](int i) { return BF ? 8 * q + i : 4 * i + q; };
+  auto load = [&](int32_t n0, u32x4 (&x)[8], float (&low)[RT][8]) {
+    const int here = count - n0;
+    const int32_t mine = (lane & 31) < here ? a.perm[s + n0 + (lane & 31)] : 0;
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) part[t][k][n] = p[t];
-      } else {
-        wide[k][n] = f;
+    for (int i = 0; i < 8; ++i) {
+      const int64_t token = __shfl(mine, at(i), 64);
+      x[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int t = 0; t < RT; ++t) low[t][i] = 0.f;
+      if (at(i) < here) {
+        x[i] = load16<TX>((const char*)a.x + token * a.ldx * TX::BYTES, c, a.D);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) low[t][i] = low_value(a.low, token, r0 + 16 * t + m);
       }
     }
-    __syncthreads();
+  };
+  auto add = [&](const u32x4 (&x)[8], const float (&low)[RT][8]) {
     if constexpr (BF) {
-      u32x4 x[8], v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int n = 8 * q + i;
-        x[i] = u32x4{0, 0, 0, 0};
-        if (n < here) x[i] = load16<TX>((const char*)a.x + (int64_t)perm[n] * a.ldx * 2, c, a.D);
-      }
+      u32x4 v[8];
       transpose8(x, v);
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
+        u32x4 p[TERMS];
 #pragma unroll
-        for (int p = TERMS - 1; p >= 0; --p) {
-          const u32x4 low = *(const u32x4*)&part[p][16 * t + m][8 * q];
+        for (int i = 0; i < 8; i += 2) {
+          uint16_t lo[TERMS], hi[TERMS];
+          split_bf16<TERMS>(scale * low[t][i], lo);
+          split_bf16<TERMS>(scale * low[t][i + 1], hi);
 #pragma unroll
-          for (int j = 0; j < E; ++j) acc[j][t] = mma_bf16(v[j], low, acc[j][t]);
+          for (int k = 0; k < TERMS; ++k) p[k][i / 2] = lo[k] | (uint32_t)hi[k] << 16;
+        }
+#pragma unroll
+        for (int k = TERMS - 1; k >= 0; --k) {
+#pragma unroll
+          for (int j = 0; j < E; ++j) acc[j][t] = mma_bf16(v[j], p[k], acc[j][t]);
         }
       }
     } else {
-      f32x4 x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int n = 4 * i + q;
-        x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (n < here) x[i] = load4_wide<TX>((const char*)a.x + (int64_t)perm[n] * a.ldx * 4, c, a.D);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
+        const f32x4 v = __builtin_bit_cast(f32x4, x[i]);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          const float low = wide[16 * t + m][4 * i + q];
+          const float f = scale * low[t][i];
 #pragma unroll
-          for (int j = 0; j < E; ++j) acc[j][t] = mma_f32(x[i][j], low, acc[j][t]);
+          for (int j = 0; j < E; ++j) acc[j][t] = mma_f32(v[j], f, acc[j][t]);
         }
       }
     }
+  };
+  const int32_t step = a.splits * kOutWaves * 32;
+  int32_t n0 = (split * kOutWaves + wave) * 32;
+  if (n0 < count) {
+    u32x4 x[8];
+    float low[RT][8];
+    load(n0, x, low);
+    if constexpr (RT <= 2) {
+      u32x4 y[8];
+      float lowy[RT][8];
+#pragma unroll 1
+      for (; (int64_t)n0 + step < count; n0 += step) {
+        load(n0 + step, y, lowy);
+        add(x, low);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] = y[i];
+#pragma unroll
+          for (int t = 0; t < RT; ++t) low[t][i] = lowy[t][i];
+        }
+      }
+    } else {  // (both do not fit the registers)
+#pragma unroll 1
+      for (; (int64_t)n0 + step < count; n0 += step) {
+        add(x, low);
+        load(n0 + step, x, low);
+      }
+    }
+    add(x, low);
   }
   // lane m holds rank m of each 16, piece 4 i + q of the columns
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int rank = r0 + 16 * t + m;
-    if (rank >= a.r) continue;
-    float* out = a.out + (int64_t)split * a.stride + ((int64_t)g * a.r + rank) * a.ldo;
+    if (t > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t at = c0 + (4 * i + q) * E;
-      if (at >= a.D) continue;
-      float f[E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) f[j] = acc[j][t][i];
-      store_values<InF32, E>((char*)out, at, a.D, f);
+      for (int j = 0; j < E; ++j) sums[wave][m][(4 * i + q) * E + j] = acc[j][t][i];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * C / 4; i += kOutThreads) {
+      const int rank = r0 + 16 * t + i / (C / 4), at = i % (C / 4) * 4;
+      if (rank >= a.r || c0 + at >= a.D) continue;
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = sums[0][i / (C / 4)][at + e];
+#pragma unroll
+        for (int v = 1; v < kOutWaves; ++v) f[e] += sums[v][i / (C / 4)][at + e];
+      }
+      float* out = a.out + (int64_t)split * a.stride + ((int64_t)g * a.r + rank) * a.ldo;
+      store_values<InF32, 4>((char*)out, c0 + at, a.D, f);
     }
   }
 }
@@ -540,41 +766,57 @@ __global__ void __launch_bounds__(256) k_outer_sum(OuterArgs a, float* out, int6
   }
 }
 
+template <class TX, class TW, int RT>
+hipError_t low_r(const LowArgs& a, hipStream_t st) {
+  // 32 tokens to a workgroup read the adapter half as often, where that leaves enough of them
+  if constexpr (RT <= 4) {
+    if (a.max_tiles * a.splits >= 100) {
+      const dim3 grid((unsigned)(a.max_tiles * (kAdTile / 32)), (unsigned)a.splits);
+      hipLaunchKernelGGL((k_low<TX, TW, RT, 2>), grid, dim3(kLowThreads), 0, st, a);
+      return hipGetLastError();
+    }
+  }
+  const dim3 grid((unsigned)(a.max_tiles * (kAdTile / 16)), (unsigned)a.splits);
+  hipLaunchKernelGGL((k_low<TX, TW, RT, 1>), grid, dim3(kLowThreads), 0, st, a);
+  return hipGetLastError();
+}
 template <class TX, class TW>
 hipError_t low_t(const LowArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.max_tiles * (kAdTile / 16)), (unsigned)a.splits);
   const int rt = (a.r + 15) / 16;
-  if (rt == 1)
-    hipLaunchKernelGGL((k_low<TX, TW, 1>), grid, dim3(kLowThreads), 0, st, a);
-  else if (rt == 2)
-    hipLaunchKernelGGL((k_low<TX, TW, 2>), grid, dim3(kLowThreads), 0, st, a);
-  else if (rt <= 4)
-    hipLaunchKernelGGL((k_low<TX, TW, 4>), grid, dim3(kLowThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_low<TX, TW, 8>), grid, dim3(kLowThreads), 0, st, a);
-  return hipGetLastError();
+  return rt == 1   ? low_r<TX, TW, 1>(a, st)
+         : rt == 2 ? low_r<TX, TW, 2>(a, st)
+         : rt <= 4 ? low_r<TX, TW, 4>(a, st)
+                   : low_r<TX, TW, 8>(a, st);
 }
 
 template <class TW, class TY>
-hipError_t expand_t(const ExpandArgs& a, hipStream_t st) {
+hipError_t expand_t(ExpandArgs a, hipStream_t st) {
   const int64_t span = kExpWaves * 16 * (TW::BYTES == 2 ? 8 : 4);
-  const dim3 grid((unsigned)a.max_tiles, (unsigned)((a.D + span - 1) / span));
-  const int rb = (a.r + 31) / 32;
-  if (rb == 1)
-    hipLaunchKernelGGL((k_expand<TW, TY, 1>), grid, dim3(kExpThreads), 0, st, a);
-  else if (rb == 2)
-    hipLaunchKernelGGL((k_expand<TW, TY, 2>), grid, dim3(kExpThreads), 0, st, a);
+  const int64_t chunks = (a.D + span - 1) / span;
+  // about as many workgroups as stay on the GPU at once
+  int64_t per = 2048 / a.max_tiles;
+  a.per = (uint32_t)(per < 1 ? 1 : per < chunks ? per : chunks);
+  const dim3 grid((unsigned)(a.max_tiles * a.per));
+#define OPD_EXPAND(KL, RB) \
+  hipLaunchKernelGGL((k_expand<TW, TY, KL, RB>), grid, dim3(kExpThreads), 0, st, a)
+  if (a.r <= 16)
+    OPD_EXPAND(4, 1);
+  else if (a.r <= 32)
+    OPD_EXPAND(8, 1);
+  else if (a.r <= 64)
+    OPD_EXPAND(8, 2);
   else
-    hipLaunchKernelGGL((k_expand<TW, TY, 4>), grid, dim3(kExpThreads), 0, st, a);
+    OPD_EXPAND(8, 4);
+#undef OPD_EXPAND
   return hipGetLastError();
 }
 
 template <class TX>
-hipError_t outer_t(const OuterArgs& a, hipStream_t st) {
-  const int64_t span = kOutWaves * 16 * (TX::BYTES == 2 ? 8 : 4);
+hipError_t outer_t(OuterArgs a, hipStream_t st) {
+  const int64_t span = 16 * (TX::BYTES == 2 ? 8 : 4);
   const int rt = (a.r + 15) / 16;
-  const dim3 grid((unsigned)(a.G * a.splits), (unsigned)((a.D + span - 1) / span),
-                  (unsigned)(rt <= 4 ? 1 : 2));
+  a.chunks = (uint32_t)((a.D + span - 1) / span);
+  const dim3 grid((unsigned)(a.G * a.splits * a.chunks), (unsigned)(rt <= 4 ? 1 : 2));
   if (rt == 1)
     hipLaunchKernelGGL((k_outer<TX, 1>), grid, dim3(kOutThreads), 0, st, a);
   else if (rt == 2)

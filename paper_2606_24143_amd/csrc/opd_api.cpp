@@ -354,10 +354,10 @@ EmbedLayout embed_layout(int64_t N, int64_t V, int64_t H) {
   l.total = l.partial + up256((size_t)((N + 63) / 64) * 2 * (size_t)l.hp * 4);
   return l;
 }
-// Entries to a workgroup that sorts: as many workgroups as the GPU has CUs, up to 1,024 entries.
+// Entries to a workgroup that sorts: some two workgroups to a CU, up to kEmbKeys entries.
 int embed_keys(int64_t V) {
   int keys = 64;
-  while (keys < 1024 && (int64_t)keys * 256 < V) keys *= 2;
+  while (keys < opd::kEmbKeys && (int64_t)keys * 512 < V) keys *= 2;
   return keys;
 }
 
@@ -410,11 +410,12 @@ AdaptLayout adapt_layout(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r, 
     at += up256((size_t)l.splits_y * N * l.ldt * 4);
     l.outer = at;
     const int64_t used = G < N ? G : N;
+    // of an adapter's tokens, a workgroup's waves take 256 at once
     auto parts = [&](int64_t D, int32_t dt) {
-      const int64_t span = dt == OPD_BF16 ? 512 : 256;
-      int64_t s = 1024 / (((D + span - 1) / span) * (used > 0 ? used : 1));
-      if (s > N / 128) s = N / 128;
-      if (s > 64) s = 64;
+      const int64_t span = dt == OPD_BF16 ? 128 : 64;
+      int64_t s = 512 / (((D + span - 1) / span) * (used > 0 ? used : 1));
+      const int64_t most = N / 512;
+      if (s > most) s = most;
       return (int)(s < 1 ? 1 : s);
     };
     l.outer_x = parts(H, dtype);
@@ -428,12 +429,12 @@ AdaptLayout adapt_layout(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r, 
   return l;
 }
 // (a launch has fewer than 2^32 work-items)
-bool adapt_fits(const AdaptLayout& l, int64_t D, int32_t G) {
-  const int64_t chunks = (D + 255) / 256;
-  return l.max_tiles * chunks * 256 <= kMaxGridLanes && (int64_t)G * 64 * chunks <= INT32_MAX &&
-         (int64_t)G * chunks * 512 <= kMaxGridLanes &&
-         l.max_tiles * 4 * 512 * (l.splits_x > l.splits_y ? l.splits_x : l.splits_y) <=
-             kMaxGridLanes;
+bool adapt_fits(const AdaptLayout& l, int64_t D, int32_t G, bool backward) {
+  const int64_t chunks = (D + 63) / 64, splits = l.splits_x > l.splits_y ? l.splits_x : l.splits_y;
+  if (l.max_tiles * 4 * 512 * splits > kMaxGridLanes) return false;
+  if (!backward) return true;
+  const int64_t parts = l.outer_x > l.outer_y ? l.outer_x : l.outer_y;
+  return (int64_t)G * parts * chunks * 2 * 512 <= kMaxGridLanes;
 }
 
 // How rows of logits are cut for the selection of beams.
@@ -919,7 +920,8 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
                      int64_t O, int32_t G, int32_t r, void* out, int64_t ldo, float* low_out,
                      void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check_adapters(dtype, y_dtype, N, H, O, G, r)) return rc;
-  if (ldy < O || ldx < H || lda < H || ldb < O || ldo < O) return OPD_ERR_SHAPE;
+  if (ldy < O || ldx < H || lda < H || ldb < O || ldo < O || lda > kMaxHidden || ldb > kMaxHidden)
+    return OPD_ERR_SHAPE;
   if (N == 0) return OPD_OK;
   if (!y || !x || !a || !b || !adapter_ids || !out) return OPD_ERR_NULL;
   if (!rows_aligned(y, ldy, y_dtype) || !rows_aligned(out, ldo, y_dtype) ||
@@ -927,7 +929,7 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
     return OPD_ERR_ALIGN;
   if (y == out && ldy != ldo) return OPD_ERR_SHAPE;
   const AdaptLayout l = adapt_layout(N, H, O, G, r, dtype, y_dtype, false);
-  if (!adapt_fits(l, O, G)) return OPD_ERR_SHAPE;
+  if (!adapt_fits(l, O, G, false)) return OPD_ERR_SHAPE;
   if (!workspace || workspace_bytes < l.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const hipStream_t st = (hipStream_t)stream;
@@ -941,7 +943,7 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r,
                           opd::LowRef{t.out, t.ldo, t.stride, t.splits, r}, scales, b, ldb, O, y,
-                          ldy, out, ldo, low_out};
+                          ldy, out, ldo, low_out, 0};
   err = opd::launch_expand(e, dtype, y_dtype, st);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }
@@ -954,7 +956,7 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
                       int64_t lddb, void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = check_adapters(dtype, y_dtype, N, H, O, G, r)) return rc;
   if (lddy < O || ldx < H || lda < H || ldb < O || ldda < H || lddb < O || (dx && lddx < H) ||
-      (dx_shared && ldds < H))
+      (dx_shared && ldds < H) || lda > kMaxHidden || ldb > kMaxHidden)
     return OPD_ERR_SHAPE;
   if (!da || !db || !a || !b) return OPD_ERR_NULL;
   if (N > 0 && (!dy || !x || !adapter_ids || (dx_shared && !dx))) return OPD_ERR_NULL;
@@ -967,7 +969,7 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
     return OPD_ERR_ALIGN;
   if (dx && dx == dx_shared && lddx != ldds) return OPD_ERR_SHAPE;
   const AdaptLayout l = adapt_layout(N, H, O, G, r, dtype, y_dtype, true);
-  if (!adapt_fits(l, H > O ? H : O, G)) return OPD_ERR_SHAPE;
+  if (!adapt_fits(l, H > O ? H : O, G, true)) return OPD_ERR_SHAPE;
   if (!workspace || workspace_bytes < l.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const hipStream_t st = (hipStream_t)stream;
@@ -994,16 +996,16 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
   }
   const int64_t hp = (H + 3) / 4 * 4, op = (O + 3) / 4 * 4, gr = (int64_t)G * r;
   const opd::OuterArgs oa{plan.perm, plan.start, G, r, uref, scales, x, ldx, H, l.outer_x, gr * hp,
-                          (float*)(ws + l.outer), hp};
+                          (float*)(ws + l.outer), hp, 0};
   err = opd::launch_outer(oa, dtype, da, ldda, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::OuterArgs ob{plan.perm, plan.start, G, r, tref, scales, dy, lddy, O, l.outer_y,
-                          gr * op, (float*)(ws + l.outer), op};
+                          gr * op, (float*)(ws + l.outer), op, 0};
   err = opd::launch_outer(ob, y_dtype, db, lddb, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   if (!dx || N == 0) return OPD_OK;
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r, uref, scales, a, lda, H,
-                          dx_shared, ldds, dx, lddx, nullptr};
+                          dx_shared, ldds, dx, lddx, nullptr, 0};
   err = opd::launch_expand(e, dtype, dtype, st);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }

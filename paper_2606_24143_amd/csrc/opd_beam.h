@@ -127,6 +127,8 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
   const float least = fmaxf(key_value(bound), -3.4028234663852886e38f);  // -inf has no mass
 
   const float off = m == kNegInf ? 0.f : m;
+#pragma unroll
+  for (int s = 0; s < S; ++s) keep_packed(x[s]);
   double sum = 0.0;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
@@ -142,6 +144,8 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
   for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if (lane == 0) sh.sum[w] = sum;
 
+#pragma unroll
+  for (int s = 0; s < S; ++s) keep_packed(x[s]);
   const bool some = mine >= least;
   if (__ballot(some)) {
 #pragma unroll
@@ -233,27 +237,119 @@ struct BeamRow {
 
 constexpr int kMergeThreads = 1024;
 constexpr int kMergeWaves = kMergeThreads / 64;
+constexpr uint32_t kMergeCap = 4096;  // candidates in LDS
+constexpr int kMergeEach = kMergeCap / kMergeThreads;
 struct MergeLds {
+  double score[kMergeCap];
+  uint64_t at[kMergeCap];  // beam, token
   BeamRow row[kBeamMax];
-  double best[kMergeWaves];
-  uint64_t at[kMergeWaves];
-  uint32_t bad;
+  uint32_t bound[2][kMergeWaves];
+  uint32_t n, bad, total;
 };
 
 // a before b: a larger score, or an equal one at a lower beam, or token.
 __device__ __forceinline__ bool beam_before(double sa, uint64_t a, double sb, uint64_t b) {
   return sa > sb || (sa == sb && a < b);
 }
+// A score's order in fp32 (equal for scores that are nearly so).
+__device__ __forceinline__ uint32_t beam_key(double s) { return order_key(__float_as_uint((float)s)); }
 
-// One workgroup to a group: its rows' sums from their parts', then the k best of
-// the parts' candidates, one after the other.
+// Of the n candidates in LDS, those that may be among the k best: what is not below a
+// bound that k lanes' largest reach.  Up to 16, a wave's k-th largest serves, the best
+// wave's (some 8 k are left); more take the k-th of all lanes, bit by bit.  Where that
+// leaves more than `most` (scores that are equal in fp32), each one's rank decides.
+__device__ __forceinline__ uint32_t merge_cut(MergeLds& sh, uint32_t n, int k, uint32_t most) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  double s[kMergeEach];
+  uint64_t at[kMergeEach];
+  uint32_t key[kMergeEach], top = 0;
+#pragma unroll
+  for (int i = 0; i < kMergeEach; ++i) {
+    const uint32_t e = i * kMergeThreads + tid;
+    key[i] = 0;
+    s[i] = 0.0;
+    at[i] = 0;
+    if (e < n) {
+      s[i] = sh.score[e];
+      at[i] = sh.at[e];
+      key[i] = beam_key(s[i]);
+      top = max(top, key[i]);
+    }
+  }
+  uint32_t bound = 0;
+  if (k <= 16) {
+#pragma unroll
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t c = bound | (1u << bit);
+      if (__popcll(__ballot(top >= c)) >= k) bound = c;
+    }
+    if (lane == 0) sh.bound[0][wave] = bound;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kMergeWaves; ++w) bound = max(bound, sh.bound[0][w]);
+  } else {
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t c = bound | (1u << bit);
+      const uint32_t reach = (uint32_t)__popcll(__ballot(top >= c));
+      if (lane == 0) sh.bound[bit & 1][wave] = reach;
+      __syncthreads();
+      uint32_t all = 0;
+#pragma unroll
+      for (int w = 0; w < kMergeWaves; ++w) all += sh.bound[bit & 1][w];
+      if (all >= (uint32_t)k) bound = c;
+    }
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+  }
+  uint32_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < kMergeEach; ++i) {
+    if (key[i] < bound) key[i] = 0;
+    mine += key[i] != 0 ? 1u : 0u;
+  }
+  if (mine) atomicAdd(&sh.n, mine);
+  __syncthreads();
+  uint32_t left = sh.n;
+  __syncthreads();
+  if (left > most) {
+#pragma unroll
+    for (int i = 0; i < kMergeEach; ++i) {
+      int rank = 0;
+      for (uint32_t e = 0; e < n; ++e)
+        rank += beam_before(sh.score[e], sh.at[e], s[i], at[i]) ? 1 : 0;
+      key[i] = rank < k ? key[i] : 0u;
+    }
+    left = min(n, (uint32_t)k);
+    __syncthreads();
+  }
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kMergeEach; ++i) {
+    if (key[i] == 0) continue;
+    const uint32_t to = atomicAdd(&sh.n, 1u);
+    sh.score[to] = s[i];
+    sh.at[to] = at[i];
+  }
+  __syncthreads();
+  return left;
+}
+
+// One workgroup to a group: its rows' sums from their parts', the scores of the parts'
+// candidates, of which LDS keeps those that may be among the best, and the k best of
+// them, each at its rank.
 __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
   __shared__ MergeLds sh;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t b = blockIdx.x;
   const int W = a.W, k = a.k;
-  if (tid == 0) sh.bad = 0;
+  if (tid == 0) {
+    sh.bad = 0;
+    sh.n = 0;
+    sh.total = W;
+  }
   __syncthreads();
   for (int w = wave; w < W; w += kMergeWaves) {
     const int64_t row = b * W + w;
@@ -275,13 +371,16 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
       for (uint32_t p = lane; p < a.parts; p += 64) m = fmaxf(m, rec[p].m);
       m = wave_max(m);
       double s = 0.0;
+      uint32_t found = 0;
       for (uint32_t p = lane; p < a.parts; p += 64) {
+        found += rec[p].n;
         // (an empty part has sum 0, one with a NaN or an infinity NaN)
         const double d = rec[p].m == kNegInf ? 0.0 : (double)rec[p].m - (double)m;
         s += rec[p].s * exp(d);
       }
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+      if (found) atomicAdd(&sh.total, found);
       r.m = m;
       if (!(s < __builtin_huge_val()))
         r.kind = kBeamBad;
@@ -293,6 +392,11 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     if (lane == 0) {
       sh.row[w] = r;
       if (r.kind == kBeamBad) atomicOr(&sh.bad, 1u);
+      if (r.kind == kBeamDone) {
+        const uint32_t to = atomicAdd(&sh.n, 1u);
+        sh.score[to] = r.score;
+        sh.at[to] = (uint64_t)w << 32;
+      }
     }
   }
   __syncthreads();
@@ -307,71 +411,62 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     }
     return;
   }
-  double last = __builtin_huge_val();
-  uint64_t last_at = 0;
-  for (int j = 0; j < k; ++j) {
-    double best = -__builtin_huge_val();
-    uint64_t at = ~0ull;
-    auto offer = [&](double s, uint64_t i) {
-      if (s > -__builtin_huge_val() && (j == 0 || beam_before(last, last_at, s, i)) &&
-          beam_before(s, i, best, at)) {
-        best = s;
-        at = i;
-      }
-    };
-    for (int w = wave; w < W; w += kMergeWaves) {
-      const BeamRow r = sh.row[w];
-      if (r.kind == kBeamDone) offer(r.score, (uint64_t)w << 32);
-      if (r.kind != kBeamLive) continue;
-      const BeamRec* rec = (const BeamRec*)a.recs + (b * W + w) * a.parts;
-      const uint64_t* cand = a.cands + (b * W + w) * (int64_t)a.parts * kBeamMax;
-      for (uint32_t p = 0; p < a.parts; ++p) {
-        if (lane >= (int)rec[p].n) continue;
-        const uint64_t c = cand[(int64_t)p * kBeamMax + lane];
-        const double logp = ((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l;
-        offer(r.score + logp, (uint64_t)w << 32 | (uint32_t)~(uint32_t)c);
-      }
+  uint32_t n = sh.n;
+  // the records of the group, one to a wave at a time
+  const uint32_t recs = W * a.parts;
+  const BeamRec* rec = (const BeamRec*)a.recs + b * recs;
+  const uint64_t* cand = a.cands + b * recs * (int64_t)kBeamMax;
+  auto take = [&](uint32_t p) {
+    const uint32_t w = p / a.parts;
+    const BeamRow r = sh.row[w];
+    if (r.kind != kBeamLive) return;
+    // (read beside the count: past it lies what the workspace held)
+    const uint64_t c = cand[(int64_t)p * kBeamMax + lane];
+    const bool mine = lane < (int)rec[p].n;
+    const double s = r.score + (((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l);
+    const uint64_t in = __ballot(mine && s > -__builtin_huge_val());
+    uint32_t to = 0;
+    if (lane == 0) to = atomicAdd(&sh.n, (uint32_t)__popcll(in));
+    to = __builtin_amdgcn_readfirstlane(to) + (uint32_t)__popcll(in & ((1ull << lane) - 1));
+    if (in >> lane & 1) {
+      sh.score[to] = s;
+      sh.at[to] = (uint64_t)w << 32 | (uint32_t)~(uint32_t)c;
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      const double s = __shfl_xor(best, o, 64);
-      const uint64_t i = (uint64_t)__shfl_xor((unsigned long long)at, o, 64);
-      if (beam_before(s, i, best, at)) {
-        best = s;
-        at = i;
-      }
-    }
+  };
+  if (sh.total <= kMergeCap) {
+    for (uint32_t p = wave; p < recs; p += kMergeWaves) take(p);
     __syncthreads();
-    if (lane == 0) {
-      sh.best[wave] = best;
-      sh.at[wave] = at;
-    }
+    n = sh.n;
     __syncthreads();
-    best = sh.best[0];
-    at = sh.at[0];
-    for (int i = 1; i < kMergeWaves; ++i) {
-      if (beam_before(sh.best[i], sh.at[i], best, at)) {
-        best = sh.best[i];
-        at = sh.at[i];
-      }
+  } else {
+    for (uint32_t p0 = 0; p0 < recs; p0 += kMergeWaves) {
+      if (n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
+      if (p0 + wave < recs) take(p0 + wave);
+      __syncthreads();
+      n = sh.n;
+      __syncthreads();
     }
-    const bool none = best == -__builtin_huge_val();
-    if (tid == 0) {
-      const int w = none ? -1 : (int)(at >> 32);
-      scores[j] = (float)best;
-      parents[j] = w;
-      ids[j] = none || sh.row[w].kind == kBeamDone ? -1 : (int32_t)(uint32_t)at;
-    }
-    if (none) {
-      for (int i = j + 1 + tid; i < k; i += kMergeThreads) {
-        scores[i] = kNegInf;
-        parents[i] = -1;
-        ids[i] = -1;
-      }
-      return;
-    }
-    last = best;
-    last_at = at;
+  }
+  while (n > 128) {
+    const uint32_t left = merge_cut(sh, n, k, 1024);
+    if (left == n) break;
+    n = left;
+  }
+  for (uint32_t i = tid; i < n; i += kMergeThreads) {
+    const double s = sh.score[i];
+    const uint64_t at = sh.at[i];
+    int rank = 0;
+    for (uint32_t e = 0; e < n; ++e) rank += beam_before(sh.score[e], sh.at[e], s, at) ? 1 : 0;
+    if (rank >= k) continue;
+    const int w = (int)(at >> 32);
+    scores[rank] = (float)s;
+    parents[rank] = w;
+    ids[rank] = sh.row[w].kind == kBeamDone ? -1 : (int32_t)(uint32_t)at;
+  }
+  for (int i = (int)n + tid; i < k; i += kMergeThreads) {
+    scores[i] = kNegInf;
+    parents[i] = -1;
+    ids[i] = -1;
   }
 }
 

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kEmbThreads = 256;
 constexpr int kEmbWaves = kEmbThreads / 64;
+constexpr int kEmbRows = 8;  // entries of a wavefront
 
 // E consecutive elements of a row, widened.
 template <class TI, int E>
@@ -134,23 +135,24 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed(EmbedArgs a) {
 
 // Tokens sorted by id: start[v] the first place of entry v, perm the tokens.
 __global__ void __launch_bounds__(kGroupThreads) k_embed_group(EmbedGradArgs a) {
-  __shared__ GroupLds sh;
+  __shared__ GroupLds<kEmbKeys> sh;
   const int32_t lo = (int32_t)((int64_t)blockIdx.x * a.keys);
   const int count = (int)(a.V - lo < a.keys ? a.V - lo : a.keys);
   const int32_t* ids = a.ids;
   const int64_t V = a.V;
   uint32_t end;
   const uint32_t first = group_tokens(
-      a.N, lo, count, [=](int64_t n) { return ids[n] < V ? ids[n] : -1; }, a.perm, sh, end);
+      a.N, lo, count, [=](int64_t n) { return (uint32_t)ids[n] < (uint32_t)V ? ids[n] : -1; }, a.perm, sh, end);
   if ((int)threadIdx.x < count) a.start[lo + (int)threadIdx.x] = (int32_t)first;
   if (threadIdx.x == 0 && lo + count == a.V) a.start[a.V] = (int32_t)end;
 }
 
-// Adds dy[token, c0 ..] for the tokens that lanes [0, count) hold, in order.
-template <class TI, int VPL>
+// Adds dy[token, c0 ..] for the tokens that lanes [0, count) hold, in order; B rows on
+// their way at once.
+template <class TI, int VPL, int B>
 __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t token, int count,
                                          int64_t c0, float (&f)[VPL][4]) {
-  constexpr int B = 4;  // rows on their way at once
+#pragma unroll 1
   for (int i = 0; i < count; i += B) {
     float x[B][VPL][4];
 #pragma unroll
@@ -179,7 +181,7 @@ __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t token, 
 // tile holds a part of at most two such entries: one that begins before or at its
 // first place (part 0), and one that begins inside it (part 1) and goes on past it.
 constexpr int kEmbTile = 64;
-template <class TI, int VPL>
+template <class TI>
 __global__ void __launch_bounds__(kEmbThreads) k_embed_tiles(EmbedGradArgs a) {
   const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_tiles(EmbedGradArgs a) {
   const int64_t p = tile * kEmbTile + lane;
   const int64_t kept = a.start[a.V];
   if (u >= a.units || tile * kEmbTile >= kept) return;
-  const int64_t c0 = (int64_t)(u % a.chunks) * (256 * VPL) + lane * 4;
+  const int64_t c0 = (int64_t)(u % a.chunks) * 256 + lane * 4;
   const int32_t token = p < kept ? a.perm[p] : 0;
   const int32_t id = p < kept ? a.ids[token] : -1;
   int32_t s = 0, e = 0;
@@ -203,75 +205,107 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_tiles(EmbedGradArgs a) {
     // (its places are consecutive: moved down to lane 0)
     const int first = __ffsll((long long)in) - 1, count = __popcll(in);
     const int32_t mine = __shfl(token, (first + lane) & 63, 64);
-    float f[VPL][4] = {};
-    add_rows<TI, VPL>(a, mine, count, c0, f);
+    float f[1][4] = {};
+    add_rows<TI, 1, 16>(a, mine, count, c0, f);
     float* to = a.partial + (tile * 2 + part) * a.hp;
-#pragma unroll
-    for (int v = 0; v < VPL; ++v)
-      if (c0 + v * 256 < a.H) *(f32x4*)(to + c0 + v * 256) = f32x4{f[v][0], f[v][1], f[v][2], f[v][3]};
+    if (c0 < a.H) *(f32x4*)(to + c0) = f32x4{f[0][0], f[0][1], f[0][2], f[0][3]};
   }
 }
 
-// One wavefront to an entry and a chunk of 256 * VPL columns: its tokens' rows, or
-// its tiles' sums, in order.  SORTED false: no list; the wave looks for its tokens
+// One wavefront to kEmbRows entries and a chunk of 256 * VPL columns: first the entries
+// without a token, which are stores alone, then the others': their tokens' rows, or their tiles'
+// sums, in order.  SORTED false: no list; the wave looks for its entries' tokens
 // among the ids itself (few tokens, one launch).
 template <class TI, class TO, int VPL, bool SORTED>
 __global__ void __launch_bounds__(kEmbThreads) k_embed_rows(EmbedGradArgs a) {
-  const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t block = xcd_eighths(blockIdx.x, gridDim.x);
+  const uint32_t u = block * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= a.units) return;
   const int lane = threadIdx.x & 63;
-  const int64_t v0 = a.row0 + u / a.chunks;
+  const int64_t v0 = (a.row0 + u / a.chunks) * kEmbRows;
   const int64_t c0 = (int64_t)(u % a.chunks) * (256 * VPL) + lane * 4;
-  float f[VPL][4] = {};
-  bool any = false;
+  const int rows = (int)(a.V - v0 < kEmbRows ? a.V - v0 : kEmbRows);
+  int32_t first = 0;
+  uint64_t some = 0;  // bit i: entry v0 + i has a token
   if constexpr (SORTED) {
-    const int32_t s = a.start[v0], e = a.start[v0 + 1];
-    any = e > s;
-    if (e - s > kEmbTile) {
-      const int64_t t1 = ((int64_t)e + kEmbTile - 1) / kEmbTile;
-      for (int64_t t = s / kEmbTile; t < t1; ++t) {
-        const float* from = a.partial + (t * 2 + (s > t * kEmbTile ? 1 : 0)) * a.hp;
-#pragma unroll
-        for (int v = 0; v < VPL; ++v) {
-          if (c0 + v * 256 >= a.H) continue;
-          const f32x4 x = *(const f32x4*)(from + c0 + v * 256);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[v][i] += x[i];
-        }
-      }
-    } else if (any) {
-      add_rows<TI, VPL>(a, lane < e - s ? a.perm[s + lane] : 0, e - s, c0, f);
-    }
+    first = a.start[v0 + (lane <= rows ? lane : rows)];
+    const int32_t past = __shfl_down(first, 1, 64);
+    some = __ballot(lane < rows && past > first);
   } else {
     for (int64_t n = 0; n < a.N; n += 64) {
-      const int32_t id = n + lane < a.N ? a.ids[n + lane] : -1;
-      uint64_t in = __ballot(id == (int32_t)v0);
+      const int64_t id = n + lane < a.N ? (int64_t)a.ids[n + lane] - v0 : -1;
+      uint64_t in = __ballot(id >= 0 && id < rows);
       while (in) {
         const int l = __ffsll((long long)in) - 1;
         in &= in - 1;
-        any = true;
-        add_rows<TI, VPL>(a, (int32_t)(n + l), 1, c0, f);
+        some |= 1ull << __builtin_amdgcn_readlane((int)id, l);
       }
     }
   }
-  if (a.accumulate && !any) return;
-  char* row = (char*)a.out + v0 * a.ldo * TO::BYTES;
+  auto out = [&](int i) { return (char*)a.out + (v0 + i) * a.ldo * TO::BYTES; };
+  if (!a.accumulate) {
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int i = 0; i < rows; ++i) {
+      if (some >> i & 1) continue;
 #pragma unroll
-  for (int v = 0; v < VPL; ++v) {
-    if (c0 + v * 256 >= a.H) continue;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[v][i] *= a.scale;
-    if (a.accumulate) {
-      float x[4];
-      load_wide<TO, 4>(row, c0 + v * 256, a.H, x);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[v][i] += x[i];
+      for (int v = 0; v < VPL; ++v)
+        if (c0 + v * 256 < a.H) store_wide<TO, 4, true>(out(i), c0 + v * 256, a.H, zero);
     }
-    store_wide<TO, 4, true>(row, c0 + v * 256, a.H, f[v]);
+  }
+#pragma unroll 1
+  while (some) {
+    const int i = __ffsll((long long)some) - 1;
+    some &= some - 1;
+    float f[VPL][4] = {};
+    if constexpr (SORTED) {
+      const int32_t s = __builtin_amdgcn_readlane(first, i);
+      const int32_t e = __builtin_amdgcn_readlane(first, i + 1);
+      if (e - s > kEmbTile) {
+        const int64_t t1 = ((int64_t)e + kEmbTile - 1) / kEmbTile;
+#pragma unroll 2
+        for (int64_t t = s / kEmbTile; t < t1; ++t) {
+          const float* from = a.partial + (t * 2 + (s > t * kEmbTile ? 1 : 0)) * a.hp;
+#pragma unroll
+          for (int v = 0; v < VPL; ++v) {
+            if (c0 + v * 256 >= a.H) continue;
+            const f32x4 x = *(const f32x4*)(from + c0 + v * 256);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[v][k] += x[k];
+          }
+        }
+      } else {
+        add_rows<TI, VPL, 4>(a, lane < e - s ? a.perm[s + lane] : 0, e - s, c0, f);
+      }
+    } else {
+      for (int64_t n = 0; n < a.N; n += 64) {
+        const int64_t id = n + lane < a.N ? (int64_t)a.ids[n + lane] - v0 : -1;
+        uint64_t in = __ballot(id == i);
+        while (in) {
+          const int l = __ffsll((long long)in) - 1;
+          in &= in - 1;
+          add_rows<TI, VPL, 1>(a, (int32_t)(n + l), 1, c0, f);
+        }
+      }
+    }
+    char* row = out(i);
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      if (c0 + v * 256 >= a.H) continue;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[v][k] *= a.scale;
+      if (a.accumulate) {
+        float x[4];
+        load_wide<TO, 4>(row, c0 + v * 256, a.H, x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[v][k] += x[k];
+      }
+      store_wide<TO, 4, true>(row, c0 + v * 256, a.H, f[v]);
+    }
   }
 }
 
-// Launches over rows (tokens, tiles, entries) in units of a row's chunk.
+// Launches over rows (tokens, tiles, groups of entries) in units of a row's chunk.
 constexpr int64_t kEmbMaxUnits = ((int64_t)1 << 32) / kEmbThreads * kEmbWaves - kEmbWaves;
 template <class Args, class F>
 hipError_t launch_units(Args a, int64_t rows, int chunk, F launch) {
@@ -302,20 +336,20 @@ hipError_t embed_t(const EmbedArgs& a, hipStream_t st) {
 
 template <class TI, class TO, int VPL>
 hipError_t embed_grad_v(const EmbedGradArgs& a, hipStream_t st) {
+  const int64_t rows = (a.V + kEmbRows - 1) / kEmbRows;
   if (!a.start)
-    return launch_units(a, a.V, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {
+    return launch_units(a, rows, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {
       hipLaunchKernelGGL((k_embed_rows<TI, TO, VPL, false>), g, dim3(kEmbThreads), 0, st, b);
     });
   hipLaunchKernelGGL(k_embed_group, dim3((unsigned)((a.V + a.keys - 1) / a.keys)),
                      dim3(kGroupThreads), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  e = launch_units(a, (a.N + kEmbTile - 1) / kEmbTile, 256 * VPL,
-                   [&](const EmbedGradArgs& b, dim3 g) {
-                     hipLaunchKernelGGL((k_embed_tiles<TI, VPL>), g, dim3(kEmbThreads), 0, st, b);
-                   });
+  e = launch_units(a, (a.N + kEmbTile - 1) / kEmbTile, 256, [&](const EmbedGradArgs& b, dim3 g) {
+    hipLaunchKernelGGL((k_embed_tiles<TI>), g, dim3(kEmbThreads), 0, st, b);
+  });
   if (e != hipSuccess) return e;
-  return launch_units(a, a.V, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {
+  return launch_units(a, rows, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {
     hipLaunchKernelGGL((k_embed_rows<TI, TO, VPL, true>), g, dim3(kEmbThreads), 0, st, b);
   });
 }

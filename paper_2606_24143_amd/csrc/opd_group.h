@@ -10,10 +10,10 @@ namespace {
 
 constexpr int kGroupThreads = 1024;
 constexpr int kGroupWaves = kGroupThreads / 64;
-constexpr int kGroupKeys = 1024;  // keys of a workgroup at most
 
+template <int KEYS>  // of a workgroup, at most
 struct GroupLds {
-  uint32_t at[kGroupWaves][kGroupKeys];  // tokens of a key in a wave's part; then where its next goes
+  uint32_t at[kGroupWaves][KEYS];  // tokens of a key in a wave's part; then where its next goes
   uint32_t sums[kGroupWaves];
   uint32_t below[kGroupWaves];
 };
@@ -45,27 +45,57 @@ __device__ __forceinline__ uint32_t block_excl_scan(uint32_t v, uint32_t* sums, 
   return before + incl - v;
 }
 
+// The lanes of `in` that hold lane's key, of `bits` bits.  Batches often lie packed, one key
+// after the other: then the first comparison is all.
+__device__ __forceinline__ uint64_t lanes_of_key(uint64_t in, int32_t k, int bits) {
+  const int32_t one = __builtin_amdgcn_readlane(k, __ffsll((long long)in) - 1);
+  if ((__ballot(k == one) & in) == in) return in;
+  uint64_t same = in;
+  for (int bit = 0; bit < bits; ++bit) {
+    const uint64_t b = __ballot(k >> bit & 1);
+    same &= k >> bit & 1 ? b : ~b;
+  }
+  return same;
+}
+
 // One workgroup sorts the tokens whose key lies in [lo, lo + count), count <=
-// kGroupKeys; key(n) of token n is < 2^31, or -1 for tokens that have no part.
+// KEYS; key(n) of token n is < 2^31, or -1 for tokens that have no part.
 // Two passes over all keys, a contiguous part of the tokens to each wave: counts
 // per wave and key, then places.  The tokens of smaller keys are counted on the
 // way, so workgroups need nothing of each other.  Writes perm for its keys;
 // returns the first place of key lo + threadIdx.x (for lanes below count) and
 // the place past the workgroup's last token.
-template <class Key>
+template <int KEYS, class Key>
 __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int count, Key key,
-                                                 int32_t* perm, GroupLds& sh, uint32_t& end) {
+                                                 int32_t* perm, GroupLds<KEYS>& sh, uint32_t& end) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int i = threadIdx.x; i < kGroupWaves * count; i += kGroupThreads)
-    sh.at[i / count][i % count] = 0;
+  const int bits = 32 - __clz(count - 1 > 0 ? count - 1 : 1);
+  if ((int)threadIdx.x < count) {
+#pragma unroll
+    for (int i = 0; i < kGroupWaves; ++i) sh.at[i][threadIdx.x] = 0;
+  }
   __syncthreads();
   const int64_t part = (N + 64 * kGroupWaves - 1) / (64 * kGroupWaves) * 64;
   const int64_t n0 = w * part, n1 = n0 + part < N ? n0 + part : N;
   uint32_t below = 0;
-  for (int64_t n = n0 + lane; n < n1; n += 64) {
-    const int32_t k = key(n);
-    if (k >= 0 && k < lo) ++below;
-    if (k >= lo && k - lo < count) atomicAdd(&sh.at[w][k - lo], 1u);
+  constexpr int A = 8;  // keys on their way at once; up to 64 A of a wave's stay in registers
+  int32_t ks[A];
+  auto load = [&](int64_t n) {
+#pragma unroll
+    for (int i = 0; i < A; ++i) ks[i] = n + 64 * i + lane < n1 ? key(n + 64 * i + lane) : -1;
+  };
+  for (int64_t n = n0; n < n1; n += 64 * A) {
+    load(n);
+#pragma unroll
+    for (int i = 0; i < A; ++i) {
+      if (ks[i] >= 0 && ks[i] < lo) ++below;
+      const int32_t k = ks[i] - lo;
+      const uint64_t in = __ballot(ks[i] >= lo && k < count);
+      if (!in) continue;
+      const uint64_t same = lanes_of_key(in, k, bits);
+      if ((in >> lane & 1) && lane == __ffsll((long long)same) - 1)
+        atomicAdd(&sh.at[w][k], (uint32_t)__popcll(same));
+    }
   }
   below = (uint32_t)__shfl((int)wave_incl_scan_u32(below), 63, 64);
   if (lane == 0) sh.below[w] = below;
@@ -91,19 +121,23 @@ __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int coun
   }
   __syncthreads();
   end = base + total;
-  // (a wave's tokens in order: 64 at a time, key by key)
-  for (int64_t n = n0; n < n1; n += 64) {
-    const int32_t k = n + lane < n1 ? key(n + lane) : -1;
-    uint64_t left = __ballot(k >= lo && k - lo < count);
-    while (left) {
-      const int lead = __ffsll((long long)left) - 1;
-      const int32_t kk = __builtin_amdgcn_readlane(k, lead);
-      const uint64_t same = __ballot(k == kk);
-      uint32_t at = 0;
-      if (lane == lead) at = atomicAdd(&sh.at[w][kk - lo], (uint32_t)__popcll(same));
-      at = (uint32_t)__builtin_amdgcn_readlane((int)at, lead);
-      if (k == kk) perm[at + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (int32_t)(n + lane);
-      left &= ~same;
+  // A wave's tokens in order, 64 at a time: a lane finds those of its key by the keys'
+  // bits, and the first of them takes their places.
+  for (int64_t m = n0; m < n1; m += 64 * A) {
+    if (part > 64 * A) load(m);
+#pragma unroll
+    for (int i = 0; i < A; ++i) {
+      const int32_t k = ks[i] - lo;
+      const uint64_t all = __ballot(ks[i] >= lo && k < count);
+      if (!all) continue;
+      const uint64_t same = lanes_of_key(all, k, bits);
+      if (all >> lane & 1) {
+        const int lead = __ffsll((long long)same) - 1;
+        uint32_t at = 0;
+        if (lane == lead) at = atomicAdd(&sh.at[w][k], (uint32_t)__popcll(same));
+        at = (uint32_t)__shfl((int)at, lead, 64) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        perm[at] = (int32_t)(m + 64 * i + lane);
+      }
     }
   }
   return first;

@@ -7,7 +7,8 @@
 namespace opd {
 
 // Token embeddings (opd_embed_tokens, opd_embed_grads).  Launches go over rows (tokens,
-// entries, tiles) times chunks of columns.
+// groups of entries, tiles) times chunks of columns.
+constexpr int kEmbKeys = 256;  // entries that a workgroup sorts, at most
 struct EmbedArgs {
   const void* table;      // [V, ld]
   int64_t V, H, ld;
@@ -88,6 +89,7 @@ struct ExpandArgs {
   void* out;              // [N, ldo]
   int64_t ldo;
   float* low_out;         // [N, r] nullable
+  uint32_t per;           // workgroups to a tile (the launch sets it)
 };
 // out[g] = scale * sum over the adapter's tokens of low^T x
 struct OuterArgs {
@@ -102,6 +104,7 @@ struct OuterArgs {
   int64_t stride;
   float* out;             // [splits][G, r, ldo]
   int64_t ldo;
+  uint32_t chunks;        // of columns (the launch sets it)
 };
 hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t stream);
 hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t stream);
