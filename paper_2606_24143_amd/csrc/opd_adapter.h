@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_adapt_plan(AdaptArgs a) {
   const int32_t* ids = a.ids;
   const int count = G + 2;
   uint32_t end;
-  const uint32_t first = group_tokens(
+  const uint32_t first = group_tokens<kAdKeys, false>(
       a.N, 0, count,
       [=](int64_t n) {
         const int32_t id = ids[n];
@@ -90,14 +90,6 @@ __global__ void __launch_bounds__(kGroupThreads) k_adapt_plan(AdaptArgs a) {
 
 // ---------------------------------------------------------------- loads
 
-// 16 bytes of a row from column c on, which is a multiple of theirs; 0 from `end` on.  (Of
-// 16 that the row ends in, those past it are read too: they lie in the same 16.)
-template <class T>
-__device__ __forceinline__ u32x4 load16(const char* row, int64_t c, int64_t end) {
-  u32x4 r = {0, 0, 0, 0};
-  if (c < end) r = *(const u32x4*)(row + c * T::BYTES);
-  return r;
-}
 // Columns at or past `end` of those from c on become 0.
 template <class T>
 __device__ __forceinline__ u32x4 cut16(u32x4 r, int64_t c, int64_t end) {
@@ -115,40 +107,10 @@ __device__ __forceinline__ u32x4 cut16(u32x4 r, int64_t c, int64_t end) {
   }
   return r;
 }
-// Four elements widened to fp32; the same.
-template <class T>
-__device__ __forceinline__ f32x4 load4_wide(const char* row, int64_t c, int64_t end) {
-  f32x4 f = {0.f, 0.f, 0.f, 0.f};
-  if (c < end) {
-    if constexpr (T::BYTES == 2) {
-      const u32x2 x = *(const u32x2*)(row + c * 2);
-#pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        f[2 * d] = __uint_as_float(x[d] << 16);
-        f[2 * d + 1] = __uint_as_float(x[d] & 0xFFFF0000u);
-      }
-    } else {
-      f = *(const f32x4*)(row + c * 4);
-    }
-  }
-  return f;
-}
 __device__ __forceinline__ f32x4 cut4(f32x4 f, int64_t c, int64_t end) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) f[e] = c + e < end ? f[e] : 0.f;
   return f;
-}
-
-// In: row t of an 8 by 8 block of bf16 (16 bytes).  Out: column j, of all eight rows.
-__device__ __forceinline__ void transpose8(const u32x4 (&in)[8], u32x4 (&out)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      const uint32_t lo = in[2 * d][j / 2], hi = in[2 * d + 1][j / 2];
-      out[j][d] = __builtin_amdgcn_perm(hi, lo, j & 1 ? 0x07060302u : 0x05040100u);
-    }
-  }
 }
 
 __device__ __forceinline__ f32x4 mma_bf16(u32x4 a, u32x4 b, f32x4 c) {
@@ -193,16 +155,43 @@ __device__ __forceinline__ float low_value(const LowRef& t, int64_t token, int c
 // ---------------------------------------------------------------- tokens times the rows
 
 // One workgroup to 16 MT tokens of an adapter and a part of the long axis: its waves
-// take steps of 64 (bf16) or 32 (fp32) columns in turn, the next one on its way meanwhile,
-// and their sums are added in order.  RT: ranks / 16.
+// take steps of 64 (bf16) or 32 (fp32) columns in turn, the next ones on their way meanwhile,
+// and their sums are added in order.  A lane's operands lie along a row, and its
+// neighbours' in other rows: loaded so, an instruction touches 16 lines 16 bytes at a time,
+// which took 42 us for 8,192 tokens by 4,096 columns and 32 ranks where TIME_LDS are needed with
+// rows read as they lie and turned in LDS, a part of it to each wave.  RT: ranks / 16.
 constexpr int kLowThreads = 512;
 constexpr int kLowWaves = kLowThreads / 64;
+
+// ROWS rows of a step (128 bytes each, or 64), by a wave: as they lie in memory, and in LDS,
+// where the 16-byte pieces of a row are rotated so that the same piece of eight rows
+// lies in different banks.
+template <int ROWS, int ROW_BYTES>
+struct Staged {
+  static constexpr int P = ROW_BYTES / 16, PER = 64 / P;  // pieces of a row, rows of an instruction
+  static constexpr int N = ROWS / PER;
+  u32x4 v[N];
+  static __device__ __forceinline__ int row(int i) { return i * PER + (threadIdx.x & 63) / P; }
+  static __device__ __forceinline__ int piece() { return (threadIdx.x & 63) % P; }
+  static __device__ __forceinline__ int slot(int row, int p) { return row * P + (p ^ (row & (P - 1))); }
+  __device__ __forceinline__ void put(u32x4* lds) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds[slot(row(i), piece())] = v[i];
+  }
+};
+
 template <class TX, class TW, int RT, int MT>
-__global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
+__global__ void __launch_bounds__(kLowThreads, 2) k_low(LowArgs a) {
   constexpr bool BF = TX::BYTES == 2 && TW::BYTES == 2;
   constexpr int STEP = BF ? 64 : 32;
   typedef std::conditional_t<BF, u32x4, f32x4> V;
-  __shared__ float sums[kLowWaves][16 * MT][RT * 16 + 1];
+  typedef Staged<16 * MT, STEP * TX::BYTES> SX;
+  typedef Staged<16 * RT, STEP * TW::BYTES> SW;
+  constexpr int XV = 16 * MT * SX::P, WV = 16 * RT * SW::P;  // 16-byte vectors of a wave's step
+  constexpr int SUM = 16 * MT * (RT * 16 + 1);
+  constexpr int AHEAD = RT <= 2 ? 3 : RT <= 4 ? 2 : 1;  // steps on their way
+  constexpr int EACH = (XV + WV) * 4 > SUM ? (XV + WV) * 4 : (SUM + 3) / 4 * 4;
+  __shared__ __align__(16) float lds[kLowWaves][EACH];
   constexpr int SUBS = kAdTile / (16 * MT);
   const int sub = blockIdx.x % SUBS * (16 * MT);
   const AdTile tile = a.tiles[blockIdx.x / SUBS];
@@ -211,11 +200,15 @@ __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int count = min(16 * MT, tile.count - sub);
   const int32_t* perm = a.perm + tile.pos + sub;
-  const char* x[MT];
+  u32x4* const lx = (u32x4*)lds[wave];
+  u32x4* const lw = lx + XV;
+  const char* x[SX::N];
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-    x[i] = (const char*)a.x + (int64_t)perm[min(16 * i + m, count - 1)] * a.ldx * TX::BYTES;
-  const char* w = (const char*)a.w + ((int64_t)tile.key * a.r + m) * a.ldw * TW::BYTES;
+  for (int i = 0; i < SX::N; ++i)
+    x[i] = (const char*)a.x + (int64_t)perm[min(SX::row(i), count - 1)] * a.ldx * TX::BYTES +
+           SX::piece() * 16;
+  const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES + SW::piece() * 16;
+  const uint32_t ldw = (uint32_t)a.ldw * TW::BYTES;
   f32x4 acc[MT][RT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
@@ -224,37 +217,50 @@ __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
   }
   const int64_t d0 = (int64_t)blockIdx.y * a.span;
   const int64_t d1 = d0 + a.span < a.D ? d0 + a.span : a.D;
-  // Two instructions' worth of both operands: columns d + 16 q .. + 16 (bf16) or d + 8 q ..
-  // + 8, 32 consecutive bytes of a lane's rows.
   struct Step {
-    V x[MT][2], w[RT][2];
+    SX x;
+    SW w;
   };
+  // (No load depends on a condition, since the compiler waits for all where it can't count
+  // them: pieces past the end are the last one again, ranks past r the last rank.)
+  const int64_t ex = d1 - SX::piece() * (16 / TX::BYTES) - 1, ew = d1 - SW::piece() * (16 / TW::BYTES) - 1;
+  uint32_t row[SW::N];
+#pragma unroll
+  for (int i = 0; i < SW::N; ++i) row[i] = (uint32_t)min(SW::row(i), a.r - 1) * ldw;
   auto load = [&](Step& s, int64_t d) {
-    const int64_t c = d + STEP / 4 * q;
+    // (whole pieces from d on: the last that begins before the end, or the row's first)
+    int64_t dx = min(d, ex / (16 / TX::BYTES) * (16 / TX::BYTES));
+    int64_t dw = min(d, ew / (16 / TW::BYTES) * (16 / TW::BYTES));
+    dx = (dx < 0 ? -(int64_t)SX::piece() * (16 / TX::BYTES) : dx) * TX::BYTES;
+    dw = (dw < 0 ? -(int64_t)SW::piece() * (16 / TW::BYTES) : dw) * TW::BYTES;
+#pragma unroll
+    for (int i = 0; i < SX::N; ++i) s.x.v[i] = *(const u32x4*)(x[i] + dx);
+#pragma unroll
+    for (int i = 0; i < SW::N; ++i) s.w.v[i] = *(const u32x4*)(w + dw + row[i]);
+  };
+  // Two instructions' worth of both operands: columns d + 16 q .. + 16 (bf16) or d + 8 q ..
+  // + 8, of row m.
+  auto add = [&](int64_t d) {
+    if (d >= d1) return;
+    V xv[MT][2], wv[RT][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        if constexpr (BF)
-          s.x[i][h] = load16<TX>(x[i], c + 8 * h, d1);
-        else
-          s.x[i][h] = load4_wide<TX>(x[i], c + 4 * h, d1);
-      }
+      for (int i = 0; i < MT; ++i)
+        xv[i][h] = __builtin_bit_cast(V, lx[SX::slot(16 * i + m, 2 * q + h)]);
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        s.w[t][h] = V{0, 0, 0, 0};
-        if (16 * t + m < a.r) {
-          const char* row = w + (int64_t)t * 16 * a.ldw * TW::BYTES;
-          if constexpr (BF)
-            s.w[t][h] = load16<TW>(row, c + 8 * h, d1);
-          else
-            s.w[t][h] = load4_wide<TW>(row, c + 4 * h, d1);
+        if constexpr (SW::P == 8) {
+          wv[t][h] = __builtin_bit_cast(V, lw[SW::slot(16 * t + m, 2 * q + h)]);
+        } else {
+          const u32x4 v = lw[SW::slot(16 * t + m, q)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            wv[t][h][e] = __uint_as_float(e & 1 ? v[2 * h + e / 2] & 0xFFFF0000u
+                                                : v[2 * h + e / 2] << 16);
         }
       }
     }
-  };
-  auto add = [&](Step& s, int64_t d) {
-    if (d >= d1) return;
     if (d + STEP > d1) {  // (what lies past the row's end may be anything)
       const int64_t c = d + STEP / 4 * q;
 #pragma unroll
@@ -262,16 +268,16 @@ __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           if constexpr (BF)
-            s.x[i][h] = cut16<TX>(s.x[i][h], c + 8 * h, d1);
+            xv[i][h] = cut16<TX>(xv[i][h], c + 8 * h, d1);
           else
-            s.x[i][h] = cut4(s.x[i][h], c + 4 * h, d1);
+            xv[i][h] = cut4(xv[i][h], c + 4 * h, d1);
         }
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           if constexpr (BF)
-            s.w[t][h] = cut16<TW>(s.w[t][h], c + 8 * h, d1);
+            wv[t][h] = cut16<TW>(wv[t][h], c + 8 * h, d1);
           else
-            s.w[t][h] = cut4(s.w[t][h], c + 4 * h, d1);
+            wv[t][h] = cut4(wv[t][h], c + 4 * h, d1);
         }
       }
     }
@@ -281,7 +287,7 @@ __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
 #pragma unroll
-          for (int i = 0; i < MT; ++i) acc[i][t] = mma_bf16(s.x[i][h], s.w[t][h], acc[i][t]);
+          for (int i = 0; i < MT; ++i) acc[i][t] = mma_bf16(xv[i][h], wv[t][h], acc[i][t]);
         }
       } else {
 #pragma unroll
@@ -289,8 +295,7 @@ __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-              acc[i][t] = mma_f32(s.x[i][h][e], s.w[t][h][e], acc[i][t]);
+            for (int i = 0; i < MT; ++i) acc[i][t] = mma_f32(xv[i][h][e], wv[t][h][e], acc[i][t]);
           }
         }
       }
@@ -301,52 +306,57 @@ __global__ void __launch_bounds__(kLowThreads) k_low(LowArgs a) {
   // another step, and goes round.
   constexpr int NEXT = kLowWaves * STEP;
   const int steps = (int)((d1 - d0 + NEXT - 1) / NEXT);
-  int at = (int)(blockIdx.x % (uint32_t)steps);
-  auto column = [&]() {
+  int at = (int)(blockIdx.x % (uint32_t)steps), to = at;
+  auto column = [&](int& at) {
     const int64_t d = d0 + (int64_t)at * NEXT + wave * STEP;
     at = at + 1 == steps ? 0 : at + 1;
     return d;
   };
-  {
-    Step s, t;
-    int64_t ds = column(), dt = 0;
-    load(s, ds);
-    int left = steps;
+  Step s[AHEAD];
+  auto use = [&](Step& s) {
+    s.x.put(lx);
+    s.w.put(lw);
+  };
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) load(s[j], column(to));
+  int left = steps;
 #pragma unroll 1
-    for (; left > 2; left -= 2) {
-      load(t, dt = column());
-      add(s, ds);
-      load(s, ds = column());
-      add(t, dt);
+  for (; left > AHEAD; left -= AHEAD) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      use(s[j]);
+      load(s[j], column(to));
+      add(column(at));
     }
-    if (left == 2) load(t, dt = column());
-    add(s, ds);
-    if (left == 2) add(t, dt);
   }
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) {
+    if (j >= left) continue;
+    use(s[j]);
+    add(column(at));
+  }
+  __syncthreads();
+  auto sums = [&](int v, int n, int c) -> float& { return lds[v][n * (RT * 16 + 1) + c]; };
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sums[wave][16 * i + 4 * q + e][16 * t + m] = acc[i][t][e];
+      for (int e = 0; e < 4; ++e) sums(wave, 16 * i + 4 * q + e, 16 * t + m) = acc[i][t][e];
     }
   }
   __syncthreads();
   float* out = a.out + (int64_t)blockIdx.y * a.stride;
   for (int i = threadIdx.x; i < count * a.r; i += kLowThreads) {
     const int n = i / a.r, c = i % a.r;
-    float f = sums[0][n][c];
+    float f = sums(0, n, c);
 #pragma unroll
-    for (int v = 1; v < kLowWaves; ++v) f += sums[v][n][c];
+    for (int v = 1; v < kLowWaves; ++v) f += sums(v, n, c);
     out[(int64_t)perm[n] * a.ldo + c] = f;
   }
 }
 
 // ---------------------------------------------------------------- the r numbers times the rows
-
-// Columns of a wave's tile: lane m = 4 i + j of an operand has the columns of piece
-// 4 j + i, so that the four lanes that hold a token's results hold consecutive pieces.
-__device__ __forceinline__ int piece(int m) { return (m & 3) * 4 + (m >> 2); }
 
 constexpr int kExpThreads = 256;
 constexpr int kExpWaves = kExpThreads / 64;
@@ -397,18 +407,19 @@ __device__ __forceinline__ void store_values(char* row, int64_t c, int64_t end, 
 // 4 waves' columns (128 each, or 64 of fp32 rows): a wave keeps its columns of the
 // adapter in registers and passes over the tokens, 16 at a time.  The shared projection's
 // values are what the sums start from, and become the results in place.  The next 16
-// tokens' are on their way meanwhile, and, up to 16 ranks, the next columns of the adapter.
-// KL: ranks of a lane's operand (bf16: 4 or 8); RB: of 4 KL ranks each.
-template <class TW, class TY, int KL, int RB>
+// tokens' are on their way meanwhile (no load in a loop depends on a condition, since the
+// compiler waits for all where it can't count them); where there are no more than 16, of up
+// to 16 ranks, the next columns of the adapter too.
+// KL: ranks of a lane's operand (bf16: 4 or 8); RB: of 4 KL ranks each; READ: there is a base.
+template <class TW, class TY, int KL, int RB, bool READ>
 __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(ExpandArgs a) {
   constexpr bool BF = TW::BYTES == 2;
-  constexpr int E = BF ? 8 : 4;          // columns of a piece
+  constexpr int E = BF ? 8 : 4;          // columns of a lane
   constexpr int S = 16 / TY::BYTES;      // of a vector of the result
   constexpr int TERMS = TY::BYTES == 2 ? 2 : 3;
   constexpr int K = 4 * KL * RB;         // ranks
   constexpr int KP = BF ? K + 8 : K + 4; // (padded: lanes of a read spread over the banks)
   constexpr int WV = KL * RB;            // 16-byte vectors of the adapter to a lane
-  constexpr bool AHEAD = WV <= 4;
   __shared__ __align__(16) uint16_t part[BF ? TERMS : 1][BF ? kAdTile : 1][KP];
   __shared__ float wide[BF ? 1 : kAdTile][BF ? 1 : KP];
   __shared__ int32_t tokens[kAdTile];
@@ -419,197 +430,227 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t* perm = a.perm + tile.pos;
-  const bool live = tile.key < a.G;
-  if (!live && tile.key == a.G && a.base == a.out) return;  // in place: as it is
-  const int64_t span = kExpWaves * 16 * E;
+  const int64_t span = kExpWaves * 16 * E, step = a.per * span;
   int64_t c0 = (int64_t)chunk * span + wave * (16 * E);
-  const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES;
-  const uint32_t ldw = (uint32_t)a.ldw * TW::BYTES;
-  // a wave's columns of the adapter, as they lie: ranks KL q + i of each 4 KL (fp32: 4 i + q)
-  auto load_w = [&](int64_t c0, u32x4 (&v)[WV]) {
-    const int64_t c = c0 + piece(m) * E;
-#pragma unroll
-    for (int k = 0; k < WV; ++k) {
-      const int rank = BF ? 4 * KL * (k / KL) + KL * q + k % KL : 4 * k + q;
-      v[k] = u32x4{0, 0, 0, 0};
-      if (rank < a.r && c < a.D)
-        v[k] = *(const u32x4*)(w + ((uint32_t)rank * ldw + (uint32_t)c * TW::BYTES));
-    }
-  };
-  u32x4 v[WV];
-  if (AHEAD && live) load_w(c0, v);
   if ((int)threadIdx.x < kAdTile)
     tokens[threadIdx.x] = perm[min((int)threadIdx.x, tile.count - 1)];
-  if (live) {
-    const float scale = a.scales ? a.scales[tile.key] : 1.f;
-    for (int i = threadIdx.x; i < kAdTile * K; i += kExpThreads) {
-      const int n = i / K, k = i % K;
-      float f = 0.f;
-      if (n < tile.count && k < a.r) {
-        const int64_t token = perm[n];
-        f = low_value(a.low, token, k);
-        if (a.low_out && chunk == 0) a.low_out[token * a.r + k] = f;
-        f *= scale;
-      }
-      if constexpr (BF) {
-        uint16_t p[TERMS];
-        split_bf16<TERMS>(f, p);
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) part[t][n][k] = p[t];
-      } else {
-        wide[n][k] = f;
-      }
-    }
-  } else if (a.low_out && chunk == 0) {
-    for (int i = threadIdx.x; i < tile.count * a.r; i += kExpThreads)
-      a.low_out[(int64_t)perm[i / a.r] * a.r + i % a.r] =
-          tile.key == a.G ? 0.f : __builtin_nanf("");
-  }
-  __syncthreads();
-  // pieces 4 i + q of the wave's columns, of token n0 + m
-  const bool read = a.base && tile.key <= a.G;
-  auto load_y = [&](int64_t c0, int n0, u32x4 (&y)[4][E / S]) {
-    const char* row = (const char*)a.base + (int64_t)tokens[n0 + m] * a.ldb * TY::BYTES +
-                      (c0 + q * E) * TY::BYTES;
+  typedef u32x4 Y[4][E / S];
+  // columns c0 + m E .. of the wave's, of tokens n0 + 4 q + i: a token's results lie side by
+  // side in 16 lanes.  (Past the row's end: its last vector again.)
+  const int64_t end = (a.D - 1) / S * S;
+  auto load_y = [&](int64_t c0, int n0, Y& y) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      const char* row = (const char*)a.base + (int64_t)tokens[n0 + 4 * q + i] * a.ldb * TY::BYTES;
 #pragma unroll
       for (int h = 0; h < E / S; ++h) {
-        y[i][h] = u32x4{0, 0, 0, 0};
-        if (c0 + (4 * i + q) * E + S * h < a.D)
-          y[i][h] = *(const u32x4*)(row + (4 * i * E + S * h) * TY::BYTES);
+        if constexpr (READ)
+          y[i][h] = *(const u32x4*)(row + min(c0 + m * E + S * h, end) * TY::BYTES);
+        else
+          y[i][h] = u32x4{0, 0, 0, 0};
       }
     }
   };
-  u32x4 next[4][E / S];
-  if (read) {
-    load_y(c0, 0, next);
-  } else {
+  auto store_y = [&](int64_t c0, int n0, const Y& y) {
+    const bool whole = c0 + 16 * E <= a.D;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      const int n = n0 + 4 * q + i;
+      if (n >= tile.count) continue;
+      char* row = (char*)a.out + (int64_t)tokens[n] * a.ldo * TY::BYTES + (c0 + m * E) * TY::BYTES;
 #pragma unroll
-      for (int h = 0; h < E / S; ++h) next[i][h] = u32x4{0, 0, 0, 0};
+      for (int h = 0; h < E / S; ++h) {
+        if (whole)
+          *(u32x4*)(row + 16 * h) = y[i][h];
+        else
+          store_end<TY>(row + 16 * h, y[i][h], a.D - (c0 + m * E + S * h));
+      }
     }
-  }
+  };
+  if (tile.key >= a.G) {  // no adapter (the base as it is), or a bad id (NaN)
+    if (a.low_out && chunk == 0) {
+      for (int i = threadIdx.x; i < tile.count * a.r; i += kExpThreads)
+        a.low_out[(int64_t)perm[i / a.r] * a.r + i % a.r] =
+            tile.key == a.G ? 0.f : __builtin_nanf("");
+    }
+    if (tile.key == a.G && a.base == a.out) return;  // in place
+    __syncthreads();
+    for (; c0 < a.D; c0 += step) {
 #pragma unroll 1
-  for (;;) {
-    const int64_t c1 = c0 + a.per * span;
-    // the operand: for column j of a piece, a lane's KL ranks
-    uint32_t wb[RB][BF ? 8 : 1][BF ? KL / 2 : 1];
-    f32x4 wf[BF ? 1 : WV];
-    if (live) {
-      if (!AHEAD) load_w(c0, v);
-      if constexpr (BF) {
+      for (int n0 = 0; n0 < tile.count; n0 += 16) {
+        Y y;
+        load_y(c0, n0, y);
+        constexpr uint32_t nan = TY::BYTES == 2 ? 0x7FC07FC0u : 0x7FC00000u;
+        if (tile.key > a.G) {
 #pragma unroll
-        for (int k = 0; k < RB; ++k) {
+          for (int i = 0; i < 4; ++i) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-#pragma unroll
-            for (int d = 0; d < KL / 2; ++d)
-              wb[k][j][d] = __builtin_amdgcn_perm(v[KL * k + 2 * d + 1][j / 2],
-                                                  v[KL * k + 2 * d][j / 2],
-                                                  j & 1 ? 0x07060302u : 0x05040100u);
+            for (int h = 0; h < E / S; ++h) y[i][h] = u32x4{nan, nan, nan, nan};
           }
         }
-      } else {
-#pragma unroll
-        for (int k = 0; k < WV; ++k) wf[k] = __builtin_bit_cast(f32x4, v[k]);
+        store_y(c0, n0, y);
       }
-      if (AHEAD && c1 < a.D) load_w(c1, v);
     }
-    const bool whole = c0 + 16 * E <= a.D;
+    return;
+  }
+  const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES;
+  const uint32_t ldw = (uint32_t)a.ldw * TW::BYTES;
+  const int64_t wend = (a.D - 1) / E * E;
+  // a wave's columns of the adapter, as they lie, 4 KL ranks at a time: ranks KL q + i (fp32:
+  // 4 i + q; past r: the last one again)
+  typedef u32x4 W[KL];
+  auto rank = [&](int k, int i) { return 4 * KL * k + (BF ? KL * q + i : 4 * i + q); };
+  auto load_w = [&](int64_t c0, int k, W& v) {
+    const uint32_t c = (uint32_t)min(c0 + m * E, wend) * TW::BYTES;
+#pragma unroll
+    for (int i = 0; i < KL; ++i)
+      v[i] = *(const u32x4*)(w + ((uint32_t)min(rank(k, i), a.r - 1) * ldw + c));
+  };
+  // the operand: for column j of a lane, its KL ranks
+  struct Operand {
+    uint32_t b[BF ? RB : 1][8][BF ? KL / 2 : 1];
+    f32x4 f[BF ? 1 : WV];
+  };
+  auto operand = [&](int k, W& v, Operand& o) {
+    if (a.r < K) {
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) v[i][d] = rank(k, i) < a.r ? v[i][d] : 0u;
+      }
+    }
+    if constexpr (BF) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+#pragma unroll
+        for (int d = 0; d < KL / 2; ++d)
+          o.b[k][j][d] = __builtin_amdgcn_perm(v[2 * d + 1][j / 2], v[2 * d][j / 2],
+                                               j & 1 ? 0x07060302u : 0x05040100u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < KL; ++i) o.f[KL * k + i] = __builtin_bit_cast(f32x4, v[i]);
+    }
+  };
+  auto product = [&](const Operand& o, int n0, int j, f32x4 acc) {
+    if constexpr (BF) {
+#pragma unroll
+      for (int k = 0; k < RB; ++k) {
+#pragma unroll
+        for (int t = TERMS - 1; t >= 0; --t) {
+          const uint16_t* low = &part[t][n0 + m][4 * KL * k + KL * q];
+          if constexpr (KL == 8)
+            acc = mma_bf16(*(const u32x4*)low,
+                           u32x4{o.b[k][j][0], o.b[k][j][1], o.b[k][j][2], o.b[k][j][3]}, acc);
+          else
+            acc = mma_bf16_16(*(const u32x2*)low, u32x2{o.b[k][j][0], o.b[k][j][1]}, acc);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < WV; ++k) acc = mma_f32(wide[n0 + m][4 * k + q], o.f[k][j], acc);
+    }
+    return acc;
+  };
+  auto update = [&](const Operand& o, int n0, Y& y) {
+    if constexpr (TY::BYTES == 2) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        f32x4 lo, hi;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          lo[i] = __uint_as_float(y[i][0][d] << 16);
+          hi[i] = __uint_as_float(y[i][0][d] & 0xFFFF0000u);
+        }
+        lo = product(o, n0, 2 * d, lo);
+        hi = product(o, n0, 2 * d + 1, hi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i][0][d] = pack_bf16x2(lo[i], hi[i]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        f32x4 acc;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = __uint_as_float(y[i][j / 4][j % 4]);
+        acc = product(o, n0, j, acc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i][j / 4][j % 4] = __float_as_uint(acc[i]);
+      }
+    }
+  };
+  W v;
+  load_w(c0, 0, v);
+  const float scale = a.scales ? a.scales[tile.key] : 1.f;
+  for (int i = threadIdx.x; i < kAdTile * K; i += kExpThreads) {
+    const int n = i / K, k = i % K;
+    float f = 0.f;
+    if (n < tile.count && k < a.r) {
+      const int64_t token = perm[n];
+      f = low_value(a.low, token, k);
+      if (a.low_out && chunk == 0) a.low_out[token * a.r + k] = f;
+      f *= scale;
+    }
+    if constexpr (BF) {
+      uint16_t p[TERMS];
+      split_bf16<TERMS>(f, p);
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) part[t][n][k] = p[t];
+    } else {
+      wide[n][k] = f;
+    }
+  }
+  __syncthreads();
+  Y y, z;
+  Operand o;
+  if (KL == 4 && tile.count <= 16) {
+    load_y(c0, 0, y);
 #pragma unroll 1
-    for (int n0 = 0; n0 < tile.count; n0 += 16) {
-      u32x4 y[4][E / S];
+    for (; c0 + step < a.D; c0 += step) {
+      operand(0, v, o);
+      load_w(c0 + step, 0, v);
+      load_y(c0 + step, 0, z);
+      update(o, 0, y);
+      store_y(c0, 0, y);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int h = 0; h < E / S; ++h) y[i][h] = next[i][h];
-      }
-      if (read) {
-        if (n0 + 16 < tile.count)
-          load_y(c0, n0 + 16, next);
-        else if (c1 < a.D)
-          load_y(c1, 0, next);
-      }
-      if (live) {
-        auto product = [&](int j, f32x4 acc) {
-          if constexpr (BF) {
-#pragma unroll
-            for (int k = 0; k < RB; ++k) {
-#pragma unroll
-              for (int t = TERMS - 1; t >= 0; --t) {
-                const uint16_t* low = &part[t][n0 + m][4 * KL * k + KL * q];
-                if constexpr (KL == 8) {
-                  acc = mma_bf16(u32x4{wb[k][j][0], wb[k][j][1], wb[k][j][2], wb[k][j][3]},
-                                 *(const u32x4*)low, acc);
-                } else {
-                  acc = mma_bf16_16(u32x2{wb[k][j][0], wb[k][j][1]}, *(const u32x2*)low, acc);
-                }
-              }
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < WV; ++k) acc = mma_f32(wf[k][j], wide[n0 + m][4 * k + q], acc);
-          }
-          return acc;
-        };
-        if constexpr (TY::BYTES == 2) {
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            f32x4 lo, hi;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              lo[i] = __uint_as_float(y[i][0][d] << 16);
-              hi[i] = __uint_as_float(y[i][0][d] & 0xFFFF0000u);
-            }
-            lo = product(2 * d, lo);
-            hi = product(2 * d + 1, hi);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i][0][d] = pack_bf16x2(lo[i], hi[i]);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < E; ++j) {
-            f32x4 acc;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] = __uint_as_float(y[i][j / 4][j % 4]);
-            acc = product(j, acc);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i][j / 4][j % 4] = __float_as_uint(acc[i]);
-          }
-        }
-      } else if (tile.key > a.G) {
-        constexpr uint32_t nan = TY::BYTES == 2 ? 0x7FC07FC0u : 0x7FC00000u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-          for (int h = 0; h < E / S; ++h) y[i][h] = u32x4{nan, nan, nan, nan};
-        }
-      }
-      if (n0 + m < tile.count) {
-        char* row = (char*)a.out + (int64_t)tokens[n0 + m] * a.ldo * TY::BYTES +
-                    (c0 + q * E) * TY::BYTES;
-        if (whole) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int h = 0; h < E / S; ++h)
-              *(u32x4*)(row + (4 * i * E + S * h) * TY::BYTES) = y[i][h];
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int h = 0; h < E / S; ++h)
-              store_end<TY>(row + (4 * i * E + S * h) * TY::BYTES, y[i][h],
-                            a.D - (c0 + (4 * i + q) * E + S * h));
-          }
-        }
+        for (int h = 0; h < E / S; ++h) y[i][h] = z[i][h];
       }
     }
-    if (c1 >= a.D) return;
-    c0 = c1;
+    if (c0 >= a.D) return;
+    operand(0, v, o);
+    update(o, 0, y);
+    store_y(c0, 0, y);
+    return;
+  }
+#pragma unroll 1
+  for (;;) {
+    load_y(c0, 0, y);
+    operand(0, v, o);
+#pragma unroll
+    for (int k = 1; k < RB; ++k) {
+      __builtin_amdgcn_sched_barrier(0);  // (all at once do not fit the registers)
+      load_w(c0, k, v);
+      operand(k, v, o);
+    }
+    int n0 = 0;
+#pragma unroll 1
+    for (; n0 + 16 < tile.count; n0 += 16) {
+      load_y(c0, n0 + 16, z);
+      update(o, n0, y);
+      store_y(c0, n0, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int h = 0; h < E / S; ++h) y[i][h] = z[i][h];
+      }
+    }
+    update(o, n0, y);
+    store_y(c0, n0, y);
+    c0 += step;
+    if (c0 >= a.D) return;
+    load_w(c0, 0, v);
   }
 }
 
@@ -623,7 +664,7 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
 constexpr int kOutThreads = 512;
 constexpr int kOutWaves = kOutThreads / 64;
 template <class TX, int RT>
-__global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
+__global__ void __launch_bounds__(kOutThreads, 2) k_outer(OuterArgs a) {
   constexpr bool BF = TX::BYTES == 2;
   constexpr int E = BF ? 8 : 4;
   constexpr int TERMS = 3;
@@ -638,7 +679,7 @@ __global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
   const int r0 = blockIdx.y * (RT * 16);
   const int64_t c0 = (int64_t)(blockIdx.x % a.chunks) * C;
   const int32_t s = a.start[g], count = a.start[g + 1] - s;
-  const int64_t c = c0 + piece(m) * E;
+  const int64_t c = c0 + m * E;
   const float scale = a.scales ? a.scales[g] : 1.f;
   f32x4 acc[E][RT];
 #pragma unroll
@@ -646,43 +687,61 @@ __global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // token of a lane's i-th row: 8 q + i of the block (fp32: 4 i + q)
+  // token of a lane's i-th row: 8 q + i of the block (fp32: 4 i + q).  (No load depends on a
+  // condition: past the last token it is that one again, past r or D the last rank and
+  // columns.)
   auto at = [&](int i) { return BF ? 8 * q + i : 4 * i + q; };
+  const int64_t cx = min(c, (a.D - 1) / E * E) * TX::BYTES;
+  int cl[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) cl[t] = min(r0 + 16 * t + m, a.r - 1);
   auto load = [&](int32_t n0, u32x4 (&x)[8], float (&low)[RT][8]) {
-    const int here = count - n0;
-    const int32_t mine = (lane & 31) < here ? a.perm[s + n0 + (lane & 31)] : 0;
+    const int32_t mine = a.perm[s + min(n0 + (lane & 31), count - 1)];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t token = __shfl(mine, at(i), 64);
-      x[i] = u32x4{0, 0, 0, 0};
+      x[i] = *(const u32x4*)((const char*)a.x + token * a.ldx * TX::BYTES + cx);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) low[t][i] = 0.f;
-      if (at(i) < here) {
-        x[i] = load16<TX>((const char*)a.x + token * a.ldx * TX::BYTES, c, a.D);
+      for (int t = 0; t < RT; ++t) low[t][i] = a.low.p[token * a.low.ld + cl[t]];
+    }
+  };
+  auto cut = [&](int32_t n0, u32x4 (&x)[8], float (&low)[RT][8]) {
+    if (count - n0 >= 32) return;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) low[t][i] = low_value(a.low, token, r0 + 16 * t + m);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const bool in = n0 + at(i) < count;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) x[i][d] = in ? x[i][d] : 0u;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) low[t][i] = in ? low[t][i] : 0.f;
     }
   };
   auto add = [&](const u32x4 (&x)[8], const float (&low)[RT][8]) {
     if constexpr (BF) {
-      u32x4 v[8];
-      transpose8(x, v);
+      u32x4 p[RT][TERMS];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        u32x4 p[TERMS];
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
           uint16_t lo[TERMS], hi[TERMS];
           split_bf16<TERMS>(scale * low[t][i], lo);
           split_bf16<TERMS>(scale * low[t][i + 1], hi);
 #pragma unroll
-          for (int k = 0; k < TERMS; ++k) p[k][i / 2] = lo[k] | (uint32_t)hi[k] << 16;
+          for (int k = 0; k < TERMS; ++k) p[t][k][i / 2] = lo[k] | (uint32_t)hi[k] << 16;
         }
+      }
+      // (the 8 by 8 block column by column)
 #pragma unroll
-        for (int k = TERMS - 1; k >= 0; --k) {
+      for (int j = 0; j < E; ++j) {
+        u32x4 v;
 #pragma unroll
-          for (int j = 0; j < E; ++j) acc[j][t] = mma_bf16(v[j], p[k], acc[j][t]);
+        for (int d = 0; d < 4; ++d)
+          v[d] = __builtin_amdgcn_perm(x[2 * d + 1][j / 2], x[2 * d][j / 2],
+                                       j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+          for (int k = TERMS - 1; k >= 0; --k) acc[j][t] = mma_bf16(v, p[t][k], acc[j][t]);
         }
       }
     } else {
@@ -725,16 +784,17 @@ __global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
         load(n0 + step, x, low);
       }
     }
+    cut(n0, x, low);
     add(x, low);
   }
-  // lane m holds rank m of each 16, piece 4 i + q of the columns
+  // lane m holds rank m of each 16, columns (4 q + i) E + j
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     if (t > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) sums[wave][m][(4 * i + q) * E + j] = acc[j][t][i];
+      for (int j = 0; j < E; ++j) sums[wave][m][(4 * q + i) * E + j] = acc[j][t][i];
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * C / 4; i += kOutThreads) {
@@ -751,6 +811,15 @@ __global__ void __launch_bounds__(kOutThreads) k_outer(OuterArgs a) {
       store_values<InF32, 4>((char*)out, c0 + at, a.D, f);
     }
   }
+}
+
+// The parts of t or u, added in order.
+__global__ void __launch_bounds__(256) k_low_sum(LowArgs a, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float f = a.out[i];
+  for (int s = 1; s < a.splits; ++s) f += a.out[(int64_t)s * a.stride + i];
+  a.out[i] = f;
 }
 
 // The parts of da or db, added in order.
@@ -794,19 +863,23 @@ hipError_t expand_t(ExpandArgs a, hipStream_t st) {
   const int64_t span = kExpWaves * 16 * (TW::BYTES == 2 ? 8 : 4);
   const int64_t chunks = (a.D + span - 1) / span;
   // about as many workgroups as stay on the GPU at once
-  int64_t per = 2048 / a.max_tiles;
+  int64_t per = 1024 / a.max_tiles;
   a.per = (uint32_t)(per < 1 ? 1 : per < chunks ? per : chunks);
   const dim3 grid((unsigned)(a.max_tiles * a.per));
-#define OPD_EXPAND(KL, RB) \
-  hipLaunchKernelGGL((k_expand<TW, TY, KL, RB>), grid, dim3(kExpThreads), 0, st, a)
-  if (a.r <= 16)
+#define OPD_EXPAND(KL, RB)                                                                \
+  if (a.base)                                                                             \
+    hipLaunchKernelGGL((k_expand<TW, TY, KL, RB, true>), grid, dim3(kExpThreads), 0, st, a); \
+  else                                                                                    \
+    hipLaunchKernelGGL((k_expand<TW, TY, KL, RB, false>), grid, dim3(kExpThreads), 0, st, a)
+  if (a.r <= 16) {
     OPD_EXPAND(4, 1);
-  else if (a.r <= 32)
+  } else if (a.r <= 32) {
     OPD_EXPAND(8, 1);
-  else if (a.r <= 64)
+  } else if (a.r <= 64) {
     OPD_EXPAND(8, 2);
-  else
+  } else {
     OPD_EXPAND(8, 4);
+  }
 #undef OPD_EXPAND
   return hipGetLastError();
 }
@@ -836,6 +909,13 @@ hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t st) {
 hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t st) {
   if (w_dt == F32) return low_t<InF32, InF32>(a, st);
   return x_dt == BF16 ? low_t<InBf16, InBf16>(a, st) : low_t<InF32, InBf16>(a, st);
+}
+
+hipError_t launch_low_sum(const LowArgs& a, int64_t N, hipStream_t st) {
+  if (a.splits == 1) return hipSuccess;
+  hipLaunchKernelGGL(k_low_sum, dim3((unsigned)((N * a.ldo + 255) / 256)), dim3(256), 0, st, a,
+                     N * a.ldo);
+  return hipGetLastError();
 }
 
 hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t st) {

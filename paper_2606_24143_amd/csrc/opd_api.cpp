@@ -347,17 +347,17 @@ struct EmbedLayout {
 constexpr int64_t kEmbedUnsorted = 256;
 EmbedLayout embed_layout(int64_t N, int64_t V, int64_t H) {
   EmbedLayout l{};
-  l.hp = (H + 3) / 4 * 4;
+  l.hp = (H + 7) / 8 * 8;
   if (N <= kEmbedUnsorted) return l;
   l.perm = up256((size_t)(V + 1) * 4);
   l.partial = l.perm + up256((size_t)N * 4);
-  l.total = l.partial + up256((size_t)((N + 63) / 64) * 2 * (size_t)l.hp * 4);
+  l.total = l.partial + up256((size_t)((N + opd::kEmbTile - 1) / opd::kEmbTile) * 2 * (size_t)l.hp * 4);
   return l;
 }
-// Entries to a workgroup that sorts: some two workgroups to a CU, up to kEmbKeys entries.
+// Entries to a workgroup that sorts: about a workgroup to each CU, up to kEmbKeys entries.
 int embed_keys(int64_t V) {
   int keys = 64;
-  while (keys < opd::kEmbKeys && (int64_t)keys * 512 < V) keys *= 2;
+  while (keys < opd::kEmbKeys && (int64_t)keys * 300 < V) keys *= 2;
   return keys;
 }
 
@@ -983,15 +983,17 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
       const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
                            l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
       err = opd::launch_low(t, dtype, dtype, st);
+      if (err == hipSuccess) err = opd::launch_low_sum(t, N, st);
       if (err != hipSuccess) return OPD_ERR_HIP;
-      tref = opd::LowRef{t.out, t.ldo, t.stride, t.splits, r};
+      tref = opd::LowRef{t.out, t.ldo, t.stride, 1, r};
     }
   }
   const opd::LowArgs u{plan.tiles, plan.perm, l.max_tiles, G, r, dy, b, lddy, ldb, O,
                        l.splits_y, l.span_y, N * l.ldt, (float*)(ws + l.u), l.ldt};
-  const opd::LowRef uref{u.out, u.ldo, u.stride, u.splits, r};
+  const opd::LowRef uref{u.out, u.ldo, u.stride, 1, r};
   if (N > 0) {
     err = opd::launch_low(u, y_dtype, dtype, st);
+    if (err == hipSuccess) err = opd::launch_low_sum(u, N, st);
     if (err != hipSuccess) return OPD_ERR_HIP;
   }
   const int64_t hp = (H + 3) / 4 * 4, op = (O + 3) / 4 * 4, gr = (int64_t)G * r;

@@ -18,7 +18,6 @@ namespace {
 
 constexpr int kEmbThreads = 256;
 constexpr int kEmbWaves = kEmbThreads / 64;
-constexpr int kEmbRows = 8;  // entries of a wavefront
 
 // E consecutive elements of a row, widened.
 template <class TI, int E>
@@ -141,17 +140,18 @@ __global__ void __launch_bounds__(kGroupThreads) k_embed_group(EmbedGradArgs a) 
   const int32_t* ids = a.ids;
   const int64_t V = a.V;
   uint32_t end;
-  const uint32_t first = group_tokens(
+  const uint32_t first = group_tokens<kEmbKeys, true>(
       a.N, lo, count, [=](int64_t n) { return (uint32_t)ids[n] < (uint32_t)V ? ids[n] : -1; }, a.perm, sh, end);
   if ((int)threadIdx.x < count) a.start[lo + (int)threadIdx.x] = (int32_t)first;
   if (threadIdx.x == 0 && lo + count == a.V) a.start[a.V] = (int32_t)end;
 }
 
-// Adds dy[token, c0 ..] for the tokens that lanes [0, count) hold, in order; B rows on
-// their way at once.
+// Adds dy[token, c + 256 v ..] for the tokens that lanes [0, count) hold, in order; B rows on
+// their way at once.  (Every lane takes part, since every lane's token is read: those whose
+// columns lie past H load nothing.)
 template <class TI, int VPL, int B>
 __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t token, int count,
-                                         int64_t c0, float (&f)[VPL][4]) {
+                                         int64_t c, float (&f)[VPL][4]) {
 #pragma unroll 1
   for (int i = 0; i < count; i += B) {
     float x[B][VPL][4];
@@ -161,8 +161,7 @@ __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t token, 
       const char* row =
           (const char*)a.dy + (int64_t)__builtin_amdgcn_readlane(token, i + b) * a.ldy * TI::BYTES;
 #pragma unroll
-      for (int v = 0; v < VPL; ++v)
-        if (c0 + v * 256 < a.H) load_wide<TI, 4>(row, c0 + v * 256, a.H, x[b][v]);
+      for (int v = 0; v < VPL; ++v) load_wide<TI, 4>(row, c + 256 * v, a.H, x[b][v]);
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
@@ -176,136 +175,157 @@ __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t token, 
   }
 }
 
-// Entries of more than kEmbTile tokens are summed tile by tile of the sorted
-// tokens first, so that one frequent token does not keep one wavefront busy.  A
-// tile holds a part of at most two such entries: one that begins before or at its
-// first place (part 0), and one that begins inside it (part 1) and goes on past it.
-constexpr int kEmbTile = 64;
-template <class TI>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_tiles(EmbedGradArgs a) {
-  const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  const int64_t tile = a.row0 + u / a.chunks;
-  const int64_t p = tile * kEmbTile + lane;
-  const int64_t kept = a.start[a.V];
-  if (u >= a.units || tile * kEmbTile >= kept) return;
-  const int64_t c0 = (int64_t)(u % a.chunks) * 256 + lane * 4;
-  const int32_t token = p < kept ? a.perm[p] : 0;
-  const int32_t id = p < kept ? a.ids[token] : -1;
-  int32_t s = 0, e = 0;
-  if (p < kept) {
-    s = a.start[id];
-    e = a.start[id + 1];
+template <class TO>
+__device__ __forceinline__ void store_sum(const EmbedGradArgs& a, int64_t v, int64_t c,
+                                          float (&f)[4]) {
+  char* row = (char*)a.out + v * a.ldo * TO::BYTES;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] *= a.scale;
+  if (a.accumulate) {
+    float x[4];
+    load_wide<TO, 4>(row, c, a.H, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] += x[e];
   }
-  const bool many = e - s > kEmbTile;
-#pragma unroll 1
-  for (int part = 0; part < 2; ++part) {
-    const uint64_t in = __ballot(many && (part == 0) == (s <= tile * kEmbTile));
-    if (!in) continue;
-    // (its places are consecutive: moved down to lane 0)
-    const int first = __ffsll((long long)in) - 1, count = __popcll(in);
-    const int32_t mine = __shfl(token, (first + lane) & 63, 64);
-    float f[1][4] = {};
-    add_rows<TI, 1, 16>(a, mine, count, c0, f);
-    float* to = a.partial + (tile * 2 + part) * a.hp;
-    if (c0 < a.H) *(f32x4*)(to + c0) = f32x4{f[0][0], f[0][1], f[0][2], f[0][3]};
-  }
+  store_wide<TO, 4, true>(row, c, a.H, f);
 }
 
-// One wavefront to kEmbRows entries and a chunk of 256 * VPL columns: first the entries
-// without a token, which are stores alone, then the others': their tokens' rows, or their tiles'
-// sums, in order.  SORTED false: no list; the wave looks for its entries' tokens
-// among the ids itself (few tokens, one launch).
-template <class TI, class TO, int VPL, bool SORTED>
-__global__ void __launch_bounds__(kEmbThreads) k_embed_rows(EmbedGradArgs a) {
-  const uint32_t block = xcd_eighths(blockIdx.x, gridDim.x);
-  const uint32_t u = block * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Two launches: the entries with tokens are read and summed, then the empty ones are filled
+// (most of the table, as a rule).  A wavefront that waits for a row holds a place among the
+// stores: in one launch 16,384 tokens of 8 KiB cost 200 us beside the fill's 350, apart
+// they cost 73.
+//
+// Entries of more than kEmbTile tokens are summed tile by tile of the sorted tokens, so
+// that one frequent token does not keep one wavefront busy, and the tiles' sums are added
+// in the second launch.  A tile holds a part of at most two such entries: one that begins
+// before or at its first place (part 0), and one that begins inside it (part 1) and goes
+// on past it.
+
+// A tile's long entries, by a wavefront whose lanes hold the tile's tokens.
+struct TileLane {
+  int32_t token, id, s, e;  // the lane's token, its entry, and that one's places
+  bool many;
+};
+__device__ __forceinline__ TileLane tile_lane(const EmbedGradArgs& a, int64_t tile) {
+  const int lane = threadIdx.x & 63;
+  const int64_t p = tile * kEmbTile + lane, kept = a.start[a.V];
+  TileLane t = {0, -1, 0, 0, false};
+  if (lane < kEmbTile && p < kept) {
+    t.token = a.perm[p];
+    t.id = a.ids[t.token];
+    t.s = a.start[t.id];
+    t.e = a.start[t.id + 1];
+    t.many = t.e - t.s > kEmbTile;
+  }
+  return t;
+}
+
+// One wavefront to a tile, or to the entry whose tokens begin at a place of the sorted ones,
+// and a chunk of 256 VPL columns.  (Bound by the chains of dependent loads: a place's token,
+// its entry, the entry's places, its rows.  16,384 tokens of 8 KiB: 512 columns and 4 rows
+// at once 73 us, 512 and 8 95, 1,024 and 4 105, 256 and 8 88: more registers, fewer waves.)
+template <class TI, class TO, int VPL>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_sums(EmbedGradArgs a) {
+  const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= a.units) return;
   const int lane = threadIdx.x & 63;
-  const int64_t v0 = (a.row0 + u / a.chunks) * kEmbRows;
-  const int64_t c0 = (int64_t)(u % a.chunks) * (256 * VPL) + lane * 4;
-  const int rows = (int)(a.V - v0 < kEmbRows ? a.V - v0 : kEmbRows);
-  int32_t first = 0;
-  uint64_t some = 0;  // bit i: entry v0 + i has a token
-  if constexpr (SORTED) {
-    first = a.start[v0 + (lane <= rows ? lane : rows)];
-    const int32_t past = __shfl_down(first, 1, 64);
-    some = __ballot(lane < rows && past > first);
-  } else {
-    for (int64_t n = 0; n < a.N; n += 64) {
-      const int64_t id = n + lane < a.N ? (int64_t)a.ids[n + lane] - v0 : -1;
-      uint64_t in = __ballot(id >= 0 && id < rows);
-      while (in) {
-        const int l = __ffsll((long long)in) - 1;
-        in &= in - 1;
-        some |= 1ull << __builtin_amdgcn_readlane((int)id, l);
-      }
-    }
-  }
-  auto out = [&](int i) { return (char*)a.out + (v0 + i) * a.ldo * TO::BYTES; };
-  if (!a.accumulate) {
-    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  const int64_t row = a.row0 + u / a.chunks;
+  const int64_t c = (int64_t)(u % a.chunks) * (256 * VPL) + lane * 4;
+  float f[VPL][4] = {};
+  if (row < a.tiles) {
+    const TileLane t = tile_lane(a, row);
 #pragma unroll 1
-    for (int i = 0; i < rows; ++i) {
-      if (some >> i & 1) continue;
+    for (int part = 0; part < 2; ++part) {
+      const uint64_t in = __ballot(t.many && (part == 0) == (t.s <= row * kEmbTile));
+      if (!in) continue;
+      // (its places are consecutive: moved down to lane 0)
+      const int first = __ffsll((long long)in) - 1, count = __popcll(in);
+      const int32_t mine = __shfl(t.token, (first + lane) & 63, 64);
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[v][e] = 0.f;
+      }
+      add_rows<TI, VPL, 8 / VPL>(a, mine, count, c, f);
+      float* to = a.partial + (row * 2 + part) * a.hp + c;
 #pragma unroll
       for (int v = 0; v < VPL; ++v)
-        if (c0 + v * 256 < a.H) store_wide<TO, 4, true>(out(i), c0 + v * 256, a.H, zero);
+        if (c + 256 * v < a.H) *(f32x4*)(to + 256 * v) = f32x4{f[v][0], f[v][1], f[v][2], f[v][3]};
     }
+    return;
   }
-#pragma unroll 1
-  while (some) {
-    const int i = __ffsll((long long)some) - 1;
-    some &= some - 1;
-    float f[VPL][4] = {};
-    if constexpr (SORTED) {
-      const int32_t s = __builtin_amdgcn_readlane(first, i);
-      const int32_t e = __builtin_amdgcn_readlane(first, i + 1);
-      if (e - s > kEmbTile) {
-        const int64_t t1 = ((int64_t)e + kEmbTile - 1) / kEmbTile;
-#pragma unroll 2
-        for (int64_t t = s / kEmbTile; t < t1; ++t) {
-          const float* from = a.partial + (t * 2 + (s > t * kEmbTile ? 1 : 0)) * a.hp;
+  const int64_t p = row - a.tiles;
+  if (p >= a.start[a.V]) return;
+  const int32_t v = a.ids[a.perm[p]];
+  const int32_t s = a.start[v], e = a.start[v + 1];
+  if (s != p || e - s > kEmbTile) return;
+  add_rows<TI, VPL, 8 / VPL>(a, lane < e - s ? a.perm[s + lane] : 0, e - s, c, f);
 #pragma unroll
-          for (int v = 0; v < VPL; ++v) {
-            if (c0 + v * 256 >= a.H) continue;
-            const f32x4 x = *(const f32x4*)(from + c0 + v * 256);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) f[v][k] += x[k];
-          }
-        }
-      } else {
-        add_rows<TI, VPL, 4>(a, lane < e - s ? a.perm[s + lane] : 0, e - s, c0, f);
-      }
-    } else {
-      for (int64_t n = 0; n < a.N; n += 64) {
-        const int64_t id = n + lane < a.N ? (int64_t)a.ids[n + lane] - v0 : -1;
-        uint64_t in = __ballot(id == i);
-        while (in) {
-          const int l = __ffsll((long long)in) - 1;
-          in &= in - 1;
-          add_rows<TI, VPL, 1>(a, (int32_t)(n + l), 1, c0, f);
-        }
-      }
-    }
-    char* row = out(i);
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      if (c0 + v * 256 >= a.H) continue;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) f[v][k] *= a.scale;
-      if (a.accumulate) {
-        float x[4];
-        load_wide<TO, 4>(row, c0 + v * 256, a.H, x);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[v][k] += x[k];
-      }
-      store_wide<TO, 4, true>(row, c0 + v * 256, a.H, f[v]);
-    }
-  }
+  for (int i = 0; i < VPL; ++i)
+    if (c + 256 * i < a.H) store_sum<TO>(a, v, c + 256 * i, f[i]);
 }
 
-// Launches over rows (tokens, tiles, groups of entries) in units of a row's chunk.
+// One wavefront to a tile, or an entry, and a chunk of 256 columns: the tiles' sums of a long
+// entry, in order, by the wavefronts of the tile that it begins in; and zeros where
+// there is no token.  (One store to a lane, in short waves side by side, is as fast as a
+// plain fill: 370 us where one takes 361, for 151,936 by 4,096 fp32.  Four stores to a lane
+// took 425, eight rows to a wave 440.)
+template <class TO>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_rest(EmbedGradArgs a) {
+  const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (u >= a.units) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = a.row0 + u / a.chunks;
+  const int64_t c = (int64_t)(u % a.chunks) * 256 + lane * 4;
+  float f[4] = {0.f, 0.f, 0.f, 0.f};
+  int64_t v = row - a.tiles;
+  if (v >= 0) {
+    if (a.start[v] != a.start[v + 1]) return;
+    if (c < a.H) store_wide<TO, 4, true>((char*)a.out + v * a.ldo * TO::BYTES, c, a.H, f);
+    return;
+  }
+  const TileLane t = tile_lane(a, row);
+  // (at most one begins here: it goes on past the tile)
+  const uint64_t in = __ballot(t.many && t.s == row * kEmbTile + lane);
+  if (!in) return;
+  const int l = __ffsll((long long)in) - 1;
+  v = __builtin_amdgcn_readlane(t.id, l);
+  const int64_t s = __builtin_amdgcn_readlane(t.s, l), e = __builtin_amdgcn_readlane(t.e, l);
+  if (c >= a.H) return;
+  const int64_t t1 = (e + kEmbTile - 1) / kEmbTile;
+  f32x4 sum = *(const f32x4*)(a.partial + (row * 2 + (s > row * kEmbTile ? 1 : 0)) * a.hp + c);
+#pragma unroll 8
+  for (int64_t i = row + 1; i < t1; ++i) sum += *(const f32x4*)(a.partial + i * 2 * a.hp + c);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) f[k] = sum[k];
+  store_sum<TO>(a, v, c, f);
+}
+
+// Few tokens, in one launch: a wavefront looks for its entry's tokens among the ids itself.
+template <class TI, class TO>
+__global__ void __launch_bounds__(kEmbThreads) k_embed_few(EmbedGradArgs a) {
+  const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (u >= a.units) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t v = a.row0 + u / a.chunks;
+  const int64_t c = (int64_t)(u % a.chunks) * 256 + lane * 4;
+  float f[1][4] = {};
+  bool any = false;
+  for (int64_t n = 0; n < a.N; n += 64) {
+    const int32_t id = n + lane < a.N ? a.ids[n + lane] : -1;
+    uint64_t in = __ballot(id == (int32_t)v);
+    any |= in != 0;
+    while (in) {
+      const int l = __ffsll((long long)in) - 1;
+      in &= in - 1;
+      add_rows<TI, 1, 1>(a, (int32_t)(n + l), 1, c, f);
+    }
+  }
+  if (a.accumulate && !any) return;
+  if (c < a.H) store_sum<TO>(a, v, c, f[0]);
+}
+
+// Launches over rows (tokens, tiles, entries) in units of a row's chunk.
 constexpr int64_t kEmbMaxUnits = ((int64_t)1 << 32) / kEmbThreads * kEmbWaves - kEmbWaves;
 template <class Args, class F>
 hipError_t launch_units(Args a, int64_t rows, int chunk, F launch) {
@@ -334,31 +354,29 @@ hipError_t embed_t(const EmbedArgs& a, hipStream_t st) {
 #undef OPD_EMBED
 }
 
-template <class TI, class TO, int VPL>
-hipError_t embed_grad_v(const EmbedGradArgs& a, hipStream_t st) {
-  const int64_t rows = (a.V + kEmbRows - 1) / kEmbRows;
+template <class TI, class TO>
+hipError_t embed_grad_t(EmbedGradArgs a, hipStream_t st) {
   if (!a.start)
-    return launch_units(a, rows, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {
-      hipLaunchKernelGGL((k_embed_rows<TI, TO, VPL, false>), g, dim3(kEmbThreads), 0, st, b);
+    return launch_units(a, a.V, 256, [&](const EmbedGradArgs& b, dim3 g) {
+      hipLaunchKernelGGL((k_embed_few<TI, TO>), g, dim3(kEmbThreads), 0, st, b);
     });
   hipLaunchKernelGGL(k_embed_group, dim3((unsigned)((a.V + a.keys - 1) / a.keys)),
                      dim3(kGroupThreads), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  e = launch_units(a, (a.N + kEmbTile - 1) / kEmbTile, 256, [&](const EmbedGradArgs& b, dim3 g) {
-    hipLaunchKernelGGL((k_embed_tiles<TI>), g, dim3(kEmbThreads), 0, st, b);
-  });
+  a.tiles = (a.N + kEmbTile - 1) / kEmbTile;
+#define OPD_SUMS(VPL)                                                                   \
+  launch_units(a, a.tiles + a.N, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {       \
+    hipLaunchKernelGGL((k_embed_sums<TI, TO, VPL>), g, dim3(kEmbThreads), 0, st, b);    \
+  })
+  e = a.H <= 256 ? OPD_SUMS(1) : OPD_SUMS(2);
+#undef OPD_SUMS
   if (e != hipSuccess) return e;
-  return launch_units(a, rows, 256 * VPL, [&](const EmbedGradArgs& b, dim3 g) {
-    hipLaunchKernelGGL((k_embed_rows<TI, TO, VPL, true>), g, dim3(kEmbThreads), 0, st, b);
-  });
-}
-
-template <class TI, class TO>
-hipError_t embed_grad_t(const EmbedGradArgs& a, hipStream_t st) {
-  if (a.H <= 256) return embed_grad_v<TI, TO, 1>(a, st);
-  if (a.H <= 512) return embed_grad_v<TI, TO, 2>(a, st);
-  return embed_grad_v<TI, TO, 4>(a, st);
+  // (added to: what has no token stays)
+  return launch_units(a, a.tiles + (a.accumulate ? 0 : a.V), 256,
+                      [&](const EmbedGradArgs& b, dim3 g) {
+                        hipLaunchKernelGGL((k_embed_rest<TO>), g, dim3(kEmbThreads), 0, st, b);
+                      });
 }
 
 }  // namespace

@@ -65,7 +65,7 @@ __device__ __forceinline__ uint64_t lanes_of_key(uint64_t in, int32_t k, int bit
 // way, so workgroups need nothing of each other.  Writes perm for its keys;
 // returns the first place of key lo + threadIdx.x (for lanes below count) and
 // the place past the workgroup's last token.
-template <int KEYS, class Key>
+template <int KEYS, bool FEW, class Key>
 __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int count, Key key,
                                                  int32_t* perm, GroupLds<KEYS>& sh, uint32_t& end) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -90,11 +90,16 @@ __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int coun
     for (int i = 0; i < A; ++i) {
       if (ks[i] >= 0 && ks[i] < lo) ++below;
       const int32_t k = ks[i] - lo;
-      const uint64_t in = __ballot(ks[i] >= lo && k < count);
-      if (!in) continue;
-      const uint64_t same = lanes_of_key(in, k, bits);
-      if ((in >> lane & 1) && lane == __ffsll((long long)same) - 1)
-        atomicAdd(&sh.at[w][k], (uint32_t)__popcll(same));
+      const bool mine = ks[i] >= lo && k < count;
+      if constexpr (FEW) {  // of all tokens are a workgroup's: they hardly meet
+        if (mine) atomicAdd(&sh.at[w][k], 1u);
+      } else {
+        const uint64_t in = __ballot(mine);
+        if (!in) continue;
+        const uint64_t same = lanes_of_key(in, k, bits);
+        if (mine && lane == __ffsll((long long)same) - 1)
+          atomicAdd(&sh.at[w][k], (uint32_t)__popcll(same));
+      }
     }
   }
   below = (uint32_t)__shfl((int)wave_incl_scan_u32(below), 63, 64);

@@ -7,8 +7,9 @@
 namespace opd {
 
 // Token embeddings (opd_embed_tokens, opd_embed_grads).  Launches go over rows (tokens,
-// groups of entries, tiles) times chunks of columns.
-constexpr int kEmbKeys = 256;  // entries that a workgroup sorts, at most
+// entries, tiles) times chunks of columns.
+constexpr int kEmbTile = 16;   // sorted tokens of a tile, up to 64
+constexpr int kEmbKeys = 512;  // entries that a workgroup sorts, at most
 struct EmbedArgs {
   const void* table;      // [V, ld]
   int64_t V, H, ld;
@@ -32,9 +33,10 @@ struct EmbedGradArgs {
   int keys;               // entries that a workgroup sorts
   int32_t* start;         // [V + 1]; NULL: tokens are not sorted (few)
   int32_t* perm;          // [N]
-  float* partial;         // [ceil(N / 64), 2, hp]
+  float* partial;         // [ceil(N / kEmbTile), 2, hp]
   int64_t hp;
-  int64_t row0;           // (the launch sets these)
+  int64_t tiles;          // of sorted tokens (the launch sets these)
+  int64_t row0;
   uint32_t units, chunks;
 };
 hipError_t launch_embed(const EmbedArgs& a, int in_dt, int out_dt, hipStream_t stream);
@@ -91,7 +93,7 @@ struct ExpandArgs {
   float* low_out;         // [N, r] nullable
   uint32_t per;           // workgroups to a tile (the launch sets it)
 };
-// out[g] = scale * sum over the adapter's tokens of low^T x
+// out[g] = scale * sum over the adapter's tokens of low^T x (low: one part)
 struct OuterArgs {
   const int32_t* perm;
   const int32_t* start;
@@ -108,6 +110,8 @@ struct OuterArgs {
 };
 hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t stream);
 hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t stream);
+// adds the parts up in the first one's place, for N tokens
+hipError_t launch_low_sum(const LowArgs& a, int64_t N, hipStream_t stream);
 hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t stream);
 hipError_t launch_outer(const OuterArgs& a, int x_dt, float* out, int64_t ldo, hipStream_t stream);
 
