@@ -550,9 +550,9 @@ size_t opd_adapter_workspace_bytes(int64_t N, int64_t H, int64_t O, int32_t G, i
  * opd_beam_select: rows b W .. b W + W - 1 of the logits are group b's beams, with
  *   scores [B, W].  Candidate (w, v) has score scores[b, w] + log softmax(row)[v]; the k
  *   largest are returned in descending order, ties to the lower beam, then the lower token.
- *   Scores are made and compared in double precision from fp32 logarithms' sums
- *   good to about 1e-8, so the order is that of exact arithmetic unless two beams' scores
- *   differ by about as little.
+ *   Scores are made and compared in double precision.  A beam's log-sum is good to about 1e-8
+ *   for rows of many different logits, and to 2e-7 for any: the order is that of exact arithmetic
+ *   unless two beams' scores differ by about as little.
  *     finished [B, W] uint8, nullable: a finished beam (not 0) is one candidate, with its
  *     own score and id -1; its row is not read.  A beam of score -inf (one that does not
  *     exist yet) and a row without a finite logit have no candidates (a masked logit, -inf,

@@ -158,8 +158,9 @@ __device__ __forceinline__ float low_value(const LowRef& t, int64_t token, int c
 // take steps of 64 (bf16) or 32 (fp32) columns in turn, the next ones on their way meanwhile,
 // and their sums are added in order.  A lane's operands lie along a row, and its
 // neighbours' in other rows: loaded so, an instruction touches 16 lines 16 bytes at a time,
-// which took 42 us for 8,192 tokens by 4,096 columns and 32 ranks where TIME_LDS are needed with
-// rows read as they lie and turned in LDS, a part of it to each wave.  RT: ranks / 16.
+// which took 42 us for 8,192 tokens by 4,096 columns and 32 ranks where 32 are needed with
+// rows read as they lie and turned in LDS, a part of it to each wave (20 where nothing has
+// just been written: reading the tokens alone takes 17.5).  RT: ranks / 16.
 constexpr int kLowThreads = 512;
 constexpr int kLowWaves = kLowThreads / 64;
 
@@ -664,7 +665,10 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
 constexpr int kOutThreads = 512;
 constexpr int kOutWaves = kOutThreads / 64;
 template <class TX, int RT>
-__global__ void __launch_bounds__(kOutThreads, 2) k_outer(OuterArgs a) {
+__global__ void __launch_bounds__(kOutThreads, RT == 1 ? 4 : 2) k_outer(OuterPair pair) {
+  const bool second = blockIdx.x >= pair.blocks;
+  const OuterArgs& a = pair.a[second];
+  const uint32_t block = blockIdx.x - (second ? pair.blocks : 0u);
   constexpr bool BF = TX::BYTES == 2;
   constexpr int E = BF ? 8 : 4;
   constexpr int TERMS = 3;
@@ -673,11 +677,11 @@ __global__ void __launch_bounds__(kOutThreads, 2) k_outer(OuterArgs a) {
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (columns first: workgroups side by side read whole rows)
-  const uint32_t item = blockIdx.x / a.chunks;
+  const uint32_t item = block / a.chunks;
   const int split = item % a.splits;
   const int g = item / a.splits;
   const int r0 = blockIdx.y * (RT * 16);
-  const int64_t c0 = (int64_t)(blockIdx.x % a.chunks) * C;
+  const int64_t c0 = (int64_t)(block % a.chunks) * C;
   const int32_t s = a.start[g], count = a.start[g + 1] - s;
   const int64_t c = c0 + m * E;
   const float scale = a.scales ? a.scales[g] : 1.f;
@@ -807,7 +811,9 @@ __global__ void __launch_bounds__(kOutThreads, 2) k_outer(OuterArgs a) {
 #pragma unroll
         for (int v = 1; v < kOutWaves; ++v) f[e] += sums[v][i / (C / 4)][at + e];
       }
-      float* out = a.out + (int64_t)split * a.stride + ((int64_t)g * a.r + rank) * a.ldo;
+      float* out = a.splits == 1
+                       ? a.sum + ((int64_t)g * a.r + rank) * a.lds
+                       : a.out + (int64_t)split * a.stride + ((int64_t)g * a.r + rank) * a.ldo;
       store_values<InF32, 4>((char*)out, c0 + at, a.D, f);
     }
   }
@@ -822,16 +828,19 @@ __global__ void __launch_bounds__(256) k_low_sum(LowArgs a, int64_t n) {
   a.out[i] = f;
 }
 
-// The parts of da or db, added in order.
-__global__ void __launch_bounds__(256) k_outer_sum(OuterArgs a, float* out, int64_t ldo) {
-  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (c >= a.D) return;
+// The parts of da and db, added in order.
+__global__ void __launch_bounds__(256) k_outer_sum(OuterPair pair) {
+  const bool second = blockIdx.x >= pair.blocks;
+  const OuterArgs& a = pair.a[second];
+  const int64_t c = ((int64_t)(blockIdx.x - (second ? pair.blocks : 0u)) * 256 + threadIdx.x) * 4;
+  if (c >= a.D || a.splits == 1) return;
   for (int64_t row = blockIdx.y; row < (int64_t)a.G * a.r; row += gridDim.y) {
     const float* p = a.out + row * a.ldo + c;
     f32x4 f = *(const f32x4*)p;
+#pragma unroll 4
     for (int s = 1; s < a.splits; ++s) f += *(const f32x4*)(p + s * a.stride);
     const float v[4] = {f[0], f[1], f[2], f[3]};
-    store_values<InF32, 4>((char*)(out + row * ldo), c, a.D, v);
+    store_values<InF32, 4>((char*)(a.sum + row * a.lds), c, a.D, v);
   }
 }
 
@@ -885,17 +894,22 @@ hipError_t expand_t(ExpandArgs a, hipStream_t st) {
 }
 
 template <class TX>
-hipError_t outer_t(OuterArgs a, hipStream_t st) {
+hipError_t outer_t(OuterPair p, int count, hipStream_t st) {
   const int64_t span = 16 * (TX::BYTES == 2 ? 8 : 4);
-  const int rt = (a.r + 15) / 16;
-  a.chunks = (uint32_t)((a.D + span - 1) / span);
-  const dim3 grid((unsigned)(a.G * a.splits * a.chunks), (unsigned)(rt <= 4 ? 1 : 2));
+  const int rt = (p.a[0].r + 15) / 16;
+  uint32_t blocks[2] = {0, 0};
+  for (int i = 0; i < count; ++i) {
+    p.a[i].chunks = (uint32_t)((p.a[i].D + span - 1) / span);
+    blocks[i] = (uint32_t)(p.a[i].G * p.a[i].splits) * p.a[i].chunks;
+  }
+  p.blocks = blocks[0];
+  const dim3 grid(blocks[0] + blocks[1], (unsigned)(rt <= 4 ? 1 : 2));
   if (rt == 1)
-    hipLaunchKernelGGL((k_outer<TX, 1>), grid, dim3(kOutThreads), 0, st, a);
+    hipLaunchKernelGGL((k_outer<TX, 1>), grid, dim3(kOutThreads), 0, st, p);
   else if (rt == 2)
-    hipLaunchKernelGGL((k_outer<TX, 2>), grid, dim3(kOutThreads), 0, st, a);
+    hipLaunchKernelGGL((k_outer<TX, 2>), grid, dim3(kOutThreads), 0, st, p);
   else
-    hipLaunchKernelGGL((k_outer<TX, 4>), grid, dim3(kOutThreads), 0, st, a);
+    hipLaunchKernelGGL((k_outer<TX, 4>), grid, dim3(kOutThreads), 0, st, p);
   return hipGetLastError();
 }
 
@@ -923,17 +937,24 @@ hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t st
   return y_dt == BF16 ? expand_t<InBf16, InBf16>(a, st) : expand_t<InBf16, InF32>(a, st);
 }
 
-hipError_t launch_outer(const OuterArgs& a, int x_dt, float* out, int64_t ldo, hipStream_t st) {
-  OuterArgs b = a;
-  if (a.splits == 1) {
-    b.out = out;
-    b.ldo = ldo;
+hipError_t launch_outer(const OuterPair& pair, int x_dt, int y_dt, hipStream_t st) {
+  hipError_t e;
+  if (x_dt == y_dt) {
+    e = x_dt == BF16 ? outer_t<InBf16>(pair, 2, st) : outer_t<InF32>(pair, 2, st);
+  } else {  // bf16 x, fp32 dy
+    OuterPair one = pair;
+    e = outer_t<InBf16>(one, 1, st);
+    if (e != hipSuccess) return e;
+    one.a[0] = pair.a[1];
+    e = outer_t<InF32>(one, 1, st);
   }
-  const hipError_t e = x_dt == BF16 ? outer_t<InBf16>(b, st) : outer_t<InF32>(b, st);
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t rows = (int64_t)a.G * a.r;
-  hipLaunchKernelGGL(k_outer_sum, dim3((unsigned)((a.D + 1023) / 1024), (unsigned)(rows < 65535 ? rows : 65535)),
-                     dim3(256), 0, st, b, out, ldo);
+  if (e != hipSuccess || (pair.a[0].splits == 1 && pair.a[1].splits == 1)) return e;
+  OuterPair p = pair;
+  const int64_t rows = (int64_t)p.a[0].G * p.a[0].r;
+  const int64_t x = (p.a[0].D + 1023) / 1024, y = (p.a[1].D + 1023) / 1024;
+  p.blocks = (uint32_t)x;
+  hipLaunchKernelGGL(k_outer_sum, dim3((unsigned)(x + y), (unsigned)(rows < 65535 ? rows : 65535)),
+                     dim3(256), 0, st, p);
   return hipGetLastError();
 }
 

@@ -377,8 +377,8 @@ struct AdaptLayout {
   int64_t max_tiles, ldt;
   int64_t span_x, span_y;      // of the long axes, parts
   int splits_x, splits_y;
-  int outer_x, outer_y;        // parts of an adapter's tokens
-  size_t start, tiles, t, u, outer, total;
+  int outer;                   // parts of an adapter's tokens
+  size_t start, tiles, t, u, part_x, part_y, total;
 };
 // Parts of a long axis of D columns: about 1,024 workgroups of 16 tokens, each
 // with 1,024 columns at least.
@@ -408,22 +408,18 @@ AdaptLayout adapt_layout(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r, 
   l.u = at;
   if (backward) {
     at += up256((size_t)l.splits_y * N * l.ldt * 4);
-    l.outer = at;
+    l.part_x = at;
     const int64_t used = G < N ? G : N;
-    // of an adapter's tokens, a workgroup's waves take 256 at once
-    auto parts = [&](int64_t D, int32_t dt) {
-      const int64_t span = dt == OPD_BF16 ? 128 : 64;
-      int64_t s = 512 / (((D + span - 1) / span) * (used > 0 ? used : 1));
-      const int64_t most = N / 512;
-      if (s > most) s = most;
-      return (int)(s < 1 ? 1 : s);
-    };
-    l.outer_x = parts(H, dtype);
-    l.outer_y = parts(O, y_dtype);
-    const size_t gr = (size_t)G * (size_t)r * 4;
-    const size_t px = l.outer_x > 1 ? (size_t)l.outer_x * gr * (size_t)((H + 3) / 4 * 4) : 0;
-    const size_t py = l.outer_y > 1 ? (size_t)l.outer_y * gr * (size_t)((O + 3) / 4 * 4) : 0;
-    at += up256(px > py ? px : py);
+    // parts of an adapter's tokens, of which a workgroup's waves take 256 at once: two
+    // workgroups to a CU, both sums together
+    const int64_t chunks = (H + (dtype == OPD_BF16 ? 127 : 63)) / (dtype == OPD_BF16 ? 128 : 64) +
+                           (O + (y_dtype == OPD_BF16 ? 127 : 63)) / (y_dtype == OPD_BF16 ? 128 : 64);
+    int64_t s = 512 / (chunks * (used > 0 ? used : 1));
+    if (s > N / 512) s = N / 512;
+    l.outer = (int)(s < 1 ? 1 : s);
+    const size_t gr = (size_t)l.outer * (size_t)G * (size_t)r * 4;
+    l.part_y = l.part_x + up256(l.outer > 1 ? gr * (size_t)((H + 3) / 4 * 4) : 0);
+    at = l.part_y + up256(l.outer > 1 ? gr * (size_t)((O + 3) / 4 * 4) : 0);
   }
   l.total = at;
   return l;
@@ -433,8 +429,7 @@ bool adapt_fits(const AdaptLayout& l, int64_t D, int32_t G, bool backward) {
   const int64_t chunks = (D + 63) / 64, splits = l.splits_x > l.splits_y ? l.splits_x : l.splits_y;
   if (l.max_tiles * 4 * 512 * splits > kMaxGridLanes) return false;
   if (!backward) return true;
-  const int64_t parts = l.outer_x > l.outer_y ? l.outer_x : l.outer_y;
-  return (int64_t)G * parts * chunks * 2 * 512 <= kMaxGridLanes;
+  return (int64_t)G * l.outer * 2 * chunks * 2 * 512 <= kMaxGridLanes;
 }
 
 // How rows of logits are cut for the selection of beams.
@@ -997,13 +992,13 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
     if (err != hipSuccess) return OPD_ERR_HIP;
   }
   const int64_t hp = (H + 3) / 4 * 4, op = (O + 3) / 4 * 4, gr = (int64_t)G * r;
-  const opd::OuterArgs oa{plan.perm, plan.start, G, r, uref, scales, x, ldx, H, l.outer_x, gr * hp,
-                          (float*)(ws + l.outer), hp, 0};
-  err = opd::launch_outer(oa, dtype, da, ldda, st);
-  if (err != hipSuccess) return OPD_ERR_HIP;
-  const opd::OuterArgs ob{plan.perm, plan.start, G, r, tref, scales, dy, lddy, O, l.outer_y,
-                          gr * op, (float*)(ws + l.outer), op, 0};
-  err = opd::launch_outer(ob, y_dtype, db, lddb, st);
+  const opd::OuterPair pair{
+      {{plan.perm, plan.start, G, r, uref, scales, x, ldx, H, l.outer, gr * hp,
+        (float*)(ws + l.part_x), hp, da, ldda, 0},
+       {plan.perm, plan.start, G, r, tref, scales, dy, lddy, O, l.outer, gr * op,
+        (float*)(ws + l.part_y), op, db, lddb, 0}},
+      0};
+  err = opd::launch_outer(pair, dtype, y_dtype, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   if (!dx || N == 0) return OPD_OK;
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r, uref, scales, a, lda, H,

@@ -5,9 +5,9 @@
 //            the k largest of the group, ties to the lower beam, then the lower
 //            token; a finished beam is a candidate as it stands
 //   reorder  state[j] = state[parent[j]], in place or to another buffer
-// Scores are compared in double precision (sums of exponentials are good to
-// about 1e-8: fp32 terms with the rounding of their argument put back, doubles from
-// a lane's vector on), so beams that are nearly as good keep their order.
+// Scores are compared in double precision, so beams that are nearly as good keep their
+// order: terms of the sums of exponentials are fp32, each good to some 2e-7 (the sum of
+// many different ones to about 1e-8), and doubles from a lane's vector on.
 #pragma once
 
 #include "opd_device.h"
@@ -19,32 +19,84 @@ namespace {
 constexpr int kBeamThreads = 256;
 constexpr int kBeamWaves = kBeamThreads / 64;
 
-// The 64 largest of two descending lists, descending.
-__device__ __forceinline__ uint32_t beam_merge_desc(uint32_t a, uint32_t b_reversed) {
-  const int lane = threadIdx.x & 63;
-  uint32_t v = max(a, b_reversed);
-#pragma unroll
-  for (int stride = 32; stride > 0; stride >>= 1) {
-    const uint32_t pv = (uint32_t)__shfl_xor((int)v, stride, 64);
-    v = (lane & stride) == 0 ? max(v, pv) : min(v, pv);
+// The value of the lane that is S away (by exclusive or): moves within a row of 16 lanes,
+// and exchanges of rows and halves, which need no LDS.
+template <int S>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  auto dpp = [](uint32_t x, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, true);
+  };
+  constexpr std::integral_constant<int, 0xB1> swap1;     // lanes 1 0 3 2 of each four
+  constexpr std::integral_constant<int, 0x4E> swap2;     // 2 3 0 1
+  constexpr std::integral_constant<int, 0x1B> reverse4;  // 3 2 1 0
+  constexpr std::integral_constant<int, 0x141> reverse8;
+  constexpr std::integral_constant<int, 0x140> reverse16;
+  if constexpr (S == 1) return dpp(v, swap1);
+  if constexpr (S == 2) return dpp(v, swap2);
+  if constexpr (S == 4) return dpp(dpp(v, reverse8), reverse4);
+  if constexpr (S == 8) return dpp(dpp(v, reverse16), reverse8);
+  if constexpr (S == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
   }
+  if constexpr (S == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+template <int S = 32>
+__device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, __uint_as_float(lane_xor<S>(__float_as_uint(v))));
+  if constexpr (S > 1) v = lanes_max<S / 2>(v);
   return v;
 }
-
-// exp(f - m), m the maximum: the argument of the power of two is a rounded
-// product, whose rounding (and that of log2 e) goes into the result afterwards.
-__device__ __forceinline__ float beam_term(float f, float m) {
-  constexpr float hi = 1.44269504f, lo = 1.92596299e-8f, ln2 = 0.693147181f;
-  const float d = f - m;
-  const float p = d * hi;
-  const float r = fmaf(d, lo, fmaf(d, hi, -p));
-  const float e = fast_exp2(p);
-  // (d = -inf: p is -inf, r NaN, the term 0)
-  return p < -150.f ? 0.f : fmaf(e * ln2, r, e);
+template <int S = 32>
+__device__ __forceinline__ double lanes_sum(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint64_t o = (uint64_t)lane_xor<S>((uint32_t)(b >> 32)) << 32 | lane_xor<S>((uint32_t)b);
+  v += __builtin_bit_cast(double, o);
+  if constexpr (S > 1) v = lanes_sum<S / 2>(v);
+  return v;
+}
+// One step of a bitonic network: lanes keep the larger where `size` and S say so.
+template <int SIZE, int S>
+__device__ __forceinline__ uint32_t bitonic_step(uint32_t v) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t o = lane_xor<S>(v);
+  const bool larger = ((lane & SIZE) == 0) == ((lane & S) == 0);
+  return larger ? max(v, o) : min(v, o);
+}
+template <int SIZE, int S>
+__device__ __forceinline__ uint32_t bitonic_merge(uint32_t v) {
+  v = bitonic_step<SIZE, S>(v);
+  if constexpr (S > 1) v = bitonic_merge<SIZE, S / 2>(v);
+  return v;
+}
+// A value of each lane, sorted, descending.
+template <int SIZE = 2>
+__device__ __forceinline__ uint32_t lanes_sorted(uint32_t v) {
+  v = bitonic_merge<SIZE, SIZE / 2>(v);
+  if constexpr (SIZE < 64) v = lanes_sorted<SIZE * 2>(v);
+  return v;
+}
+// The 64 largest of two descending lists, descending.
+__device__ __forceinline__ uint32_t beam_merge_desc(uint32_t a, uint32_t b_reversed) {
+  return bitonic_merge<64, 32>(max(a, b_reversed));
 }
 
-// Candidates of a part at most: all elements of fewer than k lanes (those above the
-// bound), and a wavefront's equal to it besides.
+// Terms of a row's sum, as powers of two: f log2 e less a whole number c near its largest,
+// in two multiply-adds, each exact but for the rounding of a result that is small where
+// the term is large (2^-23 of it, in 1 / log2 e; the instruction's own 2^-23 is as much).
+constexpr float kLog2eLow = 1.92596299e-8f;  // log2 e less its fp32 value
+__device__ __forceinline__ float beam_term(float f, float c) {
+  return fast_exp2(fmaf(f, kLog2eLow, fmaf(f, kLog2e, -c)));
+}
+// Largest magnitude of a maximum for which that holds; farther ones are subtracted first.
+constexpr float kBeamNear = 65536.f;
+
+// Candidates of a part in LDS, at most: by the bound of all lanes, all elements of fewer
+// than k lanes (those above it), and a wavefront's equal to it besides.  The bound of one
+// wave leaves more, as a rule fewer than four times as many.
 template <class TI, int S>
 constexpr uint32_t beam_cap(int k) {
   return (uint32_t)((k - 1) * S * (16 / TI::BYTES) + 64 * (16 / TI::BYTES) + k);
@@ -57,13 +109,15 @@ struct BeamLds {
   uint32_t n;
 };
 
-// One workgroup to a row's part of 256 * E * S elements, which stays in registers:
-// its maximum, its sum of exponentials, and its candidates: what is not below
-// the k-th largest of the lanes' maxima, so k of them at least are among the best k,
-// and none else can be.  Bound by HBM and the vector unit alike (about 14 instructions
-// an element).
+// One workgroup to a row's part of 256 * E * S elements, which stays in registers: its
+// maximum, its sum of exponentials, and its candidates: what is not below a bound that k
+// lanes' maxima reach, so k of them at least are among the best k, and none else can be.
+// Bound by the vector unit (some 12 instructions an element, the exponential four times as
+// long as the others).  64 groups of 8 beams, an eighth of them ended, V = 151,936 bf16: 35 us,
+// where reading takes 20; with the lanes' maxima sorted for the bound, and terms of
+// f - max with that argument's rounding put back, 43; eight waves to a SIMD spill, 43.
 template <class TI, int S>
-__global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
+__global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
   constexpr int E = 16 / TI::BYTES;
   constexpr int kSpan = kBeamThreads * E;  // elements of a slot
   __shared__ BeamLds sh;
@@ -74,28 +128,29 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = a.row0 + blockIdx.x / a.parts;
   const uint32_t part = blockIdx.x % a.parts;
-  if ((a.finished && a.finished[row]) || a.scores[row] == kNegInf) return;
+  const uint8_t done = a.finished ? a.finished[row] : 0;
+  if (a.scores[row] == kNegInf || done) return;
   const char* z = (const char*)a.logits + row * a.ld * TI::BYTES;
   const int64_t v0 = (int64_t)part * (kSpan * S) + tid * E;
   if (tid == 0) sh.n = 0;
-
+  // (past the row's end: its last vector again, cut below)
+  const int64_t last = (a.V - 1) / E * E;
   u32x4 x[S];
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    const int64_t v = v0 + s * kSpan;
-    if (v + E <= a.V) {
-      x[s] = __builtin_nontemporal_load((const u32x4*)(z + v * TI::BYTES));
-    } else {
-      constexpr uint32_t none = TI::BYTES == 2 ? 0xFF80FF80u : 0xFF800000u;
-      x[s] = u32x4{none, none, none, none};
+  for (int s = 0; s < S; ++s)
+    x[s] = __builtin_nontemporal_load((const u32x4*)(z + min(v0 + s * kSpan, last) * TI::BYTES));
+  if ((int64_t)(part + 1) * (kSpan * S) > a.V) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        if (v + e >= a.V) continue;
+        const bool out = v0 + s * kSpan + e >= a.V;
         if constexpr (TI::BYTES == 2) {
-          const uint32_t b = ((const uint16_t*)z)[v + e];
-          x[s][e / 2] = e & 1 ? (x[s][e / 2] & 0xFFFFu) | b << 16 : (x[s][e / 2] & 0xFFFF0000u) | b;
+          const uint32_t none = e & 1 ? 0xFF800000u : 0x0000FF80u;
+          const uint32_t keep = e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          x[s][e / 2] = out ? (x[s][e / 2] & keep) | none : x[s][e / 2];
         } else {
-          x[s][e] = ((const uint32_t*)z)[v + e];
+          x[s][e] = out ? 0xFF800000u : x[s][e];
         }
       }
     }
@@ -106,67 +161,102 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
     else
       return __uint_as_float(x[s][e]);
   };
-  float mine = kNegInf;  // (a NaN shows in the sum)
+  float top[S], mine = kNegInf;  // (a NaN shows in the sum)
 #pragma unroll
   for (int s = 0; s < S; ++s) {
+    top[s] = value(s, 0);
 #pragma unroll
-    for (int e = 0; e < E; ++e) mine = fmaxf(mine, value(s, e));
+    for (int e = 1; e < E; ++e) top[s] = fmaxf(top[s], value(s, e));
+    mine = fmaxf(mine, top[s]);
   }
-  // the lanes' maxima, sorted: their k-th bounds the candidates from below
-  const uint32_t sorted = wave_sort_desc(order_key(__float_as_uint(mine)));
-  sh.top[w][lane] = sorted;
-  if (lane == 0) sh.max[w] = key_value(sorted);
-  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < S; ++s) keep_packed(x[s]);
+  // What bounds the candidates from below: k lanes' maxima are not below it.  Up to 16, the
+  // largest of the waves' k-th, found by the bits of the keys; more, the k-th of all.
+  const uint32_t key = order_key(__float_as_uint(mine));
+  uint32_t bound = 0;
+  auto kth_of_all = [&]() {
+    sh.top[w][lane] = lanes_sorted(key);
+    __syncthreads();
+    const uint32_t ab = beam_merge_desc(sh.top[0][lane], sh.top[1][63 - lane]);
+    const uint32_t cd = beam_merge_desc(sh.top[2][lane], sh.top[3][63 - lane]);
+    const uint32_t all = beam_merge_desc(ab, (uint32_t)__shfl((int)cd, 63 - lane, 64));
+    return (uint32_t)__builtin_amdgcn_readlane((int)all, a.k - 1);
+  };
+  // (no key of a number is below that of the lowest; -inf has no mass)
+  auto number = [](uint32_t bound) {
+    return bound <= order_key(0xFF7FFFFFu) ? -3.4028234663852886e38f : key_value(bound);
+  };
+  if (a.k <= 16) {
+    constexpr int LOW = TI::BYTES == 2 ? 16 : 0;  // (bf16: keys vary above)
+#pragma unroll
+    for (int bit = 31; bit >= LOW; --bit) {
+      const uint32_t c = bound | (1u << bit);
+      if (__popcll(__ballot(key >= c)) >= a.k) bound = c;
+    }
+    const float m = lanes_max(mine);
+    if (lane == 0) {
+      sh.top[w][0] = bound;
+      sh.max[w] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kBeamWaves; ++i) bound = max(bound, sh.top[i][0]);
+  } else {
+    const float m = lanes_max(mine);
+    if (lane == 0) sh.max[w] = m;
+    bound = kth_of_all();
+  }
   float m = sh.max[0];
 #pragma unroll
   for (int i = 1; i < kBeamWaves; ++i) m = fmaxf(m, sh.max[i]);
-  const uint32_t ab = beam_merge_desc(sh.top[0][lane], sh.top[1][63 - lane]);
-  const uint32_t cd = beam_merge_desc(sh.top[2][lane], sh.top[3][63 - lane]);
-  const uint32_t all = beam_merge_desc(ab, (uint32_t)__shfl((int)cd, 63 - lane, 64));
-  const uint32_t bound = (uint32_t)__builtin_amdgcn_readlane((int)all, a.k - 1);
-  const float least = fmaxf(key_value(bound), -3.4028234663852886e38f);  // -inf has no mass
+  float least = number(bound);
 
   const float off = m == kNegInf ? 0.f : m;
-#pragma unroll
-  for (int s = 0; s < S; ++s) keep_packed(x[s]);
+  const bool far = !(fabsf(off) < kBeamNear);
+  const float c = far ? 0.f : rintf(off * kLog2e);
   double sum = 0.0;
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
+  auto add = [&](int s, auto is_far) {
+    constexpr bool FAR = decltype(is_far)::value;
     float t[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) t[e] = beam_term(value(s, e), off);
+    for (int e = 0; e < E; ++e) t[e] = beam_term(FAR ? value(s, e) - off : value(s, e), c);
     if constexpr (E == 8)
       sum += (double)(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
     else
       sum += (double)((t[0] + t[1]) + (t[2] + t[3]));
+  };
+  if (!far) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) add(s, std::false_type());
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s) add(s, std::true_type());
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  sum = lanes_sum(sum);
   if (lane == 0) sh.sum[w] = sum;
-
 #pragma unroll
-  for (int s = 0; s < S; ++s) keep_packed(x[s]);
-  const bool some = mine >= least;
-  if (__ballot(some)) {
+  for (int s = 0; s < S; ++s) {
+    if (__ballot(top[s] >= least) == 0) continue;  // (half the vectors, and most elements)
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (some && value(s, e) >= least) {
-          const uint32_t at = atomicAdd(&sh.n, 1u);
-          const uint32_t v = (uint32_t)(v0 + s * kSpan + e);
-          if (at < cap) cand[at] = (uint64_t)order_key(__float_as_uint(value(s, e))) << 32 | (uint32_t)~v;
-        }
+    for (int e = 0; e < E; ++e) {
+      const float f = value(s, e);
+      if (__ballot(f >= least) == 0) continue;
+      if (f >= least) {
+        const uint32_t at = atomicAdd(&sh.n, 1u);
+        const uint32_t v = (uint32_t)(v0 + s * kSpan + e);
+        if (at < cap) cand[at] = (uint64_t)order_key(__float_as_uint(f)) << 32 | (uint32_t)~v;
       }
     }
   }
   __syncthreads();
   uint32_t n = sh.n;
   if (n > cap) {
-    // Many that are equal to the bound: those above it (in fewer than k lanes), then the
+    // Too many: by the bound of all lanes, those above it (in fewer than k lanes), then the
     // equal ones slot by slot, whose tokens ascend, until there are enough.
     __syncthreads();
     if (tid == 0) sh.n = 0;
+    least = number(kth_of_all());
     __syncthreads();
     for (int equal = 0; equal < 2; ++equal) {
 #pragma unroll 1
@@ -222,6 +312,9 @@ __global__ void __launch_bounds__(kBeamThreads) k_beam_rows(BeamArgs a) {
     double t = sh.sum[0];
 #pragma unroll
     for (int i = 1; i < kBeamWaves; ++i) t += sh.sum[i];
+    // (from units of 2^c to units of exp(m))
+    constexpr double log2e = 1.4426950408889634;
+    if (!far) t *= exp2((double)c - (double)off * log2e);
     // (s NaN: a NaN or an infinity among the logits)
     *rec = BeamRec{t, m, n};
   }
@@ -351,10 +444,32 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     sh.total = W;
   }
   __syncthreads();
+  // the records of the group, one to a wave at a time; four on their way (of the first four,
+  // beside the rows' sums)
+  const uint32_t recs = W * a.parts;
+  const BeamRec* rec = (const BeamRec*)a.recs + b * recs;
+  const uint64_t* cand = a.cands + b * recs * (int64_t)kBeamMax;
+  constexpr int AHEAD = 4;
+  uint64_t cs[AHEAD];
+  uint32_t ns[AHEAD];
+  auto fetch = [&](uint32_t p0) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      // (past a record's count, or a beam that has none, lies what the workspace held)
+      const uint32_t p = min(p0 + i * kMergeWaves, recs - 1);
+      cs[i] = cand[(int64_t)p * kBeamMax + lane];
+      ns[i] = rec[p].n;
+    }
+  };
+  fetch(wave);
   for (int w = wave; w < W; w += kMergeWaves) {
     const int64_t row = b * W + w;
-    BeamRow r;
+    const BeamRec* mine = rec + w * a.parts;
+    // (a row of up to 64 parts is read once)
+    BeamRec one = mine[min((uint32_t)lane, a.parts - 1)];
     const float score = a.scores[row];
+    const uint8_t done = a.finished ? a.finished[row] : 0;
+    BeamRow r;
     r.score = (double)score;
     r.l = 0.0;
     r.m = 0.f;
@@ -363,23 +478,22 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
       r.kind = kBeamBad;
     } else if (score == kNegInf) {
       r.kind = kBeamDead;
-    } else if (a.finished && a.finished[row]) {
+    } else if (done) {
       r.kind = kBeamDone;
     } else {
-      const BeamRec* rec = (const BeamRec*)a.recs + row * a.parts;
-      float m = kNegInf;
-      for (uint32_t p = lane; p < a.parts; p += 64) m = fmaxf(m, rec[p].m);
-      m = wave_max(m);
+      float m = lane < (int)a.parts ? one.m : kNegInf;
+      for (uint32_t p = lane + 64; p < a.parts; p += 64) m = fmaxf(m, mine[p].m);
+      m = lanes_max(m);
       double s = 0.0;
       uint32_t found = 0;
       for (uint32_t p = lane; p < a.parts; p += 64) {
-        found += rec[p].n;
+        if (p >= 64) one = mine[p];
+        found += one.n;
         // (an empty part has sum 0, one with a NaN or an infinity NaN)
-        const double d = rec[p].m == kNegInf ? 0.0 : (double)rec[p].m - (double)m;
-        s += rec[p].s * exp(d);
+        const double d = one.m == kNegInf ? 0.0 : (double)one.m - (double)m;
+        s += one.s * exp(d);
       }
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+      s = lanes_sum(s);
       if (found) atomicAdd(&sh.total, found);
       r.m = m;
       if (!(s < __builtin_huge_val()))
@@ -412,19 +526,12 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     return;
   }
   uint32_t n = sh.n;
-  // the records of the group, one to a wave at a time
-  const uint32_t recs = W * a.parts;
-  const BeamRec* rec = (const BeamRec*)a.recs + b * recs;
-  const uint64_t* cand = a.cands + b * recs * (int64_t)kBeamMax;
-  auto take = [&](uint32_t p) {
+  auto take = [&](uint32_t p, uint64_t c, uint32_t count) {
     const uint32_t w = p / a.parts;
     const BeamRow r = sh.row[w];
     if (r.kind != kBeamLive) return;
-    // (read beside the count: past it lies what the workspace held)
-    const uint64_t c = cand[(int64_t)p * kBeamMax + lane];
-    const bool mine = lane < (int)rec[p].n;
     const double s = r.score + (((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l);
-    const uint64_t in = __ballot(mine && s > -__builtin_huge_val());
+    const uint64_t in = __ballot(lane < (int)count && s > -__builtin_huge_val());
     uint32_t to = 0;
     if (lane == 0) to = atomicAdd(&sh.n, (uint32_t)__popcll(in));
     to = __builtin_amdgcn_readfirstlane(to) + (uint32_t)__popcll(in & ((1ull << lane) - 1));
@@ -433,21 +540,25 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
       sh.at[to] = (uint64_t)w << 32 | (uint32_t)~(uint32_t)c;
     }
   };
-  if (sh.total <= kMergeCap) {
-    for (uint32_t p = wave; p < recs; p += kMergeWaves) take(p);
-    __syncthreads();
-    n = sh.n;
-    __syncthreads();
-  } else {
-    for (uint32_t p0 = 0; p0 < recs; p0 += kMergeWaves) {
-      if (n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
-      if (p0 + wave < recs) take(p0 + wave);
-      __syncthreads();
-      n = sh.n;
-      __syncthreads();
+  const bool fits = sh.total <= kMergeCap;
+  for (uint32_t p0 = 0; p0 < recs; p0 += AHEAD * kMergeWaves) {
+    if (p0 > 0) fetch(p0 + wave);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const uint32_t p = p0 + i * kMergeWaves + wave;
+      if (!fits && n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
+      if (p < recs) take(p, cs[i], ns[i]);
+      if (!fits) {
+        __syncthreads();
+        n = sh.n;
+        __syncthreads();
+      }
     }
   }
-  while (n > 128) {
+  __syncthreads();
+  n = sh.n;
+  __syncthreads();
+  while (n > 64) {
     const uint32_t left = merge_cut(sh, n, k, 1024);
     if (left == n) break;
     n = left;
@@ -456,6 +567,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     const double s = sh.score[i];
     const uint64_t at = sh.at[i];
     int rank = 0;
+#pragma unroll 8
     for (uint32_t e = 0; e < n; ++e) rank += beam_before(sh.score[e], sh.at[e], s, at) ? 1 : 0;
     if (rank >= k) continue;
     const int w = (int)(at >> 32);
@@ -559,10 +671,10 @@ template <class TI, int S>
 hipError_t beam_s(BeamArgs a, hipStream_t st) {
   const int64_t rows = a.B * a.W;
   const int64_t most = (((int64_t)1 << 32) / kBeamThreads - 1) / a.parts;
+  const size_t lds = beam_cap<TI, S>(a.k) * sizeof(uint64_t);
   for (int64_t r0 = 0; r0 < rows; r0 += most) {
     const int64_t n = rows - r0 < most ? rows - r0 : most;
     a.row0 = r0;
-    const size_t lds = beam_cap<TI, S>(a.k) * sizeof(uint64_t);
     hipLaunchKernelGGL((k_beam_rows<TI, S>), dim3((unsigned)(n * a.parts)), dim3(kBeamThreads), lds,
                        st, a);
     const hipError_t e = hipGetLastError();

@@ -175,19 +175,19 @@ __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t token, 
   }
 }
 
-template <class TO>
+template <class TO, int E>
 __device__ __forceinline__ void store_sum(const EmbedGradArgs& a, int64_t v, int64_t c,
-                                          float (&f)[4]) {
+                                          float (&f)[E]) {
   char* row = (char*)a.out + v * a.ldo * TO::BYTES;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) f[e] *= a.scale;
+  for (int e = 0; e < E; ++e) f[e] *= a.scale;
   if (a.accumulate) {
-    float x[4];
-    load_wide<TO, 4>(row, c, a.H, x);
+    float x[E];
+    load_wide<TO, E>(row, c, a.H, x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] += x[e];
+    for (int e = 0; e < E; ++e) f[e] += x[e];
   }
-  store_wide<TO, 4, true>(row, c, a.H, f);
+  store_wide<TO, E, true>(row, c, a.H, f);
 }
 
 // Two launches: the entries with tokens are read and summed, then the empty ones are filled
@@ -262,26 +262,27 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_sums(EmbedGradArgs a) {
   add_rows<TI, VPL, 8 / VPL>(a, lane < e - s ? a.perm[s + lane] : 0, e - s, c, f);
 #pragma unroll
   for (int i = 0; i < VPL; ++i)
-    if (c + 256 * i < a.H) store_sum<TO>(a, v, c + 256 * i, f[i]);
+    if (c + 256 * i < a.H) store_sum<TO, 4>(a, v, c + 256 * i, f[i]);
 }
 
-// One wavefront to a tile, or an entry, and a chunk of 256 columns: the tiles' sums of a long
-// entry, in order, by the wavefronts of the tile that it begins in; and zeros where
-// there is no token.  (One store to a lane, in short waves side by side, is as fast as a
-// plain fill: 370 us where one takes 361, for 151,936 by 4,096 fp32.  Four stores to a lane
-// took 425, eight rows to a wave 440.)
+// One wavefront to a tile, or an entry, and a chunk of 64 E columns, a store of 16 bytes to a
+// lane: the tiles' sums of a long entry, in order, by the wavefronts of the tile that it
+// begins in; and zeros where there is no token.  (One store to a lane, in short waves
+// side by side, is as fast as a plain fill: 370 us where one takes 361, for 151,936 by 4,096
+// fp32.  Four stores to a lane took 425, eight rows to a wave 440.)
 template <class TO>
 __global__ void __launch_bounds__(kEmbThreads) k_embed_rest(EmbedGradArgs a) {
+  constexpr int E = 16 / TO::BYTES;
   const uint32_t u = blockIdx.x * kEmbWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (u >= a.units) return;
   const int lane = threadIdx.x & 63;
   const int64_t row = a.row0 + u / a.chunks;
-  const int64_t c = (int64_t)(u % a.chunks) * 256 + lane * 4;
-  float f[4] = {0.f, 0.f, 0.f, 0.f};
+  const int64_t c = (int64_t)(u % a.chunks) * (64 * E) + lane * E;
+  float f[E] = {};
   int64_t v = row - a.tiles;
   if (v >= 0) {
     if (a.start[v] != a.start[v + 1]) return;
-    if (c < a.H) store_wide<TO, 4, true>((char*)a.out + v * a.ldo * TO::BYTES, c, a.H, f);
+    if (c < a.H) store_wide<TO, E, true>((char*)a.out + v * a.ldo * TO::BYTES, c, a.H, f);
     return;
   }
   const TileLane t = tile_lane(a, row);
@@ -293,12 +294,18 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_rest(EmbedGradArgs a) {
   const int64_t s = __builtin_amdgcn_readlane(t.s, l), e = __builtin_amdgcn_readlane(t.e, l);
   if (c >= a.H) return;
   const int64_t t1 = (e + kEmbTile - 1) / kEmbTile;
-  f32x4 sum = *(const f32x4*)(a.partial + (row * 2 + (s > row * kEmbTile ? 1 : 0)) * a.hp + c);
-#pragma unroll 8
-  for (int64_t i = row + 1; i < t1; ++i) sum += *(const f32x4*)(a.partial + i * 2 * a.hp + c);
+  f32x4 sum[E / 4];
+  const float* from = a.partial + (row * 2 + (s > row * kEmbTile ? 1 : 0)) * a.hp + c;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) f[k] = sum[k];
-  store_sum<TO>(a, v, c, f);
+  for (int k = 0; k < E / 4; ++k) sum[k] = *(const f32x4*)(from + 4 * k);
+#pragma unroll 8
+  for (int64_t i = row + 1; i < t1; ++i) {
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) sum[k] += *(const f32x4*)(a.partial + i * 2 * a.hp + c + 4 * k);
+  }
+#pragma unroll
+  for (int k = 0; k < E; ++k) f[k] = sum[k / 4][k % 4];
+  store_sum<TO, E>(a, v, c, f);
 }
 
 // Few tokens, in one launch: a wavefront looks for its entry's tokens among the ids itself.
@@ -322,7 +329,7 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_few(EmbedGradArgs a) {
     }
   }
   if (a.accumulate && !any) return;
-  if (c < a.H) store_sum<TO>(a, v, c, f[0]);
+  if (c < a.H) store_sum<TO, 4>(a, v, c, f[0]);
 }
 
 // Launches over rows (tokens, tiles, entries) in units of a row's chunk.
@@ -373,7 +380,7 @@ hipError_t embed_grad_t(EmbedGradArgs a, hipStream_t st) {
 #undef OPD_SUMS
   if (e != hipSuccess) return e;
   // (added to: what has no token stays)
-  return launch_units(a, a.tiles + (a.accumulate ? 0 : a.V), 256,
+  return launch_units(a, a.tiles + (a.accumulate ? 0 : a.V), 64 * (16 / TO::BYTES),
                       [&](const EmbedGradArgs& b, dim3 g) {
                         hipLaunchKernelGGL((k_embed_rest<TO>), g, dim3(kEmbThreads), 0, st, b);
                       });

@@ -106,14 +106,20 @@ struct OuterArgs {
   int64_t stride;
   float* out;             // [splits][G, r, ldo]
   int64_t ldo;
+  float* sum;             // [G, r, lds] the result
+  int64_t lds;
   uint32_t chunks;        // of columns (the launch sets it)
+};
+struct OuterPair {
+  OuterArgs a[2];         // da, db
+  uint32_t blocks;        // of the first (the launch sets it)
 };
 hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t stream);
 hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t stream);
 // adds the parts up in the first one's place, for N tokens
 hipError_t launch_low_sum(const LowArgs& a, int64_t N, hipStream_t stream);
 hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t stream);
-hipError_t launch_outer(const OuterArgs& a, int x_dt, float* out, int64_t ldo, hipStream_t stream);
+hipError_t launch_outer(const OuterPair& pair, int x_dt, int y_dt, hipStream_t stream);
 
 // Beam selection and reordering (opd_beam_select, opd_reorder_beams).
 constexpr int kBeamMax = 64;
