@@ -689,6 +689,12 @@ def _padded(M: int, dtype) -> int:
     return _blocks(M, each) * each
 
 
+def _rows(N: int, M: int, ld: int, dtype, dev) -> torch.Tensor:
+    """[N, M], rows ld elements apart."""
+    t = torch.empty((N, ld), dtype=dtype, device=dev)
+    return t if ld == M else t[:, :M]
+
+
 def _need_workspace(workspace, dev):
     if workspace is not None:
         _need(workspace, "workspace", (torch.uint8,), (workspace.numel(),), dev)
@@ -722,7 +728,7 @@ def embed_tokens(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, 
     with _On(dev, stream) as s:
         if out is None:
             ldo = _padded(H, dtype)
-            out = torch.empty((N, ldo), dtype=dtype, device=dev)[:, :H]
+            out = _rows(N, H, ldo, dtype, dev)
         rc = lib().opd_embed_tokens(_at(table), _dt(table), V, H, ld, _at(ids), N, scale, _at(out),
                                     _dt(out), ldo, s)
     if rc != 0:
@@ -755,7 +761,7 @@ def embed_grads(grad: torch.Tensor, ids: torch.Tensor, V: int, *, scale: float =
     with _On(dev, stream) as s:
         if out is None:
             ldo = _padded(H, dtype)
-            out = torch.empty((V, ldo), dtype=dtype, device=dev)[:, :H]
+            out = _rows(V, H, ldo, dtype, dev)
         ws, nbytes = _workspace(workspace, int(lib().opd_embed_workspace_bytes(N, V, H)), dev)
         rc = lib().opd_embed_grads(_at(grad), _dt(grad), N, H, ldy, _at(ids), V, scale, _at(out),
                                    _dt(out), ldo, 1 if accumulate else 0, _at(ws), nbytes, s)
@@ -823,7 +829,7 @@ def add_adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Ten
     with _On(dev, stream) as s:
         if out is None:
             ldo = _padded(O, y.dtype)
-            out = torch.empty((N, ldo), dtype=y.dtype, device=dev)[:, :O]
+            out = _rows(N, O, ldo, y.dtype, dev)
         low = torch.empty((N, r), dtype=torch.float32, device=dev) if want_low else None
         ws, nbytes = _workspace(workspace, int(lib().opd_adapter_workspace_bytes(
             N, H, O, G, r, dt, ydt, 0)), dev)
@@ -972,7 +978,11 @@ def reorder_beams(states: torch.Tensor, parents: torch.Tensor, *, out=None, stre
     W = states.shape[0] // B if B else k
     outer, inner, stride, apart = _slices(states, "states")
     shape = (B * k,) + tuple(states.shape[1:])
-    if out is not None:
+    if out is states:
+        if k != W:
+            raise ValueError("out must be states, with k == W, or not overlap it")
+        to_outer, to_inner, to_stride, to_apart = outer, inner, stride, apart
+    elif out is not None:
         if not isinstance(out, torch.Tensor) or out.dtype != states.dtype or \
                 tuple(out.shape) != shape or out.device != dev:
             raise ValueError("out must be %s %s on %s" % (shape, states.dtype, dev))

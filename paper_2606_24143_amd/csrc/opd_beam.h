@@ -335,6 +335,7 @@ constexpr int kMergeEach = kMergeCap / kMergeThreads;
 struct MergeLds {
   double score[kMergeCap];
   uint64_t at[kMergeCap];  // beam, token
+  uint32_t rank[kMergeCap];
   BeamRow row[kBeamMax];
   uint32_t bound[2][kMergeWaves];
   uint32_t n, bad, total;
@@ -395,16 +396,22 @@ __device__ __forceinline__ uint32_t merge_cut(MergeLds& sh, uint32_t n, int k, u
     if (tid == 0) sh.n = 0;
     __syncthreads();
   }
-  uint32_t mine = 0;
+  uint64_t in[kMergeEach];
+  auto reserve = [&]() {  // where a wave's go; sh.n becomes their number
+    uint32_t mine = 0, to = 0;
 #pragma unroll
-  for (int i = 0; i < kMergeEach; ++i) {
-    if (key[i] < bound) key[i] = 0;
-    mine += key[i] != 0 ? 1u : 0u;
-  }
-  if (mine) atomicAdd(&sh.n, mine);
-  __syncthreads();
+    for (int i = 0; i < kMergeEach; ++i) {
+      in[i] = __ballot(key[i] != 0);
+      mine += (uint32_t)__popcll(in[i]);
+    }
+    if (lane == 0 && mine) to = atomicAdd(&sh.n, mine);
+    __syncthreads();
+    return (uint32_t)__builtin_amdgcn_readfirstlane(to);
+  };
+#pragma unroll
+  for (int i = 0; i < kMergeEach; ++i) key[i] = key[i] < bound ? 0u : key[i];
+  uint32_t to = reserve();
   uint32_t left = sh.n;
-  __syncthreads();
   if (left > most) {
 #pragma unroll
     for (int i = 0; i < kMergeEach; ++i) {
@@ -413,17 +420,20 @@ __device__ __forceinline__ uint32_t merge_cut(MergeLds& sh, uint32_t n, int k, u
         rank += beam_before(sh.score[e], sh.at[e], s[i], at[i]) ? 1 : 0;
       key[i] = rank < k ? key[i] : 0u;
     }
-    left = min(n, (uint32_t)k);
     __syncthreads();
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    to = reserve();
+    left = sh.n;
   }
-  if (tid == 0) sh.n = 0;
-  __syncthreads();
 #pragma unroll
   for (int i = 0; i < kMergeEach; ++i) {
-    if (key[i] == 0) continue;
-    const uint32_t to = atomicAdd(&sh.n, 1u);
-    sh.score[to] = s[i];
-    sh.at[to] = at[i];
+    if (in[i] >> lane & 1) {
+      const uint32_t p = to + (uint32_t)__popcll(in[i] & ((1ull << lane) - 1));
+      sh.score[p] = s[i];
+      sh.at[p] = at[i];
+    }
+    to += (uint32_t)__popcll(in[i]);
   }
   __syncthreads();
   return left;
@@ -444,12 +454,12 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     sh.total = W;
   }
   __syncthreads();
-  // the records of the group, one to a wave at a time; four on their way (of the first four,
+  // the records of the group, one to a wave at a time; eight on their way (the first,
   // beside the rows' sums)
   const uint32_t recs = W * a.parts;
   const BeamRec* rec = (const BeamRec*)a.recs + b * recs;
   const uint64_t* cand = a.cands + b * recs * (int64_t)kBeamMax;
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 8;
   uint64_t cs[AHEAD];
   uint32_t ns[AHEAD];
   auto fetch = [&](uint32_t p0) {
@@ -526,28 +536,51 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     return;
   }
   uint32_t n = sh.n;
-  auto take = [&](uint32_t p, uint64_t c, uint32_t count) {
-    const uint32_t w = p / a.parts;
+  // scores of a record's candidates, those that are one
+  auto take = [&](uint32_t p, uint32_t w, uint64_t c, uint32_t count, double& score) -> uint64_t {
     const BeamRow r = sh.row[w];
-    if (r.kind != kBeamLive) return;
-    const double s = r.score + (((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l);
-    const uint64_t in = __ballot(lane < (int)count && s > -__builtin_huge_val());
-    uint32_t to = 0;
-    if (lane == 0) to = atomicAdd(&sh.n, (uint32_t)__popcll(in));
-    to = __builtin_amdgcn_readfirstlane(to) + (uint32_t)__popcll(in & ((1ull << lane) - 1));
+    score = r.score + (((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l);
+    return __ballot(p < recs && r.kind == kBeamLive && lane < (int)count &&
+                    score > -__builtin_huge_val());
+  };
+  auto put = [&](uint32_t w, uint64_t c, double score, uint64_t in, uint32_t to) {
+    to += (uint32_t)__popcll(in & ((1ull << lane) - 1));
     if (in >> lane & 1) {
-      sh.score[to] = s;
+      sh.score[to] = score;
       sh.at[to] = (uint64_t)w << 32 | (uint32_t)~(uint32_t)c;
     }
+  };
+  auto reserve = [&](uint32_t count) {
+    uint32_t to = 0;
+    if (lane == 0) to = atomicAdd(&sh.n, count);
+    return (uint32_t)__builtin_amdgcn_readfirstlane(to);
   };
   const bool fits = sh.total <= kMergeCap;
   for (uint32_t p0 = 0; p0 < recs; p0 += AHEAD * kMergeWaves) {
     if (p0 > 0) fetch(p0 + wave);
+    // (the records' beams: one division, a record to a lane)
+    const uint32_t beam = min(p0 + lane * kMergeWaves + wave, recs - 1) / a.parts;
+    uint32_t w[AHEAD];
+    double ss[AHEAD];
+    uint64_t in[AHEAD];
+    uint32_t all = 0;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const uint32_t p = p0 + i * kMergeWaves + wave;
-      if (!fits && n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
-      if (p < recs) take(p, cs[i], ns[i]);
+      w[i] = (uint32_t)__builtin_amdgcn_readlane((int)beam, i);
+      in[i] = take(p0 + i * kMergeWaves + wave, w[i], cs[i], ns[i], ss[i]);
+      all += (uint32_t)__popcll(in[i]);
+    }
+    uint32_t to = fits ? reserve(all) : 0;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const uint32_t count = (uint32_t)__popcll(in[i]);
+      if (!fits) {
+        // (each time as many as kMergeThreads at most)
+        if (n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
+        to = reserve(count);
+      }
+      put(w[i], cs[i], ss[i], in[i], to);
+      to += count;
       if (!fits) {
         __syncthreads();
         n = sh.n;
@@ -563,15 +596,26 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     if (left == n) break;
     n = left;
   }
-  for (uint32_t i = tid; i < n; i += kMergeThreads) {
+  // each one's rank: a candidate to a lane, a 16th of the others to a wave
+  for (uint32_t i = tid; i < n; i += kMergeThreads) sh.rank[i] = 0;
+  __syncthreads();
+  for (uint32_t i0 = 0; i0 < n; i0 += 64) {
+    const uint32_t i = min(i0 + lane, n - 1);
     const double s = sh.score[i];
     const uint64_t at = sh.at[i];
-    int rank = 0;
-#pragma unroll 8
-    for (uint32_t e = 0; e < n; ++e) rank += beam_before(sh.score[e], sh.at[e], s, at) ? 1 : 0;
-    if (rank >= k) continue;
+    uint32_t rank = 0;
+#pragma unroll 4
+    for (uint32_t e = wave; e < n; e += kMergeWaves)
+      rank += beam_before(sh.score[e], sh.at[e], s, at) ? 1u : 0u;
+    if (i0 + lane < n && rank) atomicAdd(&sh.rank[i], rank);
+  }
+  __syncthreads();
+  for (uint32_t i = tid; i < n; i += kMergeThreads) {
+    const uint32_t rank = sh.rank[i];
+    if (rank >= (uint32_t)k) continue;
+    const uint64_t at = sh.at[i];
     const int w = (int)(at >> 32);
-    scores[rank] = (float)s;
+    scores[rank] = (float)sh.score[i];
     parents[rank] = w;
     ids[rank] = sh.row[w].kind == kBeamDone ? -1 : (int32_t)(uint32_t)at;
   }

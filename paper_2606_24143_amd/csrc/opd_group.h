@@ -52,8 +52,9 @@ __device__ __forceinline__ uint64_t lanes_of_key(uint64_t in, int32_t k, int bit
   if ((__ballot(k == one) & in) == in) return in;
   uint64_t same = in;
   for (int bit = 0; bit < bits; ++bit) {
-    const uint64_t b = __ballot(k >> bit & 1);
-    same &= k >> bit & 1 ? b : ~b;
+    const int32_t mine = -(k >> bit & 1);  // (all bits, or none)
+    const uint64_t b = __ballot(mine != 0);
+    same &= ~(b ^ (uint64_t)(int64_t)mine);
   }
   return same;
 }
@@ -80,9 +81,13 @@ __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int coun
   uint32_t below = 0;
   constexpr int A = 8;  // keys on their way at once; up to 64 A of a wave's stay in registers
   int32_t ks[A];
+  uint64_t sames[A];
+  const bool held = part <= 64 * A;
   auto load = [&](int64_t n) {
 #pragma unroll
-    for (int i = 0; i < A; ++i) ks[i] = n + 64 * i + lane < n1 ? key(n + 64 * i + lane) : -1;
+    for (int i = 0; i < A; ++i) ks[i] = key(min(n + 64 * i + lane, n1 - 1));
+#pragma unroll
+    for (int i = 0; i < A; ++i) ks[i] = n + 64 * i + lane < n1 ? ks[i] : -1;
   };
   for (int64_t n = n0; n < n1; n += 64 * A) {
     load(n);
@@ -96,18 +101,22 @@ __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int coun
       } else {
         const uint64_t in = __ballot(mine);
         if (!in) continue;
-        const uint64_t same = lanes_of_key(in, k, bits);
-        if (mine && lane == __ffsll((long long)same) - 1)
-          atomicAdd(&sh.at[w][k], (uint32_t)__popcll(same));
+        sames[i] = lanes_of_key(in, k, bits);
+        if (mine && lane == __ffsll((long long)sames[i]) - 1)
+          atomicAdd(&sh.at[w][k], (uint32_t)__popcll(sames[i]));
       }
     }
   }
-  below = (uint32_t)__shfl((int)wave_incl_scan_u32(below), 63, 64);
-  if (lane == 0) sh.below[w] = below;
+  if (lo > 0) {
+    below = (uint32_t)__shfl((int)wave_incl_scan_u32(below), 63, 64);
+    if (lane == 0) sh.below[w] = below;
+  }
   __syncthreads();
   uint32_t base = 0;
+  if (lo > 0) {
 #pragma unroll
-  for (int i = 0; i < kGroupWaves; ++i) base += sh.below[i];
+    for (int i = 0; i < kGroupWaves; ++i) base += sh.below[i];
+  }
   uint32_t mine = 0;
   if ((int)threadIdx.x < count) {
 #pragma unroll
@@ -129,13 +138,13 @@ __device__ __forceinline__ uint32_t group_tokens(int64_t N, int32_t lo, int coun
   // A wave's tokens in order, 64 at a time: a lane finds those of its key by the keys'
   // bits, and the first of them takes their places.
   for (int64_t m = n0; m < n1; m += 64 * A) {
-    if (part > 64 * A) load(m);
+    if (!held) load(m);
 #pragma unroll
     for (int i = 0; i < A; ++i) {
       const int32_t k = ks[i] - lo;
       const uint64_t all = __ballot(ks[i] >= lo && k < count);
       if (!all) continue;
-      const uint64_t same = lanes_of_key(all, k, bits);
+      const uint64_t same = FEW || !held ? lanes_of_key(all, k, bits) : sames[i];
       if (all >> lane & 1) {
         const int lead = __ffsll((long long)same) - 1;
         uint32_t at = 0;
