@@ -182,7 +182,10 @@ struct Staged {
 };
 
 template <class TX, class TW, int RT, int MT>
-__global__ void __launch_bounds__(kLowThreads, 2) k_low(LowArgs a) {
+__global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
+  const bool second = (int)blockIdx.y >= pair.a[0].splits;
+  const LowArgs& a = pair.a[second];
+  const int split = (int)blockIdx.y - (second ? pair.a[0].splits : 0);
   constexpr bool BF = TX::BYTES == 2 && TW::BYTES == 2;
   constexpr int STEP = BF ? 64 : 32;
   typedef std::conditional_t<BF, u32x4, f32x4> V;
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const int64_t d0 = (int64_t)blockIdx.y * a.span;
+  const int64_t d0 = (int64_t)split * a.span;
   const int64_t d1 = d0 + a.span < a.D ? d0 + a.span : a.D;
   struct Step {
     SX x;
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowArgs a) {
     }
   }
   __syncthreads();
-  float* out = a.out + (int64_t)blockIdx.y * a.stride;
+  float* out = a.out + (int64_t)split * a.stride;
   for (int i = threadIdx.x; i < count * a.r; i += kLowThreads) {
     const int n = i / a.r, c = i % a.r;
     float f = sums(0, n, c);
@@ -820,7 +823,9 @@ __global__ void __launch_bounds__(kOutThreads, RT == 1 ? 4 : 2) k_outer(OuterPai
 }
 
 // The parts of t or u, added in order.
-__global__ void __launch_bounds__(256) k_low_sum(LowArgs a, int64_t n) {
+__global__ void __launch_bounds__(256) k_low_sum(LowPair pair, int64_t n) {
+  const LowArgs& a = pair.a[blockIdx.y];
+  if (a.splits <= 1) return;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   float f = a.out[i];
@@ -845,26 +850,28 @@ __global__ void __launch_bounds__(256) k_outer_sum(OuterPair pair) {
 }
 
 template <class TX, class TW, int RT>
-hipError_t low_r(const LowArgs& a, hipStream_t st) {
+hipError_t low_r(const LowPair& p, hipStream_t st) {
+  const int64_t tiles = p.a[0].max_tiles;
+  const int splits = p.a[0].splits + p.a[1].splits;
   // 32 tokens to a workgroup read the adapter half as often, where that leaves enough of them
   if constexpr (RT <= 4) {
-    if (a.max_tiles * a.splits >= 100) {
-      const dim3 grid((unsigned)(a.max_tiles * (kAdTile / 32)), (unsigned)a.splits);
-      hipLaunchKernelGGL((k_low<TX, TW, RT, 2>), grid, dim3(kLowThreads), 0, st, a);
+    if (tiles * splits >= 100) {
+      const dim3 grid((unsigned)(tiles * (kAdTile / 32)), (unsigned)splits);
+      hipLaunchKernelGGL((k_low<TX, TW, RT, 2>), grid, dim3(kLowThreads), 0, st, p);
       return hipGetLastError();
     }
   }
-  const dim3 grid((unsigned)(a.max_tiles * (kAdTile / 16)), (unsigned)a.splits);
-  hipLaunchKernelGGL((k_low<TX, TW, RT, 1>), grid, dim3(kLowThreads), 0, st, a);
+  const dim3 grid((unsigned)(tiles * (kAdTile / 16)), (unsigned)splits);
+  hipLaunchKernelGGL((k_low<TX, TW, RT, 1>), grid, dim3(kLowThreads), 0, st, p);
   return hipGetLastError();
 }
 template <class TX, class TW>
-hipError_t low_t(const LowArgs& a, hipStream_t st) {
-  const int rt = (a.r + 15) / 16;
-  return rt == 1   ? low_r<TX, TW, 1>(a, st)
-         : rt == 2 ? low_r<TX, TW, 2>(a, st)
-         : rt <= 4 ? low_r<TX, TW, 4>(a, st)
-                   : low_r<TX, TW, 8>(a, st);
+hipError_t low_t(const LowPair& p, hipStream_t st) {
+  const int rt = (p.a[0].r + 15) / 16;
+  return rt == 1   ? low_r<TX, TW, 1>(p, st)
+         : rt == 2 ? low_r<TX, TW, 2>(p, st)
+         : rt <= 4 ? low_r<TX, TW, 4>(p, st)
+                   : low_r<TX, TW, 8>(p, st);
 }
 
 template <class TW, class TY>
@@ -920,15 +927,16 @@ hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t st) {
-  if (w_dt == F32) return low_t<InF32, InF32>(a, st);
-  return x_dt == BF16 ? low_t<InBf16, InBf16>(a, st) : low_t<InF32, InBf16>(a, st);
+hipError_t launch_low(const LowPair& p, int x_dt, int w_dt, hipStream_t st) {
+  if (w_dt == F32) return low_t<InF32, InF32>(p, st);
+  return x_dt == BF16 ? low_t<InBf16, InBf16>(p, st) : low_t<InF32, InBf16>(p, st);
 }
 
-hipError_t launch_low_sum(const LowArgs& a, int64_t N, hipStream_t st) {
-  if (a.splits == 1) return hipSuccess;
-  hipLaunchKernelGGL(k_low_sum, dim3((unsigned)((N * a.ldo + 255) / 256)), dim3(256), 0, st, a,
-                     N * a.ldo);
+hipError_t launch_low_sum(const LowPair& p, int64_t N, hipStream_t st) {
+  if (p.a[0].splits <= 1 && p.a[1].splits <= 1) return hipSuccess;
+  const int64_t n = N * p.a[0].ldo;
+  hipLaunchKernelGGL(k_low_sum, dim3((unsigned)((n + 255) / 256), p.a[1].splits > 0 ? 2 : 1),
+                     dim3(256), 0, st, p, n);
   return hipGetLastError();
 }
 

@@ -426,7 +426,7 @@ AdaptLayout adapt_layout(int64_t N, int64_t H, int64_t O, int32_t G, int32_t r, 
 }
 // (a launch has fewer than 2^32 work-items)
 bool adapt_fits(const AdaptLayout& l, int64_t D, int32_t G, bool backward) {
-  const int64_t chunks = (D + 63) / 64, splits = l.splits_x > l.splits_y ? l.splits_x : l.splits_y;
+  const int64_t chunks = (D + 63) / 64, splits = l.splits_x + l.splits_y;
   if (l.max_tiles * 4 * 512 * splits > kMaxGridLanes) return false;
   if (!backward) return true;
   return (int64_t)G * l.outer * 2 * chunks * 2 * 512 <= kMaxGridLanes;
@@ -934,7 +934,7 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
                        l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
-  err = opd::launch_low(t, dtype, dtype, st);
+  err = opd::launch_low(opd::LowPair{{t, {}}}, dtype, dtype, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r,
                           opd::LowRef{t.out, t.ldo, t.stride, t.splits, r}, scales, b, ldb, O, y,
@@ -972,23 +972,22 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
                             (opd::AdTile*)(ws + l.tiles), l.max_tiles};
   hipError_t err = opd::launch_adapt_plan(plan, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
-  opd::LowRef tref{low, r, 0, 1, r};
-  if (N > 0) {
-    if (!low) {
-      const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
-                           l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
-      err = opd::launch_low(t, dtype, dtype, st);
-      if (err == hipSuccess) err = opd::launch_low_sum(t, N, st);
-      if (err != hipSuccess) return OPD_ERR_HIP;
-      tref = opd::LowRef{t.out, t.ldo, t.stride, 1, r};
-    }
-  }
+  const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
+                       l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
   const opd::LowArgs u{plan.tiles, plan.perm, l.max_tiles, G, r, dy, b, lddy, ldb, O,
                        l.splits_y, l.span_y, N * l.ldt, (float*)(ws + l.u), l.ldt};
   const opd::LowRef uref{u.out, u.ldo, u.stride, 1, r};
+  const opd::LowRef tref = low ? opd::LowRef{low, r, 0, 1, r} : opd::LowRef{t.out, t.ldo, t.stride, 1, r};
   if (N > 0) {
-    err = opd::launch_low(u, y_dtype, dtype, st);
-    if (err == hipSuccess) err = opd::launch_low_sum(u, N, st);
+    // (both products in one launch where their operands are of the same types)
+    opd::LowPair first{{u, {}}}, then{{t, {}}};
+    if (!low && dtype == y_dtype) first.a[1] = t;
+    err = opd::launch_low(first, y_dtype, dtype, st);
+    if (err == hipSuccess) err = opd::launch_low_sum(first, N, st);
+    if (err == hipSuccess && !low && dtype != y_dtype) {
+      err = opd::launch_low(then, dtype, dtype, st);
+      if (err == hipSuccess) err = opd::launch_low_sum(then, N, st);
+    }
     if (err != hipSuccess) return OPD_ERR_HIP;
   }
   const int64_t hp = (H + 3) / 4 * 4, op = (O + 3) / 4 * 4, gr = (int64_t)G * r;

@@ -70,6 +70,9 @@ struct LowArgs {
   float* out;             // [splits][N, ldo]
   int64_t ldo;
 };
+struct LowPair {
+  LowArgs a[2];           // of one plan; the second with no splits: there is none
+};
 // what they are, to the kernels that read them
 struct LowRef {
   const float* p;
@@ -115,9 +118,9 @@ struct OuterPair {
   uint32_t blocks;        // of the first (the launch sets it)
 };
 hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t stream);
-hipError_t launch_low(const LowArgs& a, int x_dt, int w_dt, hipStream_t stream);
+hipError_t launch_low(const LowPair& pair, int x_dt, int w_dt, hipStream_t stream);
 // adds the parts up in the first one's place, for N tokens
-hipError_t launch_low_sum(const LowArgs& a, int64_t N, hipStream_t stream);
+hipError_t launch_low_sum(const LowPair& pair, int64_t N, hipStream_t stream);
 hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t stream);
 hipError_t launch_outer(const OuterPair& pair, int x_dt, int y_dt, hipStream_t stream);
 
