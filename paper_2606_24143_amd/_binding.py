@@ -691,8 +691,7 @@ def _padded(M: int, dtype) -> int:
 
 def _rows(N: int, M: int, ld: int, dtype, dev) -> torch.Tensor:
     """[N, M], rows ld elements apart."""
-    t = torch.empty((N, ld), dtype=dtype, device=dev)
-    return t if ld == M else t[:, :M]
+    return torch.empty_strided((N, M), (ld, 1), dtype=dtype, device=dev)
 
 
 def _need_workspace(workspace, dev):
@@ -925,9 +924,9 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, *, k: Optional[int] 
         ld = _padded(V, logits.dtype)
     _need_gpu(logits, "logits")
     with _On(dev, stream) as s:
-        res = {"scores": torch.empty((B, k), dtype=torch.float32, device=dev),
-               "parents": torch.empty((B, k), dtype=torch.int32, device=dev),
-               "ids": torch.empty((B, k), dtype=torch.int32, device=dev)}
+        best = torch.empty_like(scores) if k == W else scores.new_empty((B, k))
+        res = {"scores": best, "parents": torch.empty_like(best, dtype=torch.int32),
+               "ids": torch.empty_like(best, dtype=torch.int32)}
         ws, nbytes = _workspace(workspace, int(lib().opd_beam_workspace_bytes(B, W, V, dt)), dev)
         rc = lib().opd_beam_select(_at(logits), dt, B, W, V, ld, _at(scores), _at(finished), k,
                                    _at(res["scores"]), _at(res["parents"]), _at(res["ids"]),
@@ -941,6 +940,9 @@ def _slices(t: torch.Tensor, name: str):
     """(outer, inner bytes, stride, outer stride) of the states along t's first axis:
     each `outer` slices of contiguous bytes, evenly apart."""
     size = t.element_size()
+    if t.is_contiguous() and t.numel() > 0:
+        n = t.numel() // t.shape[0]
+        return 1, n * size, n * size, n * size
     inner, axes = 1, [(n, st) for n, st in zip(t.shape[1:], t.stride()[1:]) if n != 1]
     while axes and axes[-1][1] == inner:
         inner *= axes.pop()[0]
@@ -993,12 +995,15 @@ def reorder_beams(states: torch.Tensor, parents: torch.Tensor, *, out=None, stre
     _need_gpu(states, "states")
     with _On(dev, stream) as s:
         if out is None:
-            # (rows a multiple of 16 bytes apart)
-            n = states[0].numel() if B else 0
-            pad = _blocks(max(n, 1) * states.element_size(), 16) * 16
-            buf = torch.empty((B * k, pad), dtype=torch.uint8, device=dev).view(states.dtype)
-            out = buf[:, :n].unflatten(1, shape[1:]) if len(shape) > 1 else buf[:, 0]
-            to_outer, to_inner, to_stride, to_apart = _slices(out, "out")
+            # (contiguous states, a multiple of 16 bytes apart)
+            strides, n, size = [], 1, states.element_size()
+            for m in reversed(shape[1:]):
+                strides.append(n)
+                n *= m
+            to_outer, to_inner, to_apart = 1, n * size, n * size
+            to_stride = _blocks(max(n, 1) * size, 16) * 16
+            out = torch.empty_strided(shape, (to_stride // size, *reversed(strides)),
+                                      dtype=states.dtype, device=dev)
         if to_inner != inner and B:
             # slices of both: the shorter ones
             outer, inner, apart, to_apart = _common(outer, inner, apart, to_outer, to_inner,
