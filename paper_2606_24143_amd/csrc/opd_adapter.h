@@ -449,7 +449,8 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
 #pragma unroll
       for (int h = 0; h < E / S; ++h) {
         if constexpr (READ)
-          y[i][h] = *(const u32x4*)(row + min(c0 + m * E + S * h, end) * TY::BYTES);
+          y[i][h] = __builtin_nontemporal_load(
+              (const u32x4*)(row + min(c0 + m * E + S * h, end) * TY::BYTES));
         else
           y[i][h] = u32x4{0, 0, 0, 0};
       }
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
 #pragma unroll
       for (int h = 0; h < E / S; ++h) {
         if (whole)
-          *(u32x4*)(row + 16 * h) = y[i][h];
+          __builtin_nontemporal_store(y[i][h], (u32x4*)(row + 16 * h));
         else
           store_end<TY>(row + 16 * h, y[i][h], a.D - (c0 + m * E + S * h));
       }
