@@ -469,20 +469,21 @@ size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype
  *
  * opd_embed_tokens: out[n, :] = scale * table[ids[n], :], in fp32, rounded once.
  * opd_embed_grads: dtable[v, :] = scale * sum of dy[n, :] over the tokens n with
- *   ids[n] == v, summed in fp32 in the order of the tokens (an entry of more than 64
- *   tokens: in parts of 64 places of the sorted batch, then over the parts).  Every row of
+ *   ids[n] == v, summed in fp32 in the order of the tokens (an entry of more than 16
+ *   tokens: in parts of 16 places of the sorted batch, then over the parts).  Every row of
  *   dtable is written, zeros among them; with accumulate = 1 the sums are added to what
  *   it holds, and the rows of entries without a token stay as they are, unread.
  *     table [V, ld], dtable [V, ldo], dy [N, ldy], out [N, ldo]: OPD_F32 or OPD_BF16, in
- *     any combination, 16-byte aligned rows; columns past H are not written.
+ *     any combination, 16-byte aligned rows; columns past H are not written.  Results may
+ *     not overlap the inputs.
  *     ids [N] int32.  -1 (what opd_verify_drafts writes past a sequence's last token)
  *     gives a row of zeros and has no part in the gradient; any other id outside
  *     [0, V) gives a row of NaN and has no part in the gradient.
  *     workspace: opd_embed_workspace_bytes(N, V, H) bytes (0 for few tokens: may be
  *     NULL), 16-byte aligned, of any content; calls (and captured graphs) that may
  *     overlap need one each.
- * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N, V >= 2^31, V < 1, H outside [1, 2^22], a
- * row stride below H), OPD_ERR_PARAM (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL,
+ * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N, V >= 2^31, the gradient's V > 2^31 - 512 where
+ * there is a workspace, V < 1, H outside [1, 2^22], a row stride below H), OPD_ERR_PARAM (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL,
  * OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0 looks nothing up; the gradient is then zeros.
  */
 int opd_embed_tokens(const void* table, int32_t dtype, int64_t V, int64_t H, int64_t ld,
@@ -505,7 +506,7 @@ size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
  *   da_g = s_g sum_n u_n^T x[n],  db_g = s_g sum_n t_n^T dy[n]   (over its tokens)
  *     x [N, ldx], a [G, r, lda], b [G, r, ldb]: dtype.  (Both matrices are held as r
  *     rows of the long axis.)  y, out [N, ..], dy [N, lddy]: y_dtype, which is dtype or
- *     OPD_F32.  out may be y.  dx_shared (the shared projection's gradient; nullable: 0)
+ *     OPD_F32.  out may be y; results overlap no other input.  dx_shared (the shared projection's gradient; nullable: 0)
  *     and dx (nullable: not wanted) [N, ..]: dtype; they may be one.  da [G, r, ldda],
  *     db [G, r, lddb]: OPD_F32; adapters without a token get zeros.
  *     scales [G] fp32, nullable (1).
@@ -522,8 +523,8 @@ size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
  * All rows are 16-byte aligned, and read up to the next multiple of 16 bytes; what is there
  * past their end may hold anything, and is not written.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N > 2^24, H or O outside [1, 2^22], a row stride
- * below its row's length (or one of a or b above 2^22), strides of in-place rows that differ, or a call whose launches
- * would pass 2^32 work-items), OPD_ERR_SUPPORT (G outside [1, OPD_ADAPTERS_MAX], r outside
+ * below its row's length (or one of a or b above 2^22), strides of in-place rows that
+ * differ, or a call whose launches would pass 2^32 work-items), OPD_ERR_SUPPORT (G outside [1, OPD_ADAPTERS_MAX], r outside
  * [1, OPD_RANK_MAX]), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0
  * adds nothing; the gradients are then zeros.
  */
@@ -567,7 +568,8 @@ size_t opd_adapter_workspace_bytes(int64_t N, int64_t H, int64_t O, int32_t G, i
  *   parents[b, j], for j < k; one whose parent is outside [0, W) becomes zeros.  A state is
  *   `outer` slices of inner_bytes bytes, outer_stride bytes apart; states lie `stride`
  *   bytes apart, b W + w of them before the state of beam w of group b (in out: b k + j).
- *   Any element type.  out may be states (k == W, the same strides): the states
+ *   States of out do not overlap: they lie one after the other, or their slices do (all
+ *   states' first slices, then all second ones).  Any element type.  out may be states (k == W, the same strides): the states
  *   are then moved in place, and those that are their own parent stay.  It may not
  *   overlap them otherwise.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SUPPORT (W or k outside [1, OPD_BEAM_MAX]), OPD_ERR_SHAPE,

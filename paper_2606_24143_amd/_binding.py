@@ -723,6 +723,8 @@ def embed_tokens(table: torch.Tensor, ids: torch.Tensor, *, scale: float = 1.0, 
         raise ValueError("dtype must be torch.float32 or torch.bfloat16")
     if out is not None:
         ldo = _need_out(out, "out", dtype, N, H, dev)
+        if _overlap(out, table):
+            raise ValueError("out must not overlap the table")
     _need_gpu(table, "table")
     with _On(dev, stream) as s:
         if out is None:
@@ -753,6 +755,8 @@ def embed_grads(grad: torch.Tensor, ids: torch.Tensor, V: int, *, scale: float =
         raise ValueError("dtype must be torch.float32 or torch.bfloat16")
     if out is not None:
         ldo = _need_out(out, "out", dtype, V, H, dev)
+        if _overlap(out, grad):
+            raise ValueError("out must not overlap grad")
     elif accumulate:
         raise ValueError("accumulate=True needs the gradient to add to (out)")
     _need_workspace(workspace, dev)
@@ -822,6 +826,8 @@ def add_adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Ten
         ldo = _need_out(out, "out", y.dtype, N, O, dev)
         if out is not y and _overlap(out, y) and (out.data_ptr() != y.data_ptr() or ldo != ldy):
             raise ValueError("out must be y or not overlap it")
+        if _overlap(out, b):
+            raise ValueError("out must not overlap b")
     _need_workspace(workspace, dev)
     _need_gpu(x, "x")
     dt, ydt = _dt(x), _dt(y)
@@ -953,8 +959,11 @@ def _slices(t: torch.Tensor, name: str):
             if st != outer * apart:
                 raise ValueError("%s must hold states of evenly spaced, contiguous slices" % name)
             outer *= n
-    if min([apart] + [st for st in t.stride()]) < 0 or (outer > 1 and apart < inner) or \
-            (t.shape[0] > 1 and t.stride(0) < (outer - 1) * apart + inner):
+    # (one state after the other, or all states' first slices, then all second ones)
+    n, st = t.shape[0], t.stride(0)
+    if min([apart] + [s for s in t.stride()]) < 0 or (outer > 1 and apart < inner) or \
+            (n > 1 and st < (outer - 1) * apart + inner and
+             (st < inner or apart < (n - 1) * st + inner)):
         raise ValueError("%s must hold states that do not overlap" % name)
     return outer, inner * size, t.stride(0) * size, apart * size
 
@@ -963,7 +972,8 @@ def reorder_beams(states: torch.Tensor, parents: torch.Tensor, *, out=None, stre
     """The beams' states in the order that beam_select returned: states [B * W, ...] of
     any type, parents [B, k] int32 in [0, W) (zeros for any other).  out: another tensor
     [B * k, ...], or `states` itself (k == W): moved in place.  A state may be strided (a
-    cache cut at its length) if its contiguous slices lie evenly apart.  Returns {"states"
+    cache cut at its length, or all layers' caches [L, B * W, ...].transpose(0, 1)) if its
+    contiguous slices lie evenly apart.  Returns {"states"
     [B * k, ...]}."""
     if not isinstance(states, torch.Tensor) or states.dim() < 1:
         raise ValueError("states must be a [B * W, ...] tensor")

@@ -876,6 +876,9 @@ int opd_embed_grads(const void* dy, int32_t dtype, int64_t N, int64_t H, int64_t
   if (!dtable || (N > 0 && (!dy || !ids))) return OPD_ERR_NULL;
   if (!rows_aligned(dtable, ldo, out_dtype) || (N > 0 && !rows_aligned(dy, ldy, dtype)))
     return OPD_ERR_ALIGN;
+  // (one launch sorts, a workgroup to embed_keys(V) entries)
+  if (N > kEmbedUnsorted && (V + embed_keys(V) - 1) / embed_keys(V) * 1024 > kMaxGridLanes)
+    return OPD_ERR_SHAPE;
   const EmbedLayout l = embed_layout(N, V, H);
   if (l.total > 0 && (!workspace || workspace_bytes < l.total || !aligned16(workspace)))
     return OPD_ERR_WORKSPACE;
@@ -1056,6 +1059,12 @@ int opd_reorder_beams(const void* states, int64_t B, int32_t W, int64_t outer, i
                                                       out_outer_stride < inner_bytes))))
     return OPD_ERR_SHAPE;
   if (B == 0 || outer == 0 || inner_bytes == 0) return OPD_OK;
+  // states of `out` lie one after the other, or their slices do, a slice of all states
+  // after the other
+  const __int128 n = (__int128)B * k, gap = out_outer_stride;
+  const bool whole = n == 1 || out_stride >= (outer - 1) * gap + inner_bytes;
+  const bool sliced = outer == 1 || gap >= (n - 1) * (__int128)out_stride + inner_bytes;
+  if (!whole && !(sliced && out_stride >= inner_bytes)) return OPD_ERR_SHAPE;
   if (!states || !parents || !out) return OPD_ERR_NULL;
   const bool in_place = states == out;
   if (in_place && (k != W || stride != out_stride || (outer > 1 && outer_stride != out_outer_stride)))

@@ -107,6 +107,13 @@ def test_long_axes(kind, ykind):
 
 
 @pytest.mark.parametrize("kind,ykind", KINDS)
+@pytest.mark.parametrize("N,G", [(8192, 3), (8193, 70), (20_001, 1000)])
+def test_many_tokens(kind, ykind, N, G):
+    """More than a wavefront of the sort holds at once, and as many."""
+    check(batch(8, N, 24, 40, G, 5, kind, ykind), kind, ykind)
+
+
+@pytest.mark.parametrize("kind,ykind", KINDS)
 def test_one_adapter_has_nearly_all_tokens(kind, ykind):
     s = batch(4, 520, 80, 140, 6, 12, kind, ykind)
     s["ids"].fill_(4)

@@ -234,6 +234,26 @@ def test_a_cache_cut_at_its_length(length):
     assert torch.equal(cache, want)
 
 
+@pytest.mark.parametrize("place", [False, True])
+def test_caches_of_all_layers(place):
+    L, B, W = 3, 2, 4
+    g = torch.Generator(DEV).manual_seed(8)
+    cache = torch.randn(L, B * W, 5, 24, device=DEV, generator=g)
+    parents = torch.randint(0, W, (B, W), device=DEV, generator=g, dtype=torch.int32)
+    at = (parents.long() + torch.arange(B, device=DEV)[:, None] * W).view(-1)
+    want = cache[:, at]
+    states = cache.transpose(0, 1)
+    got = opd.reorder_beams(states, parents, out=states if place else None)["states"]
+    assert torch.equal(got, want.transpose(0, 1))
+    if place:
+        assert torch.equal(cache, want)
+    # into another such buffer
+    if not place:
+        other = torch.zeros_like(cache)
+        opd.reorder_beams(states, parents, out=other.transpose(0, 1))
+        assert torch.equal(other, want)
+
+
 def test_states_at_odd_addresses():
     buf = torch.arange(4000, device=DEV, dtype=torch.int32).to(torch.uint8)
     states = buf[3:3 + 8 * 101].view(8, 101)

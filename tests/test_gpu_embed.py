@@ -115,6 +115,14 @@ def test_gradient(kind, out, N, V, H, skew):
     assert torch.equal(again["dtable"], got)
 
 
+@pytest.mark.parametrize("N,V", [(8192, 100), (8193, 2), (30_011, 1500)])
+def test_many_tokens(N, V):
+    """More than a wavefront of the sort holds at once, and as many."""
+    g = torch.Generator(DEV).manual_seed(N)
+    ids = ids_of(np.random.default_rng(N), N, V, True, bad=True)
+    check_grads(rows(g, N, 40, "bf16"), ids, V, 1.0, "f32")
+
+
 @pytest.mark.parametrize("N", [100, 3000])
 @pytest.mark.parametrize("first", [0, 1, 63, 64, 65])
 def test_entries_whose_tokens_end_at_any_place_of_a_tile(N, first):

@@ -67,6 +67,8 @@ def embed_grad(dy=FAKE, dtype=1, N=1000, H=256, ldy=None, ids=FAKE, V=500, out=F
     (dict(ws=None), WORKSPACE),
     (dict(ws=FAKE + 8), WORKSPACE),
     (dict(ws_bytes=1000), WORKSPACE),
+    (dict(V=2 ** 31 - 1), SHAPE),              # more workgroups than a launch has
+    (dict(V=2 ** 31 - 512), WORKSPACE),
 ])
 def test_embed_grad_errors(kw, code):
     assert embed_grad(**kw) == code
@@ -137,8 +139,8 @@ def test_adapter_errors(call, kw, code):
     (adapt, dict(ldo=256), SHAPE),
     (adapt, dict(ldo=516), ALIGN),
     (adapt, dict(out=FAKE, ldo=520), SHAPE),   # in place, another stride
-    # (rows too many to launch at once: 2^24 / 64 tiles of 2^22 / 256 chunks)
-    (adapt, dict(N=2 ** 24, O=2 ** 22), SHAPE),
+    # (too many to launch at once: 1,000 adapters' sums of 2^22 columns)
+    (adapt_grad, dict(G=1000, O=2 ** 22), SHAPE),
     (adapt_grad, dict(dy=None), NULL),
     (adapt_grad, dict(da=None), NULL),
     (adapt_grad, dict(db=None), NULL),
@@ -214,6 +216,11 @@ def move(states=FAKE, B=2, W=4, outer=3, inner=64, stride=256, apart=64, parents
     (dict(out=FAKE, k=3), SHAPE),             # in place, fewer states
     (dict(out=FAKE, to_stride=512), SHAPE),   # in place, another stride
     (dict(out=FAKE, to_apart=80), SHAPE),
+    (dict(to_stride=0), SHAPE),               # states of out on top of each other
+    (dict(outer=1, to_stride=48), SHAPE),
+    (dict(outer=2, to_stride=64, to_apart=64), SHAPE),
+    (dict(outer=2, to_stride=48, to_apart=1 << 20), SHAPE),
+    (dict(outer=2, to_stride=64, to_apart=1 << 20, parents=None), NULL),  # slices apart: sound
 ])
 def test_reorder_errors(kw, code):
     assert move(**kw) == code
@@ -338,6 +345,20 @@ def test_binding_refuses_adapter_grads(over, match):
     args.update(over)
     with pytest.raises(ValueError, match=match):
         opd.adapter_grads(**args)
+
+
+def test_binding_refuses_a_result_on_its_inputs():
+    table, ids = torch.zeros(6, 16), torch.zeros(4, dtype=I32)
+    with pytest.raises(ValueError, match="overlap"):
+        opd.embed_tokens(table, ids, out=table[2:])
+    with pytest.raises(ValueError, match="overlap"):
+        opd.embed_grads(table[:4], ids, 4, out=table[1:5])
+    s = adapters()
+    buf = torch.zeros(3 * 2 * 32)
+    b = buf.view(3, 2, 32)
+    with pytest.raises(ValueError, match="overlap"):
+        opd.add_adapters(torch.zeros(6, 32), s["x"], torch.zeros(3, 2, 64), b, s["adapter_ids"],
+                         out=buf.view(6, 32))
 
 
 def test_binding_refuses_an_overlap():
