@@ -44,6 +44,10 @@ __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
     return threadIdx.x & 32 ? r[0] : r[1];
   }
 }
+// Lanes of `in` below this one.
+__device__ __forceinline__ uint32_t lanes_below(uint64_t in) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
+}
 template <int S = 32>
 __device__ __forceinline__ float lanes_max(float v) {
   v = fmaxf(v, __uint_as_float(lane_xor<S>(__float_as_uint(v))));
@@ -102,24 +106,28 @@ constexpr uint32_t beam_cap(int k) {
   return (uint32_t)((k - 1) * S * (16 / TI::BYTES) + 64 * (16 / TI::BYTES) + k);
 }
 
+constexpr uint32_t kBeamVectors = 256;  // of a part that hold candidates
 struct BeamLds {
+  u32x4 vector[kBeamVectors];
+  uint32_t first[kBeamVectors];  // token of each
   uint32_t top[kBeamWaves][64];
   float max[kBeamWaves];
   double sum[kBeamWaves];
-  uint32_t n;
+  uint32_t n, vectors;
 };
 
 // One workgroup to a row's part of 256 * E * S elements, which stays in registers: its
 // maximum, its sum of exponentials, and its candidates: what is not below a bound that k
 // lanes' maxima reach, so k of them at least are among the best k, and none else can be.
-// Bound by the vector unit (some 12 instructions an element, the exponential four times as
-// long as the others).  64 groups of 8 beams, an eighth of them ended, V = 151,936 bf16: 35 us,
-// where reading takes 20; with the lanes' maxima sorted for the bound, and terms of
-// f - max with that argument's rounding put back, 43; eight waves to a SIMD spill, 43.
+// Bound by the vector unit (some 11 instructions an element, the exponential four times as
+// long as the others).  64 groups of 8 beams, an eighth of them ended, V = 151,936 bf16:
+// 30.4 us, where reading takes 20.  With elements compared out of the lanes' registers, and
+// a sum for far values beside the other one (copies of all registers), 35; with the lanes'
+// maxima sorted for the bound besides, 43; half as many vectors to a lane, 33.
 template <class TI, int S>
-__global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
+__global__ void __launch_bounds__(kBeamThreads, 6) k_beam_rows(BeamArgs a) {
   constexpr int E = 16 / TI::BYTES;
-  constexpr int kSpan = kBeamThreads * E;  // elements of a slot
+  constexpr uint32_t kSpan = kBeamThreads * E;  // elements of a slot
   __shared__ BeamLds sh;
   extern __shared__ uint64_t beam_cand[];  // beam_cap
   uint64_t* const cand = beam_cand;
@@ -130,21 +138,24 @@ __global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
   const uint32_t part = blockIdx.x % a.parts;
   const uint8_t done = a.finished ? a.finished[row] : 0;
   if (a.scores[row] == kNegInf || done) return;
-  const char* z = (const char*)a.logits + row * a.ld * TI::BYTES;
-  const int64_t v0 = (int64_t)part * (kSpan * S) + tid * E;
-  if (tid == 0) sh.n = 0;
+  // (within a part: 32 bits)
+  const int64_t part0 = (int64_t)part * (kSpan * S);
+  const char* z = (const char*)a.logits + (row * a.ld + part0) * TI::BYTES;
+  const uint32_t size = (uint32_t)min(a.V - part0, (int64_t)(kSpan * S));
+  const uint32_t v0 = tid * E;
+  if (tid == 0) sh.n = sh.vectors = 0;
   // (past the row's end: its last vector again, cut below)
-  const int64_t last = (a.V - 1) / E * E;
+  const uint32_t last = (size - 1) / E * E;
   u32x4 x[S];
 #pragma unroll
   for (int s = 0; s < S; ++s)
     x[s] = __builtin_nontemporal_load((const u32x4*)(z + min(v0 + s * kSpan, last) * TI::BYTES));
-  if ((int64_t)(part + 1) * (kSpan * S) > a.V) {
+  if (size < kSpan * S) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const bool out = v0 + s * kSpan + e >= a.V;
+        const bool out = v0 + s * kSpan + e >= size;
         if constexpr (TI::BYTES == 2) {
           const uint32_t none = e & 1 ? 0xFF800000u : 0x0000FF80u;
           const uint32_t keep = e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
@@ -161,13 +172,28 @@ __global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
     else
       return __uint_as_float(x[s][e]);
   };
-  float top[S], mine = kNegInf;  // (a NaN shows in the sum)
+  // a slot's values once more, for what is rare (registers can't be indexed)
+  auto slot_values = [&](int s, float (&f)[E]) {
+    const uint32_t v = v0 + s * kSpan;
+    const u32x4 y = *(const u32x4*)(z + min(v, last) * TI::BYTES);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if constexpr (TI::BYTES == 2)
+        f[e] = __uint_as_float(e & 1 ? y[e / 2] & 0xFFFF0000u : y[e / 2] << 16);
+      else
+        f[e] = __uint_as_float(y[e]);
+      f[e] = v + e < size ? f[e] : kNegInf;
+    }
+  };
+  // (a NaN is a lane's maximum here, which saves quieting every operand; what the row is then
+  // shows in the sum)
+  float top[S], mine = kNegInf;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     top[s] = value(s, 0);
 #pragma unroll
-    for (int e = 1; e < E; ++e) top[s] = fmaxf(top[s], value(s, e));
-    mine = fmaxf(mine, top[s]);
+    for (int e = 1; e < E; ++e) top[s] = __builtin_elementwise_maximum(top[s], value(s, e));
+    mine = __builtin_elementwise_maximum(mine, top[s]);
   }
 #pragma unroll
   for (int s = 0; s < S; ++s) keep_packed(x[s]);
@@ -211,16 +237,35 @@ __global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
 #pragma unroll
   for (int i = 1; i < kBeamWaves; ++i) m = fmaxf(m, sh.max[i]);
   float least = number(bound);
+  // Vectors with a candidate, some of a part's, to LDS: looked at element by element below
+  // by all lanes, a lane's registers would each take a comparison of the wave's.
+  uint64_t hit[S];
+  uint32_t hits = 0, to = 0;
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    hit[s] = __ballot(top[s] >= least);
+    hits += (uint32_t)__popcll(hit[s]);
+  }
+  if (lane == 0 && hits) to = atomicAdd(&sh.vectors, hits);
+  to = __builtin_amdgcn_readfirstlane(to);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    if (hit[s] == 0) continue;
+    if (hit[s] >> lane & 1) {
+      const uint32_t p = to + lanes_below(hit[s]);
+      if (p < kBeamVectors) {
+        sh.vector[p] = x[s];
+        sh.first[p] = (uint32_t)part0 + v0 + s * kSpan;
+      }
+    }
+    to += (uint32_t)__popcll(hit[s]);
+  }
 
   const float off = m == kNegInf ? 0.f : m;
   const bool far = !(fabsf(off) < kBeamNear);
   const float c = far ? 0.f : rintf(off * kLog2e);
   double sum = 0.0;
-  auto add = [&](int s, auto is_far) {
-    constexpr bool FAR = decltype(is_far)::value;
-    float t[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) t[e] = beam_term(FAR ? value(s, e) - off : value(s, e), c);
+  auto add = [&](const float (&t)[E]) {
     if constexpr (E == 8)
       sum += (double)(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
     else
@@ -228,30 +273,40 @@ __global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
   };
   if (!far) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) add(s, std::false_type());
-  } else {
+    for (int s = 0; s < S; ++s) {
+      float t[E];
 #pragma unroll
-    for (int s = 0; s < S; ++s) add(s, std::true_type());
+      for (int e = 0; e < E; ++e) t[e] = beam_term(value(s, e), c);
+      add(t);
+    }
+  } else {  // (rolled: unrolled beside the other, it costs that one copies of the registers)
+#pragma unroll 1
+    for (int s = 0; s < S; ++s) {
+      float t[E];
+      slot_values(s, t);
+#pragma unroll
+      for (int e = 0; e < E; ++e) t[e] = beam_term(t[e] - off, 0.f);
+      add(t);
+    }
   }
   sum = lanes_sum(sum);
   if (lane == 0) sh.sum[w] = sum;
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-    if (__ballot(top[s] >= least) == 0) continue;  // (half the vectors, and most elements)
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float f = value(s, e);
-      if (__ballot(f >= least) == 0) continue;
-      if (f >= least) {
-        const uint32_t at = atomicAdd(&sh.n, 1u);
-        const uint32_t v = (uint32_t)(v0 + s * kSpan + e);
-        if (at < cap) cand[at] = (uint64_t)order_key(__float_as_uint(f)) << 32 | (uint32_t)~v;
-      }
+  __syncthreads();
+  const uint32_t vectors = sh.vectors;
+  for (uint32_t i = tid; i < min(vectors, kBeamVectors) * E; i += kBeamThreads) {
+    uint32_t b;
+    if constexpr (TI::BYTES == 2)
+      b = (uint32_t)((const uint16_t*)sh.vector)[i] << 16;
+    else
+      b = ((const uint32_t*)sh.vector)[i];
+    if (__uint_as_float(b) >= least) {
+      const uint32_t at = atomicAdd(&sh.n, 1u);
+      if (at < cap) cand[at] = (uint64_t)order_key(b) << 32 | (uint32_t)~(sh.first[i / E] + i % E);
     }
   }
   __syncthreads();
   uint32_t n = sh.n;
-  if (n > cap) {
+  if (n > cap || vectors > kBeamVectors) {
     // Too many: by the bound of all lanes, those above it (in fewer than k lanes), then the
     // equal ones slot by slot, whose tokens ascend, until there are enough.
     __syncthreads();
@@ -261,18 +316,8 @@ __global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
     for (int equal = 0; equal < 2; ++equal) {
 #pragma unroll 1
       for (int s = 0; s < S; ++s) {
-        // (the slot's vector, without indexing the registers)
-        u32x4 y = x[0];
-#pragma unroll
-        for (int i = 1; i < S; ++i) y = s == i ? x[i] : y;
         float f[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          if constexpr (TI::BYTES == 2)
-            f[e] = __uint_as_float(e & 1 ? y[e / 2] & 0xFFFF0000u : y[e / 2] << 16);
-          else
-            f[e] = __uint_as_float(y[e]);
-        }
+        slot_values(s, f);
         // (lanes in turn waves: a slot's tokens ascend with the lanes)
 #pragma unroll 1
         for (int turn = 0; turn < kBeamWaves; ++turn) {
@@ -283,7 +328,7 @@ __global__ void __launch_bounds__(kBeamThreads, 4) k_beam_rows(BeamArgs a) {
             for (int e = 0; e < E; ++e) {
               if (equal ? f[e] == least : f[e] > least) {
                 const uint32_t at = atomicAdd(&sh.n, 1u);
-                const uint32_t v = (uint32_t)(v0 + s * kSpan + e);
+                const uint32_t v = (uint32_t)part0 + v0 + s * kSpan + e;
                 if (at < cap) cand[at] = (uint64_t)order_key(__float_as_uint(f[e])) << 32 | (uint32_t)~v;
               }
             }
@@ -429,7 +474,7 @@ __device__ __forceinline__ uint32_t merge_cut(MergeLds& sh, uint32_t n, int k, u
 #pragma unroll
   for (int i = 0; i < kMergeEach; ++i) {
     if (in[i] >> lane & 1) {
-      const uint32_t p = to + (uint32_t)__popcll(in[i] & ((1ull << lane) - 1));
+      const uint32_t p = to + lanes_below(in[i]);
       sh.score[p] = s[i];
       sh.at[p] = at[i];
     }
@@ -544,7 +589,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
                     score > -__builtin_huge_val());
   };
   auto put = [&](uint32_t w, uint64_t c, double score, uint64_t in, uint32_t to) {
-    to += (uint32_t)__popcll(in & ((1ull << lane) - 1));
+    to += lanes_below(in);
     if (in >> lane & 1) {
       sh.score[to] = score;
       sh.at[to] = (uint64_t)w << 32 | (uint32_t)~(uint32_t)c;
