@@ -931,7 +931,7 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
   if (!workspace || workspace_bytes < l.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
   char* ws = (char*)workspace;
   const hipStream_t st = (hipStream_t)stream;
-  const opd::AdaptArgs plan{adapter_ids, N, G, (int32_t*)ws, (int32_t*)(ws + l.start),
+  const opd::AdaptArgs plan{adapter_ids, N, G, (int32_t*)ws, nullptr,
                             (opd::AdTile*)(ws + l.tiles), l.max_tiles};
   hipError_t err = opd::launch_adapt_plan(plan, st);
   if (err != hipSuccess) return OPD_ERR_HIP;

@@ -52,7 +52,7 @@ struct AdaptArgs {
   int64_t N;
   int G;
   int32_t* perm;          // [N] tokens by adapter
-  int32_t* start;         // [G + 3] first places
+  int32_t* start;         // [G + 3] first places; nullable
   AdTile* tiles;          // [max_tiles]
   int64_t max_tiles;
 };
