@@ -62,6 +62,24 @@ __device__ __forceinline__ double lanes_sum(double v) {
   if constexpr (S > 1) v = lanes_sum<S / 2>(v);
   return v;
 }
+// A bound that k lanes' keys at least are not below: the k-th largest key, without its bits
+// below LOW.  Two bits at a time, as each waits for the count of the one before.
+template <int LOW>
+__device__ __forceinline__ uint32_t wave_kth(uint32_t key, int k) {
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 30; bit >= LOW; bit -= 2) {
+    uint32_t c[3];
+    bool reach[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      c[i] = bound | (uint32_t)(i + 1) << bit;
+      reach[i] = __popcll(__ballot(key >= c[i])) >= k;
+    }
+    bound = reach[2] ? c[2] : reach[1] ? c[1] : reach[0] ? c[0] : bound;
+  }
+  return bound;
+}
 // One step of a bitonic network: lanes keep the larger where `size` and S say so.
 template <int SIZE, int S>
 __device__ __forceinline__ uint32_t bitonic_step(uint32_t v) {
@@ -214,12 +232,7 @@ __global__ void __launch_bounds__(kBeamThreads, 6) k_beam_rows(BeamArgs a) {
     return bound <= order_key(0xFF7FFFFFu) ? -3.4028234663852886e38f : key_value(bound);
   };
   if (a.k <= 16) {
-    constexpr int LOW = TI::BYTES == 2 ? 16 : 0;  // (bf16: keys vary above)
-#pragma unroll
-    for (int bit = 31; bit >= LOW; --bit) {
-      const uint32_t c = bound | (1u << bit);
-      if (__popcll(__ballot(key >= c)) >= a.k) bound = c;
-    }
+    bound = wave_kth<TI::BYTES == 2 ? 16 : 8>(key, a.k);  // (bf16: keys vary above)
     const float m = lanes_max(mine);
     if (lane == 0) {
       sh.top[w][0] = bound;
@@ -382,7 +395,7 @@ struct MergeLds {
   uint64_t at[kMergeCap];  // beam, token
   uint32_t rank[kMergeCap];
   BeamRow row[kBeamMax];
-  uint32_t bound[2][kMergeWaves];
+  uint32_t bound[2][kMergeWaves], first[2][kMergeWaves];
   uint32_t n, bad, total;
 };
 
@@ -417,11 +430,7 @@ __device__ __forceinline__ uint32_t merge_cut(MergeLds& sh, uint32_t n, int k, u
   }
   uint32_t bound = 0;
   if (k <= 16) {
-#pragma unroll
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t c = bound | (1u << bit);
-      if (__popcll(__ballot(top >= c)) >= k) bound = c;
-    }
+    bound = wave_kth<8>(top, k);
     if (lane == 0) sh.bound[0][wave] = bound;
     if (tid == 0) sh.n = 0;
     __syncthreads();
@@ -485,8 +494,10 @@ __device__ __forceinline__ uint32_t merge_cut(MergeLds& sh, uint32_t n, int k, u
 }
 
 // One workgroup to a group: its rows' sums from their parts', the scores of the parts'
-// candidates, of which LDS keeps those that may be among the best, and the k best of
-// them, each at its rank.
+// candidates, of which LDS gets those that may be among the best, and the k best of
+// them, each at its rank.  One workgroup's latencies: the records (2 us), the rows' logarithms,
+// the scores in double precision, four barriers.  7.2 us for 128 records of 9 candidates; a
+// wave to a record, whose lanes are mostly idle, took 9.1, all candidates through LDS 9.8.
 __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
   __shared__ MergeLds sh;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -499,24 +510,31 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     sh.total = W;
   }
   __syncthreads();
-  // the records of the group, one to a wave at a time; eight on their way (the first,
-  // beside the rows' sums)
+  // The records of the group, a quarter of a wave to each (most hold fewer than 16
+  // candidates): eight to a wave at a time, their first 32 candidates on their way beside
+  // the rows' sums.
   const uint32_t recs = W * a.parts;
   const BeamRec* rec = (const BeamRec*)a.recs + b * recs;
   const uint64_t* cand = a.cands + b * recs * (int64_t)kBeamMax;
-  constexpr int AHEAD = 8;
-  uint64_t cs[AHEAD];
-  uint32_t ns[AHEAD];
+  constexpr int GROUPS = 2;
+  constexpr uint32_t BATCH = GROUPS * kMergeWaves * 4;
+  const int slot = lane & 15;
+  auto record = [&](uint32_t p0, int i) {
+    return p0 + (uint32_t)(i * kMergeWaves + wave) * 4 + (uint32_t)(lane >> 4);
+  };
+  uint64_t cs[GROUPS][2];
+  uint32_t ns[GROUPS];
   auto fetch = [&](uint32_t p0) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
+    for (int i = 0; i < GROUPS; ++i) {
       // (past a record's count, or a beam that has none, lies what the workspace held)
-      const uint32_t p = min(p0 + i * kMergeWaves, recs - 1);
-      cs[i] = cand[(int64_t)p * kBeamMax + lane];
+      const uint32_t p = min(record(p0, i), recs - 1);
       ns[i] = rec[p].n;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) cs[i][h] = cand[(int64_t)p * kBeamMax + 16 * h + slot];
     }
   };
-  fetch(wave);
+  fetch(0);
   for (int w = wave; w < W; w += kMergeWaves) {
     const int64_t row = b * W + w;
     const BeamRec* mine = rec + w * a.parts;
@@ -581,12 +599,10 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
     return;
   }
   uint32_t n = sh.n;
-  // scores of a record's candidates, those that are one
-  auto take = [&](uint32_t p, uint32_t w, uint64_t c, uint32_t count, double& score) -> uint64_t {
-    const BeamRow r = sh.row[w];
-    score = r.score + (((double)key_value((uint32_t)(c >> 32)) - (double)r.m) - r.l);
-    return __ballot(p < recs && r.kind == kBeamLive && lane < (int)count &&
-                    score > -__builtin_huge_val());
+  auto reserve = [&](uint32_t count) {
+    uint32_t to = 0;
+    if (lane == 0 && count) to = atomicAdd(&sh.n, count);
+    return (uint32_t)__builtin_amdgcn_readfirstlane(to);
   };
   auto put = [&](uint32_t w, uint64_t c, double score, uint64_t in, uint32_t to) {
     to += lanes_below(in);
@@ -595,41 +611,78 @@ __global__ void __launch_bounds__(kMergeThreads) k_beam_merge(BeamArgs a) {
       sh.at[to] = (uint64_t)w << 32 | (uint32_t)~(uint32_t)c;
     }
   };
-  auto reserve = [&](uint32_t count) {
-    uint32_t to = 0;
-    if (lane == 0) to = atomicAdd(&sh.n, count);
-    return (uint32_t)__builtin_amdgcn_readfirstlane(to);
-  };
   const bool fits = sh.total <= kMergeCap;
-  for (uint32_t p0 = 0; p0 < recs; p0 += AHEAD * kMergeWaves) {
-    if (p0 > 0) fetch(p0 + wave);
-    // (the records' beams: one division, a record to a lane)
-    const uint32_t beam = min(p0 + lane * kMergeWaves + wave, recs - 1) / a.parts;
-    uint32_t w[AHEAD];
-    double ss[AHEAD];
-    uint64_t in[AHEAD];
-    uint32_t all = 0;
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      w[i] = (uint32_t)__builtin_amdgcn_readlane((int)beam, i);
-      in[i] = take(p0 + i * kMergeWaves + wave, w[i], cs[i], ns[i], ss[i]);
-      all += (uint32_t)__popcll(in[i]);
+  // (of what may not fit: a wave's 64 at a time, 1,024 of the workgroup's)
+  auto place = [&](uint32_t w, uint64_t c, double score, uint64_t in) {
+    if (!fits && n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
+    put(w, c, score, in, reserve((uint32_t)__popcll(in)));
+    if (!fits) {
+      __syncthreads();
+      n = sh.n;
+      __syncthreads();
     }
-    uint32_t to = fits ? reserve(all) : 0;
+  };
+  uint32_t bound = 0;  // of what k candidates are not below (k <= 16: cut before they pass LDS)
+  for (uint32_t p0 = 0; p0 < recs; p0 += BATCH) {
+    if (p0 > 0) fetch(p0);
+    uint32_t w[GROUPS];
+    BeamRow row[GROUPS];
+    double ss[GROUPS][2];
+    uint64_t in[GROUPS][2];
+    auto score = [&](int i, uint64_t c) {
+      return row[i].score + (((double)key_value((uint32_t)(c >> 32)) - (double)row[i].m) - row[i].l);
+    };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const uint32_t count = (uint32_t)__popcll(in[i]);
-      if (!fits) {
-        // (each time as many as kMergeThreads at most)
-        if (n > kMergeCap - kMergeThreads) n = merge_cut(sh, n, k, kMergeCap / 2);
-        to = reserve(count);
+    for (int i = 0; i < GROUPS; ++i) {
+      const uint32_t p = record(p0, i);
+      w[i] = min(p, recs - 1) / a.parts;
+      row[i] = sh.row[w[i]];
+      if (p >= recs || row[i].kind != kBeamLive) ns[i] = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        in[i][h] = 0;
+        ss[i][h] = 0.0;
+        if (__ballot(ns[i] > 16u * h) == 0) continue;
+        ss[i][h] = score(i, cs[i][h]);
+        in[i][h] = __ballot(slot + 16u * h < ns[i] && ss[i][h] > -__builtin_huge_val());
       }
-      put(w[i], cs[i], ss[i], in[i], to);
-      to += count;
-      if (!fits) {
-        __syncthreads();
-        n = sh.n;
-        __syncthreads();
+    }
+    if (k <= 16) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) top = max(top, in[i][h] >> lane & 1 ? beam_key(ss[i][h]) : 0u);
+      }
+      top = wave_kth<8>(top, k);
+      uint32_t* const first = sh.first[p0 / BATCH & 1];
+      if (lane == 0) first[wave] = top;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kMergeWaves; ++i) bound = max(bound, first[i]);
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) in[i][h] &= __ballot(beam_key(ss[i][h]) >= bound);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!fits || in[i][h]) place(w[i], cs[i][h], ss[i][h], in[i][h]);
+      }
+    }
+    // what a record holds past 32
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+#pragma unroll 1
+      for (uint32_t h = 32; h < (uint32_t)kBeamMax; h += 16) {
+        if (fits && __ballot(ns[i] > h) == 0) break;
+        const uint64_t c = cand[(int64_t)min(record(p0, i), recs - 1) * kBeamMax + h + slot];
+        const double s = score(i, c);
+        place(w[i], c, s,
+              __ballot(slot + h < ns[i] && s > -__builtin_huge_val() && beam_key(s) >= bound));
       }
     }
   }
