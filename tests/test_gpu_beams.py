@@ -54,6 +54,22 @@ def test_sizes(kind, B, W, V, k):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [8, 16, 17, 64])
+def test_more_candidates_than_are_kept_at_once(kind, k):
+    """64 beams of many parts; one beam far ahead, and all of them near each other."""
+    g = torch.Generator(DEV).manual_seed(k)
+    B, W, V = 2, 64, 20_000
+    z = logits(g, B, W, V, kind)
+    scores = -torch.rand(B, W, device=DEV, generator=g)
+    scores[0, 50] = 60.0
+    check(z, scores, k)
+    # rows alike: equal candidates of all beams
+    z[W:] = z[W]
+    scores[1] = -0.25
+    check(z, scores, k, ties=True)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 def test_finished_and_missing_beams(kind):
     g = torch.Generator(DEV).manual_seed(1)
     B, W, V = 12, 4, 1000
