@@ -902,13 +902,13 @@ hipError_t low_t(const LowPair& p, hipStream_t st) {
 }
 
 template <class TW, class TY>
-hipError_t expand_t(ExpandArgs a, hipStream_t st) {
+hipError_t expand_t(ExpandArgs a, int64_t N, hipStream_t st) {
   const int64_t span = kExpWaves * 16 * (TW::BYTES == 2 ? 8 : 4);
   const int64_t chunks = (a.D + span - 1) / span;
-  // about four times as many workgroups as stay on the GPU at once, since tiles differ (and
-  // some have no tokens): 64 tokens of 32 adapters by 151,936 columns 37.7 us, with as many as
-  // stay 41.5, eight times 40.9; tiles of 64 tokens by 4,096 columns 36.1, 34.9, 36.1
-  int64_t per = 4096 / a.max_tiles;
+  // about as many workgroups as stay on the GPU at once; four times as many where tiles are of
+  // few tokens, since they differ then, and some have none: 64 tokens of 32 adapters by 151,936
+  // columns 37.7 us (as many 41.5, eight times 40.9), 8,192 of 8 by 4,096 36.1 (as many 34.9)
+  int64_t per = (N < 16 * a.max_tiles ? 4096 : 1024) / a.max_tiles;
   a.per = (uint32_t)(per < 1 ? 1 : per < chunks ? per : chunks);
   const dim3 grid((unsigned)(a.max_tiles * a.per));
 #define OPD_EXPAND(KL, RB)                                                                \
@@ -972,9 +972,9 @@ hipError_t launch_low_sum(const LowPair& p, int64_t N, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t st) {
-  if (w_dt == F32) return expand_t<InF32, InF32>(a, st);
-  return y_dt == BF16 ? expand_t<InBf16, InBf16>(a, st) : expand_t<InBf16, InF32>(a, st);
+hipError_t launch_expand(const ExpandArgs& a, int64_t N, int w_dt, int y_dt, hipStream_t st) {
+  if (w_dt == F32) return expand_t<InF32, InF32>(a, N, st);
+  return y_dt == BF16 ? expand_t<InBf16, InBf16>(a, N, st) : expand_t<InBf16, InF32>(a, N, st);
 }
 
 hipError_t launch_outer(const OuterPair& pair, int x_dt, int y_dt, hipStream_t st) {

@@ -943,7 +943,7 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r,
                           opd::LowRef{t.out, t.ldo, t.stride, t.splits, r}, scales, b, ldb, O, y,
                           ldy, out, ldo, low_out, 0};
-  err = opd::launch_expand(e, dtype, y_dtype, st);
+  err = opd::launch_expand(e, N, dtype, y_dtype, st);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }
 
@@ -1006,7 +1006,7 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
   if (!dx || N == 0) return OPD_OK;
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r, uref, scales, a, lda, H,
                           dx_shared, ldds, dx, lddx, nullptr, 0};
-  err = opd::launch_expand(e, dtype, dtype, st);
+  err = opd::launch_expand(e, N, dtype, dtype, st);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }
 

@@ -121,7 +121,7 @@ hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t stream);
 hipError_t launch_low(const LowPair& pair, int x_dt, int w_dt, hipStream_t stream);
 // adds the parts up in the first one's place, for N tokens
 hipError_t launch_low_sum(const LowPair& pair, int64_t N, hipStream_t stream);
-hipError_t launch_expand(const ExpandArgs& a, int w_dt, int y_dt, hipStream_t stream);
+hipError_t launch_expand(const ExpandArgs& a, int64_t N, int w_dt, int y_dt, hipStream_t stream);
 hipError_t launch_outer(const OuterPair& pair, int x_dt, int y_dt, hipStream_t stream);
 
 // Beam selection and reordering (opd_beam_select, opd_reorder_beams).
