@@ -184,9 +184,9 @@ __device__ __forceinline__ float low_value(const LowRef& t, int64_t token, int c
 // take steps of 64 (bf16) or 32 (fp32) columns in turn, the next ones on their way meanwhile,
 // and their sums are added in order.  A lane's operands lie along a row, and its
 // neighbours' in other rows: loaded so, an instruction touches 16 lines 16 bytes at a time,
-// which took 42 us for 8,192 tokens by 4,096 columns and 32 ranks where 32 are needed with
-// rows read as they lie and turned in LDS, a part of it to each wave (20 where nothing has
-// just been written: reading the tokens alone takes 17.5).  RT: ranks / 16.
+// which took 10 us more for 8,192 tokens by 4,096 columns and 32 ranks than rows read as they
+// lie and turned in LDS, a part of it to each wave: 24.5 us, 20 where nothing has just been
+// written (reading the tokens alone takes 17.5).  RT: ranks / 16.
 constexpr int kLowThreads = 512;
 constexpr int kLowWaves = kLowThreads / 64;
 
@@ -440,6 +440,9 @@ __device__ __forceinline__ void store_values(char* row, int64_t c, int64_t end, 
 // tokens' are on their way meanwhile (no load in a loop depends on a condition, since the
 // compiler waits for all where it can't count them); where there are no more than 16, of up
 // to 16 ranks, the next columns of the adapter too.
+// 8,192 tokens by 4,096 columns and 32 ranks: 34.9 us, 28 at a copy's rate.  The shared
+// projection's values and the results pass the caches: kept there, they drain while the next
+// call's k_low reads, which then takes 32.7 us instead of 24.5 (and this 33.6).
 // KL: ranks of a lane's operand (bf16: 4 or 8); RB: of 4 KL ranks each; READ: there is a base.
 template <class TW, class TY, int KL, int RB, bool READ>
 __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(ExpandArgs a) {
@@ -691,7 +694,9 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
 // rows): its waves take blocks of 32 tokens in turn (with those of the other `splits`),
 // and their sums are added in order.  A lane loads eight tokens' 16 bytes and
 // transposes them; the block's r numbers come straight into the layout of the
-// second operand.  The next block's rows are on their way meanwhile.
+// second operand.  The next block's rows are on their way meanwhile.  Both sums of 8,192 tokens
+// of 4 adapters by 4,096 columns and 16 ranks: 30.2 us, where reading takes 20; a wave has two
+// blocks there, so little of its own overlaps.
 constexpr int kOutThreads = 512;
 constexpr int kOutWaves = kOutThreads / 64;
 template <class TX, int RT>
@@ -881,6 +886,8 @@ hipError_t low_r(const LowPair& p, hipStream_t st) {
   const int64_t tiles = p.a[0].max_tiles;
   const int splits = p.a[0].splits + p.a[1].splits;
   // 32 tokens to a workgroup read the adapter half as often, where that leaves enough of them
+  // (4,096 columns, the call: 8,192 tokens of 8 adapters 45.5 us, 46.4 with 16; 2,048 of 4 23.1,
+  // 22.3 with 16)
   if constexpr (RT <= 4) {
     if (tiles * splits >= 100) {
       const dim3 grid((unsigned)(tiles * (kAdTile / 32)), (unsigned)splits);

@@ -343,18 +343,25 @@ struct EmbedLayout {
   size_t perm, partial, total;
   int64_t hp;
 };
-// Up to so many tokens are looked for by each entry's wavefront itself.
-constexpr int64_t kEmbedUnsorted = 256;
+// Few tokens are looked for by each entry's wavefronts themselves: 64, which they load at
+// once, or up to 256 where there are few wavefronts.  256 tokens: 27.7 us unsorted and 32.7
+// sorted for 32,000 by 1,000 fp32, 415 and 357 for 151,936 by 4,096; 64: 25.6 and 32.7, 360 and
+// 358.
+bool embed_unsorted(int64_t N, int64_t V, int64_t H) {
+  return N <= 64 || (N <= 256 && V * ((H + 255) / 256) <= (1 << 18));
+}
 EmbedLayout embed_layout(int64_t N, int64_t V, int64_t H) {
   EmbedLayout l{};
   l.hp = (H + 7) / 8 * 8;
-  if (N <= kEmbedUnsorted) return l;
+  if (embed_unsorted(N, V, H)) return l;
   l.perm = up256((size_t)(V + 1) * 4);
   l.partial = l.perm + up256((size_t)N * 4);
   l.total = l.partial + up256((size_t)((N + opd::kEmbTile - 1) / opd::kEmbTile) * 2 * (size_t)l.hp * 4);
   return l;
 }
-// Entries to a workgroup that sorts: about a workgroup to each CU, up to kEmbKeys entries.
+// Entries to a workgroup that sorts: about a workgroup to each CU, up to kEmbKeys entries.  The
+// gradient of 4,096 tokens of 64 columns: 16.3 us for 32,000 entries (64 to a workgroup 20.1,
+// 512 17.6), 14.6 for 2,000 (512 15.8); of 16,384 for 151,936 43.5 (64 90.7).
 int embed_keys(int64_t V) {
   int keys = 64;
   while (keys < opd::kEmbKeys && (int64_t)keys * 300 < V) keys *= 2;
@@ -380,10 +387,11 @@ struct AdaptLayout {
   int outer;                   // parts of an adapter's tokens
   size_t start, tiles, t, u, part_x, part_y, total;
 };
-// Parts of a long axis of D columns: about 1,024 workgroups of 16 tokens, each
-// with 1,024 columns at least.
+// Parts of a long axis of D columns: about 256 workgroups of 16 tokens, each
+// with 1,024 columns at least.  4,096 columns, the whole call: 1 token 7.9 us (undivided 9.1),
+// 64 of 32 adapters 11.8 (12.8); 2,048 of 4 20.0 undivided, 23.1 in four parts.
 void split_axis(int64_t groups, int64_t D, int64_t* span, int* splits) {
-  int64_t s = 1024 / groups, most = D / 1024;
+  int64_t s = 256 / groups, most = D / 1024;
   if (s > most) s = most;
   if (s < 1) s = 1;
   *span = ((D + s - 1) / s + 511) / 512 * 512;
@@ -446,15 +454,21 @@ struct BeamPlan {
   int64_t parts;
   size_t cands, total;
 };
-// Parts of up to 8 vectors of 16 bytes a lane, fewer where the rows are few: 1,024
-// workgroups.
-BeamPlan beam_plan(int64_t rows, int64_t V, int32_t dtype) {
+// Parts of 8 vectors of 16 bytes a lane; fewer where that makes fewer than 1,024 workgroups, as
+// long as a group's parts are no more than its merge takes at once.  bf16, the call on the
+// GPU: 4 rows of 32,000 10.3 us with 1 vector (8: 11.1), 4 of 151,936 11.2 with 4
+// (1: 18.0, 8: 11.6), 32 of 151,936 14.1 with 8 (1: 46.9).
+BeamPlan beam_plan(int64_t B, int32_t W, int64_t V, int32_t dtype) {
+  constexpr int64_t at_once = 128;
+  const int64_t rows = B * W;
   BeamPlan p{8, 0, 0, 0};
-  for (;; p.slots /= 2) {
-    const int64_t part = 256 * (16 / elt_bytes(dtype)) * (int64_t)p.slots;
-    p.parts = (V + part - 1) / part;
-    if (p.slots == 1 || rows * p.parts >= 1024) break;
-  }
+  const auto parts = [&](int slots) {
+    const int64_t part = 256 * (16 / elt_bytes(dtype)) * (int64_t)slots;
+    return (V + part - 1) / part;
+  };
+  while (p.slots > 1 && rows * parts(p.slots) < 1024 && W * parts(p.slots / 2) <= at_once)
+    p.slots /= 2;
+  p.parts = parts(p.slots);
   p.cands = up256((size_t)rows * (size_t)p.parts * sizeof(opd::BeamRec));
   p.total = p.cands + (size_t)rows * (size_t)p.parts * opd::kBeamMax * 8;
   return p;
@@ -878,7 +892,7 @@ int opd_embed_grads(const void* dy, int32_t dtype, int64_t N, int64_t H, int64_t
   if (!rows_aligned(dtable, ldo, out_dtype) || (N > 0 && !rows_aligned(dy, ldy, dtype)))
     return OPD_ERR_ALIGN;
   // (one launch sorts, a workgroup to embed_keys(V) entries)
-  if (N > kEmbedUnsorted && (V + embed_keys(V) - 1) / embed_keys(V) * 1024 > kMaxGridLanes)
+  if (!embed_unsorted(N, V, H) && (V + embed_keys(V) - 1) / embed_keys(V) * 1024 > kMaxGridLanes)
     return OPD_ERR_SHAPE;
   const EmbedLayout l = embed_layout(N, V, H);
   if (l.total > 0 && (!workspace || workspace_bytes < l.total || !aligned16(workspace)))
@@ -1012,7 +1026,7 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
 
 size_t opd_beam_workspace_bytes(int64_t B, int32_t W, int64_t V, int32_t dtype) {
   if (check_beams(dtype, B, W, V, V) != OPD_OK || B == 0) return 0;
-  return beam_plan(B * W, V, dtype).total;
+  return beam_plan(B, W, V, dtype).total;
 }
 
 int opd_beam_select(const void* logits, int32_t dtype, int64_t B, int32_t W, int64_t V, int64_t ld,
@@ -1024,7 +1038,7 @@ int opd_beam_select(const void* logits, int32_t dtype, int64_t B, int32_t W, int
   if (B == 0) return OPD_OK;
   if (!logits || !scores || !out_scores || !parents || !ids) return OPD_ERR_NULL;
   if (!rows_aligned(logits, ld, dtype)) return OPD_ERR_ALIGN;
-  const BeamPlan p = beam_plan(B * W, V, dtype);
+  const BeamPlan p = beam_plan(B, W, V, dtype);
   if (!workspace || workspace_bytes < p.total || !aligned16(workspace)) return OPD_ERR_WORKSPACE;
   opd::BeamArgs a{};
   a.logits = logits;

@@ -97,7 +97,8 @@ __device__ __forceinline__ void store_wide(char* row, int64_t c, int64_t H, cons
 // ---------------------------------------------------------------- lookup
 
 // One wavefront to a token and a chunk of 64 * E * VPL columns, four to a
-// workgroup.  E: elements of a lane's store (16 bytes of it).
+// workgroup.  E: elements of a lane's store (16 bytes of it).  32,768 tokens of 8 KiB, some
+// frequent: 80 us, 75 at a copy's rate; with one vector to a lane 91.
 template <class TI, class TO, int VPL>
 __global__ void __launch_bounds__(kEmbThreads) k_embed(EmbedArgs a) {
   constexpr int E = 16 / TO::BYTES;
@@ -132,7 +133,8 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed(EmbedArgs a) {
 
 // ---------------------------------------------------------------- gradient
 
-// Tokens sorted by id: start[v] the first place of entry v, perm the tokens.
+// Tokens sorted by id: start[v] the first place of entry v, perm the tokens.  16,384 tokens and
+// 151,936 entries: 19 us, two passes over all ids by each workgroup.
 __global__ void __launch_bounds__(kGroupThreads) k_embed_group(EmbedGradArgs a) {
   __shared__ GroupLds<kEmbKeys> sh;
   const int32_t lo = (int32_t)((int64_t)blockIdx.x * a.keys);
