@@ -115,6 +115,14 @@ def test_gradient(kind, out, N, V, H, skew):
     assert torch.equal(again["dtable"], got)
 
 
+@pytest.mark.parametrize("N", [64, 65, 200, 256])
+def test_few_tokens_of_a_large_table(N):
+    V = 300_000
+    g = torch.Generator(DEV).manual_seed(N)
+    ids = ids_of(np.random.default_rng(N), N, V, True, bad=True)
+    check_grads(rows(g, N, 12, "f32"), ids, V, 1.0, "bf16")
+
+
 @pytest.mark.parametrize("N,V", [(8192, 100), (8193, 2), (30_011, 1500)])
 def test_many_tokens(N, V):
     """More than a wavefront of the sort holds at once, and as many."""
