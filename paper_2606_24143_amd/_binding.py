@@ -868,9 +868,9 @@ def adapter_grads(dy: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.T
     f32 = torch.float32
     with _On(dev, stream) as s:
         ldda, lddb, lddx = _padded(H, f32), _padded(O, f32), _padded(H, x.dtype)
-        da = torch.empty((G, r, ldda), dtype=f32, device=dev)
-        db = torch.empty((G, r, lddb), dtype=f32, device=dev)
-        to = torch.empty((N, lddx), dtype=x.dtype, device=dev) if want_dx else None
+        da = torch.empty_strided((G, r, H), (r * ldda, ldda, 1), dtype=f32, device=dev)
+        db = torch.empty_strided((G, r, O), (r * lddb, lddb, 1), dtype=f32, device=dev)
+        to = _rows(N, H, lddx, x.dtype, dev) if want_dx else None
         ws, nbytes = _workspace(workspace, int(lib().opd_adapter_workspace_bytes(
             N, H, O, G, r, dt, ydt, 1)), dev)
         rc = lib().opd_adapter_grads(_at(dy), ydt, lddy, _at(x), dt, ldx, _at(a), lda, _at(b), ldb,
@@ -879,9 +879,9 @@ def adapter_grads(dy: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.T
                                      _at(ws), nbytes, s)
     if rc != 0:
         raise OpdError(rc, "opd_adapter_grads")
-    res = {"da": da[:, :, :H], "db": db[:, :, :O]}
+    res = {"da": da, "db": db}
     if want_dx:
-        res["dx"] = to[:, :H]
+        res["dx"] = to
     return res
 
 
