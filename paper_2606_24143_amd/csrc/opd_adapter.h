@@ -88,30 +88,30 @@ __global__ void __launch_bounds__(kGroupThreads) k_adapt_plan(AdaptArgs a) {
   }
 }
 
-// The same for up to 64 tokens, by one wavefront, without the first places: a step of 64
-// tokens waits 4.3 us for it, 5.5 for the workgroup above and its barriers.
-__global__ void __launch_bounds__(64) k_adapt_plan_few(AdaptArgs a) {
-  const int lane = threadIdx.x, N = (int)a.N;
-  const int32_t id = a.ids[min(lane, N - 1)];
-  const int32_t key = id == -1 ? a.G : (uint32_t)id < (uint32_t)a.G ? id : a.G + 1;
+// The same for up to kAdFew tokens, by a wavefront of each workgroup that needs them: perm
+// [kAdFew] and tiles [kAdFew] (one to a key) in LDS; the number of tiles.  64 tokens of 32
+// adapters by 4,096 columns, the call on the GPU: 9.5 us, 12.8 with a launch before for the tiles.
+__device__ __forceinline__ int plan_few(const int32_t* ids, int N, int32_t G, int32_t* perm,
+                                        AdTile* tiles) {
+  const int lane = threadIdx.x & 63;
+  const int32_t id = ids[min(lane, N - 1)];
+  const int32_t key = id == -1 ? G : (uint32_t)id < (uint32_t)G ? id : G + 1;
   const uint64_t in = N == 64 ? ~0ull : (1ull << N) - 1;
-  const uint64_t same = lanes_of_key(in, key, 32 - __clz(a.G + 1)) & in;
-  const int count = __popcll(same);
-  const bool first = lane < N && lane == __ffsll((long long)same) - 1;
-  // places, and tiles (one to a key), of smaller keys
-  uint64_t keys = __ballot(first);
-  const int tiles = __popcll(keys);
-  int place = 0, tile = 0;
-  while (keys) {
-    const int l = __ffsll((long long)keys) - 1;
-    keys &= keys - 1;
-    const bool smaller = __builtin_amdgcn_readlane(key, l) < key;
-    place += smaller ? __builtin_amdgcn_readlane(count, l) : 0;
-    tile += smaller ? 1 : 0;
+  // lanes of smaller keys, and of this one, by the keys' bits
+  uint64_t less = 0, same = in;
+  for (int bit = 31 - __clz(G + 1); bit >= 0; --bit) {
+    const int32_t mine = -(key >> bit & 1);  // (all bits, or none)
+    const uint64_t b = __ballot(mine != 0);
+    less |= same & ~b & (uint64_t)(int64_t)mine;
+    same &= ~(b ^ (uint64_t)(int64_t)mine);
   }
-  if (lane < N) a.perm[place + __popcll(same & ((1ull << lane) - 1))] = lane;
-  if (first) a.tiles[tile] = AdTile{key, place, count, 0};
-  for (int i = tiles + lane; i < (int)a.max_tiles; i += 64) a.tiles[i] = AdTile{0, 0, 0, 0};
+  const int count = __popcll(same), place = __popcll(less);
+  const bool first = lane < N && lane == __ffsll((long long)same) - 1;
+  const uint64_t firsts = __ballot(first);
+  const int all = __popcll(firsts), tile = __popcll(less & firsts);
+  if (lane < N) perm[place + __popcll(same & ((1ull << lane) - 1))] = lane;
+  if (first) tiles[tile] = AdTile{key, place, count, 0};
+  return all;
 }
 
 // ---------------------------------------------------------------- loads
@@ -222,20 +222,45 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
   constexpr int AHEAD = RT <= 2 ? 3 : RT <= 4 ? 2 : 1;  // steps on their way
   constexpr int EACH = (XV + WV) * 4 > SUM ? (XV + WV) * 4 : (SUM + 3) / 4 * 4;
   __shared__ __align__(16) float lds[kLowWaves][EACH];
+  __shared__ int32_t tokens[16 * MT];
   constexpr int SUBS = kAdTile / (16 * MT);
   const int sub = blockIdx.x % SUBS * (16 * MT);
-  const AdTile tile = a.tiles[blockIdx.x / SUBS];
-  if (sub >= tile.count || tile.key >= a.G) return;
+  AdTile tile;
+  if (a.ids) {
+    __shared__ struct {
+      int32_t perm[kAdFew];
+      AdTile tiles[kAdFew];
+      int all;
+    } few;
+    if (threadIdx.x < 64) few.all = plan_few(a.ids, a.N, a.G, few.perm, few.tiles);
+    __syncthreads();
+    if (blockIdx.x == 0 && blockIdx.y == 0) {  // for the second product
+      if ((int)threadIdx.x < a.N) a.perm[threadIdx.x] = few.perm[threadIdx.x];
+      if ((int)threadIdx.x < (int)a.max_tiles)
+        a.tiles[threadIdx.x] =
+            (int)threadIdx.x < few.all ? few.tiles[threadIdx.x] : AdTile{0, 0, 0, 0};
+    }
+    if ((int)(blockIdx.x / SUBS) >= few.all) return;
+    tile = few.tiles[blockIdx.x / SUBS];
+    if (sub >= tile.count || tile.key >= a.G) return;
+    if (threadIdx.x < 16 * MT)
+      tokens[threadIdx.x] = few.perm[tile.pos + min(sub + (int)threadIdx.x, tile.count - 1)];
+  } else {
+    tile = a.tiles[blockIdx.x / SUBS];
+    if (sub >= tile.count || tile.key >= a.G) return;
+    if (threadIdx.x < 16 * MT)
+      tokens[threadIdx.x] = a.perm[tile.pos + min(sub + (int)threadIdx.x, tile.count - 1)];
+  }
+  __syncthreads();
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int count = min(16 * MT, tile.count - sub);
-  const int32_t* perm = a.perm + tile.pos + sub;
   u32x4* const lx = (u32x4*)lds[wave];
   u32x4* const lw = lx + XV;
   const char* x[SX::N];
 #pragma unroll
   for (int i = 0; i < SX::N; ++i)
-    x[i] = (const char*)a.x + (int64_t)perm[min(SX::row(i), count - 1)] * a.ldx * TX::BYTES +
+    x[i] = (const char*)a.x + (int64_t)tokens[SX::row(i)] * a.ldx * TX::BYTES +
            SX::piece() * 16;
   const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES + SW::piece() * 16;
   const uint32_t ldw = (uint32_t)a.ldw * TW::BYTES;
@@ -382,7 +407,7 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
     float f = sums(0, n, c);
 #pragma unroll
     for (int v = 1; v < kLowWaves; ++v) f += sums(v, n, c);
-    out[(int64_t)perm[n] * a.ldo + c] = f;
+    out[(int64_t)tokens[n] * a.ldo + c] = f;
   }
 }
 
@@ -959,10 +984,7 @@ hipError_t outer_t(OuterPair p, int count, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_adapt_plan(const AdaptArgs& a, hipStream_t st) {
-  if (!a.start && a.N <= 64)
-    hipLaunchKernelGGL(k_adapt_plan_few, dim3(1), dim3(64), 0, st, a);
-  else
-    hipLaunchKernelGGL(k_adapt_plan, dim3(1), dim3(kGroupThreads), 0, st, a);
+  hipLaunchKernelGGL(k_adapt_plan, dim3(1), dim3(kGroupThreads), 0, st, a);
   return hipGetLastError();
 }
 

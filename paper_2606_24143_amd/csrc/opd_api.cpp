@@ -948,10 +948,13 @@ int opd_add_adapters(const void* y, int32_t y_dtype, int64_t ldy, const void* x,
   const hipStream_t st = (hipStream_t)stream;
   const opd::AdaptArgs plan{adapter_ids, N, G, (int32_t*)ws, nullptr,
                             (opd::AdTile*)(ws + l.tiles), l.max_tiles};
-  hipError_t err = opd::launch_adapt_plan(plan, st);
+  // (few tokens are grouped by the first product itself: a launch less)
+  const bool few = N <= opd::kAdFew;
+  hipError_t err = few ? hipSuccess : opd::launch_adapt_plan(plan, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
-                       l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
+                       l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt,
+                       few ? adapter_ids : nullptr, (int)N};
   err = opd::launch_low(opd::LowPair{{t, {}}}, dtype, dtype, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::ExpandArgs e{plan.tiles, plan.perm, l.max_tiles, G, r,
@@ -991,9 +994,9 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
   hipError_t err = opd::launch_adapt_plan(plan, st);
   if (err != hipSuccess) return OPD_ERR_HIP;
   const opd::LowArgs t{plan.tiles, plan.perm, l.max_tiles, G, r, x, a, ldx, lda, H,
-                       l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt};
+                       l.splits_x, l.span_x, N * l.ldt, (float*)(ws + l.t), l.ldt, nullptr, 0};
   const opd::LowArgs u{plan.tiles, plan.perm, l.max_tiles, G, r, dy, b, lddy, ldb, O,
-                       l.splits_y, l.span_y, N * l.ldt, (float*)(ws + l.u), l.ldt};
+                       l.splits_y, l.span_y, N * l.ldt, (float*)(ws + l.u), l.ldt, nullptr, 0};
   const opd::LowRef uref{u.out, u.ldo, u.stride, 1, r};
   const opd::LowRef tref = low ? opd::LowRef{low, r, 0, 1, r} : opd::LowRef{t.out, t.ldo, t.stride, 1, r};
   if (N > 0) {

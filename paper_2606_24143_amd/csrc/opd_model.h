@@ -44,6 +44,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs& a, int in_dt, int out_dt, hipS
 
 // Low-rank adapters (opd_add_adapters, opd_adapter_grads).
 constexpr int kAdTile = 64;  // tokens of one adapter in a tile, at most
+constexpr int kAdFew = 64;  // tokens that the first product groups itself
 struct AdTile {
   int32_t key, pos, count, unused;  // adapter (G: none, G + 1: bad id), place of its first token
 };
@@ -58,8 +59,8 @@ struct AdaptArgs {
 };
 // tokens times the rows of an adapter: out[n, 0 .. r)
 struct LowArgs {
-  const AdTile* tiles;
-  const int32_t* perm;
+  AdTile* tiles;
+  int32_t* perm;
   int64_t max_tiles;
   int G, r;
   const void* x;          // [N, ldx]
@@ -69,6 +70,8 @@ struct LowArgs {
   int64_t span, stride;
   float* out;             // [splits][N, ldo]
   int64_t ldo;
+  const int32_t* ids;     // [N] nullable: the tiles are made here, from kAdFew tokens at most
+  int N;
 };
 struct LowPair {
   LowArgs a[2];           // of one plan; the second with no splits: there is none
