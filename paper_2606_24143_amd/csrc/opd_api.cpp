@@ -1087,13 +1087,9 @@ int opd_reorder_beams(const void* states, int64_t B, int32_t W, int64_t outer, i
   const bool in_place = states == out;
   if (in_place && (k != W || stride != out_stride || (outer > 1 && outer_stride != out_outer_stride)))
     return OPD_ERR_SHAPE;
-  uint64_t all = (uint64_t)(uintptr_t)states | (uint64_t)(uintptr_t)out | (uint64_t)stride |
-                 (uint64_t)out_stride;
-  if (outer > 1) all |= (uint64_t)outer_stride | (uint64_t)out_outer_stride;
-  const int unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
   const opd::ReorderArgs a{states, B, W, k, outer, inner_bytes, stride, outer_stride, parents, out,
                            out_stride, out_outer_stride, in_place ? 1 : 0, 0, 0, 0};
-  const hipError_t err = opd::launch_reorder(a, unit, (hipStream_t)stream);
+  const hipError_t err = opd::launch_reorder(a, (hipStream_t)stream);
   return err == hipSuccess ? OPD_OK : OPD_ERR_HIP;
 }
 

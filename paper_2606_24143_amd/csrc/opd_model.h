@@ -163,6 +163,6 @@ struct ReorderArgs {
 };
 hipError_t launch_beam(const BeamArgs& a, int in_dt, hipStream_t stream);
 // unit: 16, 4 or 1 bytes, which divide every address and stride
-hipError_t launch_reorder(const ReorderArgs& a, int unit, hipStream_t stream);
+hipError_t launch_reorder(const ReorderArgs& a, hipStream_t stream);
 
 }  // namespace opd

@@ -283,6 +283,27 @@ def test_states_at_odd_addresses():
     assert torch.equal(buf[:3], before) and torch.equal(buf[811:], after)
 
 
+@pytest.mark.parametrize("k", [3, 20])
+@pytest.mark.parametrize("inner", list(range(1, 36)) + [255, 4095, 4097, 4111])
+def test_states_of_any_length(inner, k):
+    """Bytes of a state that are no multiple of what a lane moves, to another buffer and in
+    place, with guards around each."""
+    rng = np.random.default_rng(inner)
+    raw = torch.from_numpy(rng.integers(0, 256, (2 * k, inner + 5))).to(torch.uint8).to(DEV)
+    parents = torch.from_numpy(rng.integers(-1, k, (2, k)).astype(np.int32)).to(DEV)
+    want = ref.reorder(raw[:, 2:2 + inner].cpu().numpy(), parents.cpu().numpy(), k)
+    to = torch.full_like(raw, 9)
+    opd.reorder_beams(raw[:, 2:2 + inner], parents, out=to[:, 2:2 + inner])
+    assert np.array_equal(to[:, 2:2 + inner].cpu().numpy(), want)
+    assert (to[:, :2] == 9).all() and (to[:, 2 + inner:] == 9).all()
+    before = raw.clone()
+    states = raw[:, 2:2 + inner]
+    opd.reorder_beams(states, parents, out=states)
+    assert np.array_equal(states.cpu().numpy(), want)
+    assert torch.equal(raw[:, :2], before[:, :2]) and torch.equal(raw[:, 2 + inner:],
+                                                                  before[:, 2 + inner:])
+
+
 def test_states_past_four_gib():
     W, n = 4, 1_300_000_000
     states = torch.zeros(W, n, dtype=torch.uint8, device=DEV)
