@@ -469,10 +469,10 @@ size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype
  *
  * opd_embed_tokens: out[n, :] = scale * table[ids[n], :], in fp32, rounded once.
  * opd_embed_grads: dtable[v, :] = scale * sum of dy[n, :] over the tokens n with
- *   ids[n] == v, summed in fp32 in the order of the tokens (an entry of more than 16
- *   tokens: in parts of 16 places of the sorted batch, then over the parts).  Every row of
- *   dtable is written, zeros among them; with accumulate = 1 the sums are added to what
- *   it holds, and the rows of entries without a token stay as they are, unread.
+ *   ids[n] == v, summed in fp32 in the order of the tokens (where there is a workspace, an
+ *   entry of more than 16 tokens in parts of 16 places of the sorted batch, then over the
+ *   parts).  Every row of dtable is written, zeros among them; with accumulate = 1 the sums are
+ *   added to what it holds, and the rows of entries without a token stay as they are, unread.
  *     table [V, ld], dtable [V, ldo], dy [N, ldy], out [N, ldo]: OPD_F32 or OPD_BF16, in
  *     any combination, 16-byte aligned rows; columns past H are not written.  Results may
  *     not overlap the inputs.
@@ -483,8 +483,8 @@ size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype
  *     NULL), 16-byte aligned, of any content; calls (and captured graphs) that may
  *     overlap need one each.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N, V >= 2^31, the gradient's V > 2^31 - 512 where
- * there is a workspace, V < 1, H outside [1, 2^22], a row stride below H), OPD_ERR_PARAM (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL,
- * OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0 looks nothing up; the gradient is then zeros.
+ * there is a workspace, V < 1, H outside [1, 2^22], a row stride below H), OPD_ERR_PARAM
+ * (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0 looks nothing up; the gradient is then zeros.
  */
 int opd_embed_tokens(const void* table, int32_t dtype, int64_t V, int64_t H, int64_t ld,
                      const int32_t* ids, int64_t N, float scale, void* out, int32_t out_dtype,
@@ -506,9 +506,10 @@ size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
  *   da_g = s_g sum_n u_n^T x[n],  db_g = s_g sum_n t_n^T dy[n]   (over its tokens)
  *     x [N, ldx], a [G, r, lda], b [G, r, ldb]: dtype.  (Both matrices are held as r
  *     rows of the long axis.)  y, out [N, ..], dy [N, lddy]: y_dtype, which is dtype or
- *     OPD_F32.  out may be y; results overlap no other input.  dx_shared (the shared projection's gradient; nullable: 0)
- *     and dx (nullable: not wanted) [N, ..]: dtype; they may be one.  da [G, r, ldda],
- *     db [G, r, lddb]: OPD_F32; adapters without a token get zeros.
+ *     OPD_F32.  out may be y; results overlap no other input.  dx_shared (the shared
+ *     projection's gradient; nullable: 0) and dx (nullable: not wanted) [N, ..]: dtype; they
+ *     may be one.  da [G, r, ldda], db [G, r, lddb]: OPD_F32; adapters without a token get
+ *     zeros.
  *     scales [G] fp32, nullable (1).
  *     adapter_ids [N] int32: -1 for a token without an adapter (out is y, dx is dx_shared);
  *     any other id outside [0, G) gives a row of NaN in out and dx, and no part in da and db.

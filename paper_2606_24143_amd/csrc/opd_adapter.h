@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
   };
   // (No load depends on a condition, since the compiler waits for all where it can't count
   // them: pieces past the end are the last one again, ranks past r the last rank.)
-  const int64_t ex = d1 - SX::piece() * (16 / TX::BYTES) - 1, ew = d1 - SW::piece() * (16 / TW::BYTES) - 1;
+  const int64_t ex = d1 - SX::piece() * (16 / TX::BYTES) - 1;
+  const int64_t ew = d1 - SW::piece() * (16 / TW::BYTES) - 1;
   uint32_t row[SW::N];
 #pragma unroll
   for (int i = 0; i < SW::N; ++i) row[i] = (uint32_t)min(SW::row(i), a.r - 1) * ldw;

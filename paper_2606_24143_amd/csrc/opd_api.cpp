@@ -998,7 +998,8 @@ int opd_adapter_grads(const void* dy, int32_t y_dtype, int64_t lddy, const void*
   const opd::LowArgs u{plan.tiles, plan.perm, l.max_tiles, G, r, dy, b, lddy, ldb, O,
                        l.splits_y, l.span_y, N * l.ldt, (float*)(ws + l.u), l.ldt, nullptr, 0};
   const opd::LowRef uref{u.out, u.ldo, u.stride, 1, r};
-  const opd::LowRef tref = low ? opd::LowRef{low, r, 0, 1, r} : opd::LowRef{t.out, t.ldo, t.stride, 1, r};
+  const opd::LowRef tref =
+      low ? opd::LowRef{low, r, 0, 1, r} : opd::LowRef{t.out, t.ldo, t.stride, 1, r};
   if (N > 0) {
     // (both products in one launch where their operands are of the same types)
     opd::LowPair first{{u, {}}}, then{{t, {}}};

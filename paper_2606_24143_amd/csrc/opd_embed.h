@@ -143,7 +143,8 @@ __global__ void __launch_bounds__(kGroupThreads) k_embed_group(EmbedGradArgs a) 
   const int64_t V = a.V;
   uint32_t end;
   const uint32_t first = group_tokens<kEmbKeys, true>(
-      a.N, lo, count, [=](int64_t n) { return (uint32_t)ids[n] < (uint32_t)V ? ids[n] : -1; }, a.perm, sh, end);
+      a.N, lo, count, [=](int64_t n) { return (uint32_t)ids[n] < (uint32_t)V ? ids[n] : -1; },
+      a.perm, sh, end);
   if ((int)threadIdx.x < count) a.start[lo + (int)threadIdx.x] = (int32_t)first;
   if (threadIdx.x == 0 && lo + count == a.V) a.start[a.V] = (int32_t)end;
 }
