@@ -16,7 +16,7 @@ HEADERS = [os.path.join(CSRC, "opd_internal.h"), os.path.join(CSRC, "opd_device.
            os.path.join(CSRC, "opd_head.h"), os.path.join(CSRC, "opd_verify.h"),
            os.path.join(CSRC, "opd_embed.h"), os.path.join(CSRC, "opd_adapter.h"),
            os.path.join(CSRC, "opd_beam.h"), os.path.join(CSRC, "opd_group.h"),
-           os.path.join(CSRC, "opd_model.h"),
+           os.path.join(CSRC, "opd_model.h"), os.path.join(CSRC, "opd_piece.h"),
            os.path.join(ROOT, "include", "opd.h")]
 
 # -packed-fp32-ops: no v_pk_* fp32 arithmetic in device code.

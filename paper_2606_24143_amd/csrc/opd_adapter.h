@@ -19,6 +19,7 @@
 #include "opd_device.h"
 #include "opd_group.h"
 #include "opd_model.h"
+#include "opd_piece.h"
 
 namespace opd {
 namespace {
@@ -260,9 +261,8 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
   const char* x[SX::N];
 #pragma unroll
   for (int i = 0; i < SX::N; ++i)
-    x[i] = (const char*)a.x + (int64_t)tokens[SX::row(i)] * a.ldx * TX::BYTES +
-           SX::piece() * 16;
-  const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES + SW::piece() * 16;
+    x[i] = (const char*)a.x + (int64_t)tokens[SX::row(i)] * a.ldx * TX::BYTES;
+  const char* w = (const char*)a.w + (int64_t)tile.key * a.r * a.ldw * TW::BYTES;
   const uint32_t ldw = (uint32_t)a.ldw * TW::BYTES;
   f32x4 acc[MT][RT];
 #pragma unroll
@@ -278,17 +278,12 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
   };
   // (No load depends on a condition, since the compiler waits for all where it can't count
   // them: pieces past the end are the last one again, ranks past r the last rank.)
-  const int64_t ex = d1 - SX::piece() * (16 / TX::BYTES) - 1;
-  const int64_t ew = d1 - SW::piece() * (16 / TW::BYTES) - 1;
   uint32_t row[SW::N];
 #pragma unroll
   for (int i = 0; i < SW::N; ++i) row[i] = (uint32_t)min(SW::row(i), a.r - 1) * ldw;
   auto load = [&](Step& s, int64_t d) {
-    // (whole pieces from d on: the last that begins before the end, or the row's first)
-    int64_t dx = min(d, ex / (16 / TX::BYTES) * (16 / TX::BYTES));
-    int64_t dw = min(d, ew / (16 / TW::BYTES) * (16 / TW::BYTES));
-    dx = (dx < 0 ? -(int64_t)SX::piece() * (16 / TX::BYTES) : dx) * TX::BYTES;
-    dw = (dw < 0 ? -(int64_t)SW::piece() * (16 / TW::BYTES) : dw) * TW::BYTES;
+    const int64_t dx = piece_column<16 / TX::BYTES>(d, SX::piece(), d1) * TX::BYTES;
+    const int64_t dw = piece_column<16 / TW::BYTES>(d, SW::piece(), d1) * TW::BYTES;
 #pragma unroll
     for (int i = 0; i < SX::N; ++i) s.x.v[i] = *(const u32x4*)(x[i] + dx);
 #pragma unroll
