@@ -518,8 +518,7 @@ size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
  *     workspace: opd_adapter_workspace_bytes(...) bytes, 16-byte aligned, of any
  *     content; calls (and captured graphs) that may overlap need one each.
  * Sums are fp32, each result is rounded once.  bf16 operands are multiplied exactly; t
- * and u enter the second product to 2^-17 of themselves where its result is bf16, to
- * 2^-25 where it is fp32.  A NaN or an infinity in a token's x (dy) or in its adapter reaches
+ * and u enter the second product to 2^-25 of themselves.  A NaN or an infinity in a token's x (dy) or in its adapter reaches
  * its own row, and its adapter's da and db; no other's.
  * All rows are 16-byte aligned, and read up to the next multiple of 16 bytes; what is there
  * past their end may hold anything, and is not written.

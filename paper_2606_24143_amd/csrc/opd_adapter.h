@@ -11,8 +11,8 @@
 // none needs LDS for them: the sum's index may run in any order, and where
 // a product needs a lane's eight values to lie along tokens or ranks instead, the lane
 // loads an 8 by 8 block and transposes it in its registers.
-// Sums are fp32; t and u pass to the second product as two bf16 parts for bf16 results
-// (2^-17 of them), three for fp32 ones (2^-25).  fp32 operands take the fp32
+// Sums are fp32; beside bf16 operands t and u pass to the second product as three bf16 parts
+// (2^-25 of them, as good as fp32, also where results cancel).  fp32 operands take the fp32
 // matrix instructions, exact products throughout.
 #pragma once
 
@@ -154,12 +154,12 @@ __device__ __forceinline__ f32x4 mma_f32(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// A number as TERMS bf16 parts that add up to it (to 2^-9, 2^-17, 2^-25 of it); one that
-// is not finite in bf16 is its first part.
-template <int TERMS>
-__device__ __forceinline__ void split_bf16(float f, uint16_t (&p)[TERMS]) {
+// A number as bf16 parts that add up to it (one to 2^-9, two to 2^-17, three to 2^-25 of it); one
+// that is not finite in bf16 is its first part.
+constexpr int kAdTerms = 3;
+__device__ __forceinline__ void split_bf16(float f, uint16_t (&p)[kAdTerms]) {
 #pragma unroll
-  for (int i = 0; i < TERMS; ++i) {
+  for (int i = 0; i < kAdTerms; ++i) {
     const __bf16 h = (__bf16)f;
     p[i] = __builtin_bit_cast(uint16_t, h);
     const float r = f - (float)h;
@@ -463,14 +463,15 @@ __device__ __forceinline__ void store_values(char* row, int64_t c, int64_t end, 
 // to 16 ranks, the next columns of the adapter too.
 // 8,192 tokens by 4,096 columns and 32 ranks: 34.9 us, 28 at a copy's rate.  The shared
 // projection's values and the results pass the caches: kept there, they drain while the next
-// call's k_low reads, which then takes 32.7 us instead of 24.5 (and this 33.6).
+// call's k_low reads, which then takes 32.7 us instead of 24.5 (and this 33.6).  Two parts of t
+// instead of three would save 0.3 us of it, 2 of 90 with 64 ranks, 10 of 141 with 128.
 // KL: ranks of a lane's operand (bf16: 4 or 8); RB: of 4 KL ranks each; READ: there is a base.
 template <class TW, class TY, int KL, int RB, bool READ>
 __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(ExpandArgs a) {
   constexpr bool BF = TW::BYTES == 2;
   constexpr int E = BF ? 8 : 4;          // columns of a lane
   constexpr int S = 16 / TY::BYTES;      // of a vector of the result
-  constexpr int TERMS = TY::BYTES == 2 ? 2 : 3;
+  constexpr int TERMS = kAdTerms;
   constexpr int K = 4 * KL * RB;         // ranks
   constexpr int KP = BF ? K + 8 : K + 4; // (padded: lanes of a read spread over the banks)
   constexpr int WV = KL * RB;            // 16-byte vectors of the adapter to a lane
@@ -648,7 +649,7 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
     }
     if constexpr (BF) {
       uint16_t p[TERMS];
-      split_bf16<TERMS>(f, p);
+      split_bf16(f, p);
 #pragma unroll
       for (int t = 0; t < TERMS; ++t) part[t][n][k] = p[t];
     } else {
@@ -727,7 +728,7 @@ __global__ void __launch_bounds__(kOutThreads, RT == 1 ? 4 : 2) k_outer(OuterPai
   const uint32_t block = blockIdx.x - (second ? pair.blocks : 0u);
   constexpr bool BF = TX::BYTES == 2;
   constexpr int E = BF ? 8 : 4;
-  constexpr int TERMS = 3;
+  constexpr int TERMS = kAdTerms;
   constexpr int C = 16 * E;
   __shared__ float sums[kOutWaves][16][C + 4];
   const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
@@ -784,8 +785,8 @@ __global__ void __launch_bounds__(kOutThreads, RT == 1 ? 4 : 2) k_outer(OuterPai
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
           uint16_t lo[TERMS], hi[TERMS];
-          split_bf16<TERMS>(scale * low[t][i], lo);
-          split_bf16<TERMS>(scale * low[t][i + 1], hi);
+          split_bf16(scale * low[t][i], lo);
+          split_bf16(scale * low[t][i + 1], hi);
 #pragma unroll
           for (int k = 0; k < TERMS; ++k) p[t][k][i / 2] = lo[k] | (uint32_t)hi[k] << 16;
         }

@@ -215,3 +215,22 @@ def test_gradients_are_differences_of_the_forward(which):
         step = float(up[at].double() - down[at].double())
         # (sums of 40, then of 6: each addition off by a unit)
         assert abs((loss(up) - loss(down)) / step - float(d[at])) <= 64 * ref.ULP * size / abs(step)
+
+
+@pytest.mark.parametrize("kind,ykind", KINDS)
+@pytest.mark.parametrize("N", [1, 70])
+def test_results_that_cancel_keep_their_bits(kind, ykind, N):
+    """t (and u) = (1 + 2^-12 + 2^-20, -2^-12), which meet a -1: 2^-20 is left.  Exact, since
+    every partial sum in any order is a multiple of 2^-20 below 2: 21 bits of the 24 of fp32."""
+    put = lambda t, rows: aligned(torch.tensor(rows, dtype=DT[t], device=DEV))
+    long = [1.0, 2.0 ** -12, 2.0 ** -20] + [0.0] * 13
+    pick = [[[1.0] * 3 + [0.0] * 13, [0.0, -1.0] + [0.0] * 14]]
+    ones = [[[1.0] * 40] * 2]
+    ids = torch.zeros(N, dtype=torch.int32, device=DEV)
+    y = put(ykind, [[-1.0] * 40] * N)
+    out = opd.add_adapters(y, put(kind, [long] * N), put(kind, pick), put(kind, ones), ids)["out"]
+    assert (out.double() == 2.0 ** -20).all()
+    # the gradient of x, where the shared projection's is -1
+    dx = opd.adapter_grads(put(ykind, [long] * N), put(kind, [[0.0] * 40] * N), put(kind, ones),
+                           put(kind, pick), ids, dx=put(kind, [[-1.0] * 40] * N))["dx"]
+    assert (dx.double() == 2.0 ** -20).all()
