@@ -364,9 +364,19 @@ __global__ void __launch_bounds__(kLowThreads, 2) k_low(LowPair pair) {
     return d;
   };
   Step s[AHEAD];
+  // (Lanes read what others wrote, and write over what others read.  A wave's LDS accesses are
+  // done in order; this keeps the compiler to that order.  No wait comes of it, and loads from
+  // memory pass.)
+  auto ordered = []() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  };
   auto use = [&](Step& s) {
+    ordered();
     s.x.put(lx);
     s.w.put(lw);
+    ordered();
   };
 #pragma unroll
   for (int j = 0; j < AHEAD; ++j) load(s[j], column(to));
