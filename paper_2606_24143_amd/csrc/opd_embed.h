@@ -331,8 +331,11 @@ __global__ void __launch_bounds__(kEmbThreads) k_embed_few(EmbedGradArgs a) {
       add_rows<TI, 1, 1>(a, (int32_t)(n + l), 1, c, f);
     }
   }
-  if (a.accumulate && !any) return;
-  if (c < a.H) store_sum<TO, 4>(a, v, c, f[0]);
+  if (c >= a.H) return;
+  if (any)
+    store_sum<TO, 4>(a, v, c, f[0]);
+  else if (!a.accumulate)  // (zeros, whatever the scale)
+    store_wide<TO, 4, true>((char*)a.out + v * a.ldo * TO::BYTES, c, a.H, f[0]);
 }
 
 // Launches over rows (tokens, tiles, entries) in units of a row's chunk.

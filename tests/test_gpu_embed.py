@@ -204,3 +204,13 @@ def test_infinities_and_nan_stay_in_their_entries():
     assert d[7, 3].isnan() and d[13, 5] == float("inf")
     d[7, 3] = d[13, 5] = 10.0
     assert (d[:40] == 10).all() and (d[40:] == 0).all()
+
+
+@pytest.mark.parametrize("N", [5, 400])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), -2.0])
+def test_entries_without_a_token_are_zeros_whatever_the_scale(N, scale):
+    ids = torch.arange(N, dtype=torch.int32, device=DEV) % 5
+    d = opd.embed_grads(torch.ones(N, 24, device=DEV), ids, 20, scale=scale)["dtable"]
+    assert (d[5:] == 0).all() and not d[5:].signbit().any()
+    want = torch.full_like(d[:5], scale * (N // 5))
+    assert torch.equal(d[:5].nan_to_num(9.0), want.nan_to_num(9.0))
