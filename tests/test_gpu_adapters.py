@@ -234,3 +234,10 @@ def test_results_that_cancel_keep_their_bits(kind, ykind, N):
     dx = opd.adapter_grads(put(ykind, [long] * N), put(kind, [[0.0] * 40] * N), put(kind, ones),
                            put(kind, pick), ids, dx=put(kind, [[-1.0] * 40] * N))["dx"]
     assert (dx.double() == 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("N,r", [(40, 16), (130, 5)])
+def test_adapters_of_a_head(N, r):
+    """bf16 states and adapters, fp32 rows of a whole vocabulary: forward, and the gradients
+    from the loss's dlogits."""
+    check(batch(N, N, 136, 151_936, 3, r, "bf16", "f32"), "bf16", "f32")

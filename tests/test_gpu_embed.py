@@ -214,3 +214,17 @@ def test_entries_without_a_token_are_zeros_whatever_the_scale(N, scale):
     assert (d[5:] == 0).all() and not d[5:].signbit().any()
     want = torch.full_like(d[:5], scale * (N // 5))
     assert torch.equal(d[:5].nan_to_num(9.0), want.nan_to_num(9.0))
+
+
+@pytest.mark.parametrize("kind,out", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("first", [0, 1, 15, 16, 17])
+def test_runs_of_tokens_around_a_tile_of_16(kind, out, first):
+    """Entries of up to 16 tokens are summed by themselves, longer ones tile by tile: runs on
+    both sides of that, which begin and end at, before and past the tiles' borders."""
+    lengths = [first, 15, 16, 17, 31, 32, 33, 1, 2, 48, 16, 16, 17, 14, 18, 30]
+    ids = np.repeat(np.arange(len(lengths)), lengths).astype(np.int32)
+    assert len(ids) > 256  # (sorted)
+    np.random.default_rng(first).shuffle(ids)
+    g = torch.Generator(DEV).manual_seed(first)
+    for H in (100, 300):  # one vector to a lane, and two
+        check_grads(rows(g, len(ids), H, kind), ids, len(lengths) + 3, 1.0, out)
