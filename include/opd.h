@@ -484,7 +484,8 @@ size_t opd_verify_workspace_bytes(int64_t B, int32_t D, int64_t V, int32_t dtype
  *     overlap need one each.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N, V >= 2^31, the gradient's V > 2^31 - 512 where
  * there is a workspace, V < 1, H outside [1, 2^22], a row stride below H), OPD_ERR_PARAM
- * (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0 looks nothing up; the gradient is then zeros.
+ * (accumulate), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0 looks
+ * nothing up; the gradient is then zeros.
  */
 int opd_embed_tokens(const void* table, int32_t dtype, int64_t V, int64_t H, int64_t ld,
                      const int32_t* ids, int64_t N, float scale, void* out, int32_t out_dtype,
@@ -518,14 +519,16 @@ size_t opd_embed_workspace_bytes(int64_t N, int64_t V, int64_t H);
  *     workspace: opd_adapter_workspace_bytes(...) bytes, 16-byte aligned, of any
  *     content; calls (and captured graphs) that may overlap need one each.
  * Sums are fp32, each result is rounded once.  bf16 operands are multiplied exactly; t
- * and u enter the second product to 2^-25 of themselves.  A NaN or an infinity in a token's x (dy) or in its adapter reaches
- * its own row, and its adapter's da and db; no other's.
+ * and u enter the second product to 2^-25 of themselves.  A NaN or an infinity in a
+ * token's x (dy) or in its adapter reaches its own row, and its adapter's da and db; no
+ * other's.  (An infinity among bf16 values meets the other factor's parts, of either
+ * sign: what would be infinite may then be NaN.)
  * All rows are 16-byte aligned, and read up to the next multiple of 16 bytes; what is there
  * past their end may hold anything, and is not written.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SHAPE (N > 2^24, H or O outside [1, 2^22], a row stride
  * below its row's length (or one of a or b above 2^22), strides of in-place rows that
- * differ, or a call whose launches would pass 2^32 work-items), OPD_ERR_SUPPORT (G outside [1, OPD_ADAPTERS_MAX], r outside
- * [1, OPD_RANK_MAX]), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0
+ * differ, or a call whose launches would pass 2^32 work-items), OPD_ERR_SUPPORT (G outside
+ * [1, OPD_ADAPTERS_MAX], r outside [1, OPD_RANK_MAX]), OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  N == 0
  * adds nothing; the gradients are then zeros.
  */
 #define OPD_ADAPTERS_MAX 1000
@@ -569,9 +572,9 @@ size_t opd_adapter_workspace_bytes(int64_t N, int64_t H, int64_t O, int32_t G, i
  *   `outer` slices of inner_bytes bytes, outer_stride bytes apart; states lie `stride`
  *   bytes apart, b W + w of them before the state of beam w of group b (in out: b k + j).
  *   States of out do not overlap: they lie one after the other, or their slices do (all
- *   states' first slices, then all second ones).  Any element type.  out may be states (k == W, the same strides): the states
- *   are then moved in place, and those that are their own parent stay.  It may not
- *   overlap them otherwise.
+ *   states' first slices, then all second ones).  Any element type.  out may be states
+ *   (k == W, the same strides): the states are then moved in place, and those that are
+ *   their own parent stay.  It may not overlap them otherwise.
  * Errors: OPD_ERR_DTYPE, OPD_ERR_SUPPORT (W or k outside [1, OPD_BEAM_MAX]), OPD_ERR_SHAPE,
  * OPD_ERR_ALIGN, OPD_ERR_NULL, OPD_ERR_WORKSPACE, OPD_ERR_HIP.  B == 0 is a no-op returning
  * OPD_OK.

@@ -90,8 +90,9 @@ __global__ void __launch_bounds__(kGroupThreads) k_adapt_plan(AdaptArgs a) {
 }
 
 // The same for up to kAdFew tokens, by a wavefront of each workgroup that needs them: perm
-// [kAdFew] and tiles [kAdFew] (one to a key) in LDS; the number of tiles.  64 tokens of 32
-// adapters by 4,096 columns, the call on the GPU: 9.5 us, 12.8 with a launch before for the tiles.
+// [kAdFew] and tiles [kAdFew] (one to a key) in LDS; the number of tiles.  4,096 columns, the
+// call on the GPU: 64 tokens of 32 adapters 9.6 us, 13.8 with a launch before for the tiles; 1
+// token 6.9 and 11.3.
 __device__ __forceinline__ int plan_few(const int32_t* ids, int N, int32_t G, int32_t* perm,
                                         AdTile* tiles) {
   const int lane = threadIdx.x & 63;
@@ -186,7 +187,7 @@ __device__ __forceinline__ float low_value(const LowRef& t, int64_t token, int c
 // and their sums are added in order.  A lane's operands lie along a row, and its
 // neighbours' in other rows: loaded so, an instruction touches 16 lines 16 bytes at a time,
 // which took 10 us more for 8,192 tokens by 4,096 columns and 32 ranks than rows read as they
-// lie and turned in LDS, a part of it to each wave: 24.5 us, 20 where nothing has just been
+// lie and turned in LDS, a part of it to each wave: 23.2 us, 20 where nothing has just been
 // written (reading the tokens alone takes 17.5).  RT: ranks / 16.
 constexpr int kLowThreads = 512;
 constexpr int kLowWaves = kLowThreads / 64;
@@ -473,7 +474,7 @@ __device__ __forceinline__ void store_values(char* row, int64_t c, int64_t end, 
 // to 16 ranks, the next columns of the adapter too.
 // 8,192 tokens by 4,096 columns and 32 ranks: 34.9 us, 28 at a copy's rate.  The shared
 // projection's values and the results pass the caches: kept there, they drain while the next
-// call's k_low reads, which then takes 32.7 us instead of 24.5 (and this 33.6).  Two parts of t
+// call's k_low reads, which then takes 31.8 us instead of 23.2 (and this 33.3).  Two parts of t
 // instead of three would save 0.3 us of it, 2 of 90 with 64 ranks, 10 of 141 with 128.
 // KL: ranks of a lane's operand (bf16: 4 or 8); RB: of 4 KL ranks each; READ: there is a base.
 template <class TW, class TY, int KL, int RB, bool READ>
@@ -727,7 +728,7 @@ __global__ void __launch_bounds__(kExpThreads, KL * RB <= 8 ? 4 : 2) k_expand(Ex
 // and their sums are added in order.  A lane loads eight tokens' 16 bytes and
 // transposes them; the block's r numbers come straight into the layout of the
 // second operand.  The next block's rows are on their way meanwhile.  Both sums of 8,192 tokens
-// of 4 adapters by 4,096 columns and 16 ranks: 30.2 us, where reading takes 20; a wave has two
+// of 4 adapters by 4,096 columns and 16 ranks: 29.8 us, where reading takes 20; a wave has two
 // blocks there, so little of its own overlaps.
 constexpr int kOutThreads = 512;
 constexpr int kOutWaves = kOutThreads / 64;
@@ -918,8 +919,8 @@ hipError_t low_r(const LowPair& p, hipStream_t st) {
   const int64_t tiles = p.a[0].max_tiles;
   const int splits = p.a[0].splits + p.a[1].splits;
   // 32 tokens to a workgroup read the adapter half as often, where that leaves enough of them
-  // (4,096 columns, the call: 8,192 tokens of 8 adapters 45.5 us, 46.4 with 16; 2,048 of 4 23.1,
-  // 22.3 with 16)
+  // (4,096 columns, the call: 8,192 tokens of 8 adapters 44.1 us, 44.4 with 16; 2,048 of 4 21.9,
+  // 20.6 with 16)
   if constexpr (RT <= 4) {
     if (tiles * splits >= 100) {
       const dim3 grid((unsigned)(tiles * (kAdTile / 32)), (unsigned)splits);
@@ -945,8 +946,10 @@ hipError_t expand_t(ExpandArgs a, int64_t N, hipStream_t st) {
   const int64_t span = kExpWaves * 16 * (TW::BYTES == 2 ? 8 : 4);
   const int64_t chunks = (a.D + span - 1) / span;
   // about as many workgroups as stay on the GPU at once; four times as many where tiles are of
-  // few tokens, since they differ then, and some have none: 64 tokens of 32 adapters by 151,936
-  // columns 37.7 us (as many 41.5, eight times 40.9), 8,192 of 8 by 4,096 36.1 (as many 34.9)
+  // few tokens, since they differ then, and some have none: the call of 64 tokens of 32 adapters
+  // by 151,936 columns 41.3 us (as many 44.4, eight times 44.7), of 8,192 of 8 by 4,096 67.6 (as
+  // many 66.7).  Where a tile's workgroups become few, as many are too few: 32,768 of 8 take 241
+  // us, and 207 with four times as many.
   int64_t per = (N < 16 * a.max_tiles ? 4096 : 1024) / a.max_tiles;
   a.per = (uint32_t)(per < 1 ? 1 : per < chunks ? per : chunks);
   const dim3 grid((unsigned)(a.max_tiles * a.per));

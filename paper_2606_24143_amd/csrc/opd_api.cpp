@@ -388,8 +388,8 @@ struct AdaptLayout {
   size_t start, tiles, t, u, part_x, part_y, total;
 };
 // Parts of a long axis of D columns: about 256 workgroups of 16 tokens, each
-// with 1,024 columns at least.  4,096 columns, the whole call: 1 token 7.9 us (undivided 9.1),
-// 64 of 32 adapters 11.8 (12.8); 2,048 of 4 20.0 undivided, 23.1 in four parts.
+// with 1,024 columns at least.  4,096 columns, the whole call: 1 token 6.9 us (undivided 8.3),
+// 64 of 32 adapters 9.6 (9.9); 2,048 of 4 20.6 undivided, 23.3 in four parts.
 void split_axis(int64_t groups, int64_t D, int64_t* span, int* splits) {
   int64_t s = 256 / groups, most = D / 1024;
   if (s > most) s = most;

@@ -1,4 +1,4 @@
-// Internal interface between the C-ABI layer (opd_model_api.cpp) and the kernels around
+// Internal interface between the C-ABI layer (opd_api.cpp) and the kernels around
 // the rows of logits: token embeddings, adapters, beams.  Not installed.
 #pragma once
 
@@ -8,7 +8,7 @@ namespace opd {
 
 // Token embeddings (opd_embed_tokens, opd_embed_grads).  Launches go over rows (tokens,
 // entries, tiles) times chunks of columns.
-constexpr int kEmbTile = 16;   // sorted tokens of a tile, up to 64
+constexpr int kEmbTile = 16;   // sorted tokens of a tile (a lane each: no more than 64)
 constexpr int kEmbKeys = 512;  // entries that a workgroup sorts, at most
 struct EmbedArgs {
   const void* table;      // [V, ld]
@@ -162,7 +162,7 @@ struct ReorderArgs {
   uint32_t spans;
 };
 hipError_t launch_beam(const BeamArgs& a, int in_dt, hipStream_t stream);
-// unit: 16, 4 or 1 bytes, which divide every address and stride
+// states lie at any address and stride: 16 bytes at a time, or 4 where there are many beams
 hipError_t launch_reorder(const ReorderArgs& a, hipStream_t stream);
 
 }  // namespace opd
