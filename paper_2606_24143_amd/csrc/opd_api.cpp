@@ -344,9 +344,9 @@ struct EmbedLayout {
   int64_t hp;
 };
 // Few tokens are looked for by each entry's wavefronts themselves: 64, which they load at
-// once, or up to 256 where there are few wavefronts.  256 tokens: 27.7 us unsorted and 32.7
-// sorted for 32,000 by 1,000 fp32, 415 and 357 for 151,936 by 4,096; 64: 25.6 and 32.7, 360 and
-// 358.
+// once, or up to 256 where there are few wavefronts.  256 tokens: 27.1 us unsorted and 33.1
+// sorted for 32,000 by 1,000 fp32, 411 and 362 for 151,936 by 4,096; 64: 26.2 and 33.2, 365 and
+// 360.
 bool embed_unsorted(int64_t N, int64_t V, int64_t H) {
   return N <= 64 || (N <= 256 && V * ((H + 255) / 256) <= (1 << 18));
 }
